@@ -209,6 +209,73 @@ typedef struct spla_events {
   void* stop[SPLA_NUM_PHASES];
 } spla_events;
 
+/* ------------------------------------------------------- rotary positions
+ * A rotation of the leading rot_dim coordinates of each head by angles that
+ * grow with the token's position. Pair i (0 <= i < rot_dim / 2) of a row x at
+ * position p becomes
+ *   y0 = gain (x0 cos a - x1 sin a),  y1 = gain (x1 cos a + x0 sin a),
+ * a = p w_i, with (x0, x1) the coordinates (i, i + rot_dim / 2) for
+ * SPLA_ROPE_HALF and (2 i, 2 i + 1) for SPLA_ROPE_INTERLEAVED; the
+ * coordinates from rot_dim on stay as they are. w_i = base^(-2 i / rot_dim),
+ * changed for contexts longer than the trained one by `scaling`:
+ *   NONE    w_i
+ *   LINEAR  w_i / factor (positions interpolated)
+ *   BASE    base replaced by base factor^(rot_dim / (rot_dim - 2)) (the last
+ *           pair is slowed down by factor, the first not at all)
+ *   PARTS   w_i (c + (1 - c) / factor), c = clamp((n - low) / (high - low), 0, 1)
+ *           and n = orig_len w_i / (2 pi) the turns pair i makes over the
+ *           trained length: pairs of many turns stay, pairs of few are
+ *           interpolated
+ * Angles and products are formed in fp64 (positions of a long context times
+ * w_i lose the angle in fp32), and each result is rounded to fp32, then to the
+ * element type. */
+enum { SPLA_ROPE_HALF = 0, SPLA_ROPE_INTERLEAVED = 1 };
+enum {
+  SPLA_ROPE_SCALE_NONE = 0,
+  SPLA_ROPE_SCALE_LINEAR = 1,
+  SPLA_ROPE_SCALE_BASE = 2,
+  SPLA_ROPE_SCALE_PARTS = 3
+};
+enum { SPLA_ROPE_MAX_PAIRS = 64 };
+
+typedef struct spla_rope_config {
+  int32_t head_dim;  /* 64 or 128 */
+  int32_t rot_dim;   /* rotated coordinates, even, 2 .. head_dim */
+  int32_t layout;    /* SPLA_ROPE_HALF or SPLA_ROPE_INTERLEAVED */
+  int32_t scaling;   /* SPLA_ROPE_SCALE_* */
+  double base;       /* > 1 */
+  double factor;     /* >= 1; read by LINEAR, BASE and PARTS */
+  double orig_len;   /* > 0; read by PARTS, as low and high are (low < high) */
+  double low, high;
+  double gain;       /* finite factor of every rotated coordinate (1: a rotation) */
+} spla_rope_config;
+
+/* A rotation ready for use: host memory, filled by spla_rope_init and passed
+ * by pointer to the calls, which copy what they need. */
+typedef struct spla_rope {
+  int32_t head_dim, rot_dim, layout, reserved;
+  double gain;
+  double turns[SPLA_ROPE_MAX_PAIRS]; /* w_i / (2 pi) */
+} spla_rope;
+
+/* ---------------------------------------------------- options of spla_attend
+ * Zero-filled (or a NULL pointer): every query sees the tokens up to its own. */
+typedef struct spla_attend_opts {
+  float softcap;             /* c > 0: scores x become c tanh(x / c); 0: none */
+  float reserved;
+  const float* slopes;       /* device fp32 [Hq] or NULL: slopes[m] |p - j| is
+                                subtracted from the (capped) score of the query
+                                at position p and the key at j */
+  const int32_t* first_key;  /* device int32 [n_tokens][batch] or NULL: the query
+                                sees no key before this position (documents packed
+                                into one sequence, a sliding window) */
+  const int32_t* prefix_len; /* device int32 [batch] or NULL: every query sees the
+                                keys before this position, later ones included */
+  const int32_t* n_new;      /* device int32 [batch] or NULL: the queries sequence b
+                                really has, 0 <= n_b <= n_tokens (clamped); NULL:
+                                n_tokens */
+} spla_attend_opts;
+
 /* ---------------------------------------------------------- host-only calls */
 
 /* Text of a status code (static storage). */
@@ -251,6 +318,22 @@ int32_t spla_append_workspace_bytes(const spla_config* cfg, int32_t max_new, siz
  * what 32 positions need, whichever is more. */
 int32_t spla_prefill_workspace_bytes(const spla_config* cfg, int32_t n_tokens,
                                      size_t* out_bytes);
+
+/* Fills *out from cfg; SPLA_ERR_INVALID_ARG or SPLA_ERR_UNSUPPORTED (head_dim)
+ * when cfg is not as documented at spla_rope_config. Host only. */
+int32_t spla_rope_init(const spla_rope_config* cfg, spla_rope* out);
+
+/* Device workspace that spla_append_rope needs for up to max_new tokens per
+ * sequence (host-only query). */
+int32_t spla_append_rope_workspace_bytes(const spla_config* cfg, int32_t max_new,
+                                         size_t* out_bytes);
+
+/* Device workspace that spla_attend needs for n_tokens queries per sequence
+ * (host-only query): the partial results of sequences whose keys are split over
+ * several workgroups. It does not grow monotonically with n_tokens (few queries
+ * split more). */
+int32_t spla_attend_workspace_bytes(const spla_config* cfg, int32_t n_tokens,
+                                    size_t* out_bytes);
 
 /* ---------------------------------------------------------- device calls */
 
@@ -369,6 +452,71 @@ int32_t spla_step_ex(const spla_config* cfg, const spla_cache* cache, const void
                      const void* v_new, const void* q, const float* rms_weight, void* out,
                      int32_t* sel_idx, void* workspace, size_t workspace_bytes,
                      const spla_events* events, void* stream);
+
+/* Rotates the queries and / or keys of n_tokens positions per sequence.
+ *  rope:       host, of spla_rope_init, for cfg's head_dim.
+ *  positions:  device int32 [n_tokens][batch], the position of each row; or NULL
+ *              for base + t, base = seq_lens[b] (the rows an append, step or
+ *              prefill is about to bring) or 0 when seq_lens is NULL too. Any
+ *              int32 value is a position.
+ *  q, k:       device, dtype; row (t, b) starts q_stride (k_stride) elements
+ *              after row (t, b - 1), in the order [n_tokens][batch], and holds
+ *              the Hq (Hkv) heads of d elements one after the other. NULL: not
+ *              rotated (one of the two must be given).
+ *  q_out, k_out: device, laid out alike with strides of their own; q_out = q
+ *              with the same stride rotates in place. Other overlaps of inputs
+ *              and outputs are not allowed.
+ *  transpose:  0, or 1 for the transposed map (the angles negated): the gradient
+ *              with respect to the input from the gradient with respect to the
+ *              output, and for gain = 1 the inverse rotation.
+ * Pointers are 16-byte aligned and strides multiples of 16 bytes that hold a row
+ * (SPLA_ERR_INVALID_ARG otherwise). The cfg fields read are batch, n_q_heads,
+ * n_kv_heads, head_dim and dtype. n_tokens = 0 does nothing. */
+int32_t spla_rotate(const spla_config* cfg, const spla_rope* rope, int32_t n_tokens,
+                    const int32_t* positions, const int32_t* seq_lens, const void* q,
+                    int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k,
+                    int64_t k_stride, void* k_out, int64_t k_out_stride, int32_t transpose,
+                    void* stream);
+
+/* spla_append with the rotation applied to the keys on the way: the row at
+ * position p = L_b + t (plus pos_shift[b]) is rotated, rounded to the cache
+ * dtype and appended; values are appended as they are. The result is that of
+ * spla_append of the rotated rows.
+ *  pos_shift:  device int32 [batch] or NULL (0): added to the cache position to
+ *              give the rotary position (a sequence whose oldest tokens were
+ *              dropped, or that begins in the middle of a text).
+ * The other arguments as spla_append; the workspace from
+ * spla_append_rope_workspace_bytes. Queries of the same tokens: spla_rotate. */
+int32_t spla_append_rope(const spla_config* cfg, const spla_cache* cache, const spla_rope* rope,
+                         const void* k_new, const void* v_new, int32_t max_new,
+                         const int32_t* n_new, const int32_t* pos_shift, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* Exact (dense) attention of the last n_tokens tokens of every sequence over
+ * its cache, for layers that are not sparse: the cache already holds them
+ * (spla_append, spla_append_rope), and query t of sequence b, with n_b =
+ * n_new[b] queries, stands at position p = L_b - n_b + t. One token per
+ * sequence (n_tokens = 1) is a decode step.
+ *   out = sum_j e^(x_j - lse) v_j,  lse = ln sum_j e^(x_j),
+ *   x_j = cap(s q.k_j) - slope |p - j|
+ * over the visible keys j: first_key <= j < L_b and (j <= p or j < prefix_len).
+ *  q:    device, dtype [n_tokens][batch][Hq][d].
+ *  opts: host, or NULL; the arrays it names are on the device.
+ *  out:  device, dtype [n_tokens][batch][Hq][d] (may not alias q). Rows t >= n_b
+ *        are left as they are; a query that sees no key gives zeros.
+ *  lse:  device fp32 [n_tokens][batch][Hq] or NULL (natural logarithm; -inf for a
+ *        query that sees no key).
+ *  workspace: device, at least spla_attend_workspace_bytes(cfg, n_tokens),
+ *        256-byte aligned (no preparation needed).
+ * Keys and values that a query does not see do not change its result, whatever
+ * they hold (infinities and NaN included). Sums and softmax statistics are fp32;
+ * for bf16 caches the weights e^(x_j - m) are rounded to bf16 before the product
+ * with the values. Reads the K/V rows, seq_lens and the block table of the cache;
+ * top_k, the statistics and the linear state play no part. The cache is only
+ * read. n_tokens = 0 does nothing. */
+int32_t spla_attend(const spla_config* cfg, const spla_cache* cache, int32_t n_tokens,
+                    const void* q, const spla_attend_opts* opts, void* out, float* lse,
+                    void* workspace, size_t workspace_bytes, void* stream);
 
 /* --------------------------------------------- decode without a workspace */
 

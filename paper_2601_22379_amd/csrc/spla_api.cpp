@@ -289,6 +289,104 @@ extern "C" int32_t spla_prefill(const spla_config* cfg, const spla_cache* cache,
                          nullptr, stream);
 }
 
+// ---- rotary positions and exact attention ------------------------------------
+namespace {
+
+int32_t check_rope(const spla_config* cfg, const spla_rope* r) {
+  if (!r || r->head_dim != cfg->head_dim) return SPLA_ERR_INVALID_ARG;
+  if (r->rot_dim < 2 || r->rot_dim > r->head_dim || r->rot_dim % 2 != 0)
+    return SPLA_ERR_INVALID_ARG;
+  if (r->layout != SPLA_ROPE_HALF && r->layout != SPLA_ROPE_INTERLEAVED)
+    return SPLA_ERR_INVALID_ARG;
+  return SPLA_OK;
+}
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// rows of `heads` heads at a stride of `stride` elements
+bool good_rows(const Dims& m, const void* p, int64_t stride, int heads) {
+  return p && aligned16(p) && stride >= (int64_t)heads * m.d && stride * m.elem % 16 == 0;
+}
+
+}  // namespace
+
+extern "C" int32_t spla_rotate(const spla_config* cfg, const spla_rope* rope, int32_t n_tokens,
+                               const int32_t* positions, const int32_t* seq_lens, const void* q,
+                               int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k,
+                               int64_t k_stride, void* k_out, int64_t k_out_stride,
+                               int32_t transpose, void* stream) {
+  int32_t s = spla_validate(cfg);
+  if (s != SPLA_OK) return s;
+  if ((s = check_rope(cfg, rope)) != SPLA_OK) return s;
+  if (n_tokens < 0 || (transpose != 0 && transpose != 1)) return SPLA_ERR_INVALID_ARG;
+  if (n_tokens == 0) return SPLA_OK;
+  if ((!q && !k) || (q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr))
+    return SPLA_ERR_INVALID_ARG;
+  const Dims m = spla::make_dims(*cfg);
+  if (q && (!good_rows(m, q, q_stride, m.hq) || !good_rows(m, q_out, q_out_stride, m.hq)))
+    return SPLA_ERR_INVALID_ARG;
+  if (k && (!good_rows(m, k, k_stride, m.hkv) || !good_rows(m, k_out, k_out_stride, m.hkv)))
+    return SPLA_ERR_INVALID_ARG;
+  if ((q == q_out && q_stride != q_out_stride) || (k == k_out && k_stride != k_out_stride))
+    return SPLA_ERR_INVALID_ARG;
+  const int64_t nb = m.batch;
+  const spla::RotateSet a{q, q_out, nb * q_stride, q_stride, m.d, nb * q_out_stride, q_out_stride,
+                          m.d, q ? m.hq : 0};
+  const spla::RotateSet b{k, k_out, nb * k_stride, k_stride, m.d, nb * k_out_stride, k_out_stride,
+                          m.d, k ? m.hkv : 0};
+  const spla::RotateRows rows{n_tokens, m.batch, positions, positions ? nullptr : seq_lens, nullptr,
+                              nullptr};
+  SPLA_TRY(spla::launch_rotate(m, *rope, rows, a, b, transpose != 0,
+                               static_cast<hipStream_t>(stream)));
+  return SPLA_OK;
+}
+
+extern "C" int32_t spla_append_rope(const spla_config* cfg, const spla_cache* cache,
+                                    const spla_rope* rope, const void* k_new, const void* v_new,
+                                    int32_t max_new, const int32_t* n_new,
+                                    const int32_t* pos_shift, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  int32_t s = spla_validate(cfg);
+  if (s != SPLA_OK) return s;
+  if ((s = check_cache(cfg, cache)) != SPLA_OK) return s;
+  if ((s = check_rope(cfg, rope)) != SPLA_OK) return s;
+  if (max_new < 0) return SPLA_ERR_INVALID_ARG;
+  if (max_new > cfg->max_seq_len) return SPLA_ERR_CAPACITY;
+  if (max_new == 0) return SPLA_OK;
+  if (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new)) return SPLA_ERR_INVALID_ARG;
+  const Dims m = spla::make_dims(*cfg);
+  const spla::AppendRopeWs L = spla::append_rope_ws_layout(m, max_new);
+  if ((s = check_ws(workspace, workspace_bytes, (size_t)L.total)) != SPLA_OK) return s;
+  char* ws = static_cast<char*>(workspace);
+  const int64_t s_h = (int64_t)max_new * m.d, s_b = s_h * m.hkv;
+  const spla::RotateSet set{k_new, ws + L.k_rot, m.d, s_b, s_h, m.d, s_b, s_h, m.hkv};
+  const spla::RotateRows rows{max_new, m.batch, nullptr, cache->seq_lens, pos_shift, n_new};
+  SPLA_TRY(spla::launch_rotate(m, *rope, rows, set, spla::RotateSet{}, false,
+                               static_cast<hipStream_t>(stream)));
+  return spla_append(cfg, cache, ws + L.k_rot, v_new, max_new, n_new, ws + L.append,
+                     (size_t)(L.total - L.append), stream);
+}
+
+extern "C" int32_t spla_attend(const spla_config* cfg, const spla_cache* cache, int32_t n_tokens,
+                               const void* q, const spla_attend_opts* opts, void* out, float* lse,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+  int32_t s = spla_validate(cfg);
+  if (s != SPLA_OK) return s;
+  if ((s = check_cache(cfg, cache)) != SPLA_OK) return s;
+  if (n_tokens < 0) return SPLA_ERR_INVALID_ARG;
+  if (n_tokens > cfg->max_seq_len) return SPLA_ERR_CAPACITY;
+  const spla_attend_opts o = opts ? *opts : spla_attend_opts{};
+  if (!(o.softcap >= 0.f) || o.softcap > 3.4e38f) return SPLA_ERR_INVALID_ARG;  // NaN, infinite
+  if (n_tokens == 0) return SPLA_OK;
+  if (!q || !out || out == q || !aligned16(q) || !aligned16(out)) return SPLA_ERR_INVALID_ARG;
+  const Dims m = spla::make_dims(*cfg);
+  const spla::AttendWs L = spla::attend_ws_layout(m, n_tokens);
+  if ((s = check_ws(workspace, workspace_bytes, (size_t)L.total)) != SPLA_OK) return s;
+  SPLA_TRY(spla::launch_attend(m, *cfg, *cache, n_tokens, q, o, out, lse, L,
+                               static_cast<char*>(workspace), static_cast<hipStream_t>(stream)));
+  return SPLA_OK;
+}
+
 // ---- decode without a caller workspace (callers that cannot allocate) ------
 // The decode workspace of spla_decode_noalloc: one copy of this array per
 // device, held by every GPU the library runs on until the process ends. In

@@ -129,3 +129,64 @@ extern "C" int32_t spla_prefill_workspace_bytes(const spla_config* c, int32_t n_
                                                : spla::decode_ws_layout(m).total);
   return SPLA_OK;
 }
+
+extern "C" int32_t spla_rope_init(const spla_rope_config* c, spla_rope* out) {
+  if (!c || !out) return SPLA_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128) return SPLA_ERR_UNSUPPORTED;
+  if (c->rot_dim < 2 || c->rot_dim > c->head_dim || c->rot_dim % 2 != 0)
+    return SPLA_ERR_INVALID_ARG;
+  if (c->layout != SPLA_ROPE_HALF && c->layout != SPLA_ROPE_INTERLEAVED)
+    return SPLA_ERR_INVALID_ARG;
+  if (c->scaling < SPLA_ROPE_SCALE_NONE || c->scaling > SPLA_ROPE_SCALE_PARTS)
+    return SPLA_ERR_INVALID_ARG;
+  if (!isfinite(c->base) || !(c->base > 1.0) || !isfinite(c->gain)) return SPLA_ERR_INVALID_ARG;
+  if (c->scaling != SPLA_ROPE_SCALE_NONE && (!isfinite(c->factor) || !(c->factor >= 1.0)))
+    return SPLA_ERR_INVALID_ARG;
+  if (c->scaling == SPLA_ROPE_SCALE_PARTS &&
+      (!isfinite(c->orig_len) || !(c->orig_len > 0.0) || !isfinite(c->low) || !isfinite(c->high) ||
+       !(c->low < c->high)))
+    return SPLA_ERR_INVALID_ARG;
+  const double r = c->rot_dim, two_pi = 6.283185307179586;
+  // with one pair there is no slowest pair to reach the factor: w_0 = 1 stays
+  const double base = c->scaling == SPLA_ROPE_SCALE_BASE && c->rot_dim > 2
+                          ? c->base * pow(c->factor, r / (r - 2.0))
+                          : c->base;
+  memset(out, 0, sizeof *out);
+  out->head_dim = c->head_dim;
+  out->rot_dim = c->rot_dim;
+  out->layout = c->layout;
+  out->gain = c->gain;
+  for (int i = 0; i < c->rot_dim / 2; ++i) {
+    double w = pow(base, -2.0 * i / r);
+    if (c->scaling == SPLA_ROPE_SCALE_LINEAR) w /= c->factor;
+    if (c->scaling == SPLA_ROPE_SCALE_PARTS) {
+      double keep = (c->orig_len * w / two_pi - c->low) / (c->high - c->low);
+      keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+      w *= keep + (1.0 - keep) / c->factor;
+    }
+    out->turns[i] = w / two_pi;
+  }
+  return SPLA_OK;
+}
+
+extern "C" int32_t spla_append_rope_workspace_bytes(const spla_config* c, int32_t max_new,
+                                                    size_t* out) {
+  if (!out) return SPLA_ERR_INVALID_ARG;
+  int32_t st = spla_validate(c);
+  if (st != SPLA_OK) return st;
+  if (max_new < 0) return SPLA_ERR_INVALID_ARG;
+  if (max_new > c->max_seq_len) return SPLA_ERR_CAPACITY;
+  *out = (size_t)spla::append_rope_ws_layout(spla::make_dims(*c), max_new).total;
+  return SPLA_OK;
+}
+
+extern "C" int32_t spla_attend_workspace_bytes(const spla_config* c, int32_t n_tokens,
+                                               size_t* out) {
+  if (!out) return SPLA_ERR_INVALID_ARG;
+  int32_t st = spla_validate(c);
+  if (st != SPLA_OK) return st;
+  if (n_tokens < 0) return SPLA_ERR_INVALID_ARG;
+  if (n_tokens > c->max_seq_len) return SPLA_ERR_CAPACITY;
+  *out = (size_t)spla::attend_ws_layout(spla::make_dims(*c), n_tokens).total;
+  return SPLA_OK;
+}

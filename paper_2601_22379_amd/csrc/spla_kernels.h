@@ -109,4 +109,28 @@ hipError_t launch_decode_fused_step(const Dims& m, const spla_config& cfg, const
                                     const float* rms_weight, void* out, int32_t* sel_out,
                                     const DecodeWs& ws, char* wsbase, hipStream_t st);
 
+// rotate.hip: rows x (element of head h, position t, sequence b at t s_t + b s_b
+// + h s_h) of `heads` heads rotated into y; up to two such sets in a launch (the
+// queries and the keys of the same positions)
+struct RotateSet {
+  const void* x;
+  void* y;
+  int64_t xs_t, xs_b, xs_h, ys_t, ys_b, ys_h;  // strides in elements
+  int heads;                                   // 0: no set
+};
+// position of row (t, b): positions[t batch + b], or base[b] + t + shift[b] (NULL
+// arrays count as zeros); rows t >= count[b] (count NULL: n_tokens) are left out
+struct RotateRows {
+  int n_tokens, batch;
+  const int32_t *positions, *base, *shift, *count;
+  int64_t first = 0;  // row the launch starts at (set by launch_rotate)
+};
+hipError_t launch_rotate(const Dims& m, const spla_rope& rope, const RotateRows& rows,
+                         const RotateSet& a, const RotateSet& b, bool transpose, hipStream_t st);
+
+// attend.hip: exact attention over the cache
+hipError_t launch_attend(const Dims& m, const spla_config& cfg, const spla_cache& c, int n_tokens,
+                         const void* q, const spla_attend_opts& opts, void* out, float* lse,
+                         const AttendWs& ws, char* wsbase, hipStream_t st);
+
 }  // namespace spla

@@ -405,4 +405,59 @@ SPLA_HD AppendWs append_ws_layout(const Dims& m, int max_new) {
   return w;
 }
 
+// The rotating append: the rotated keys, then the append's own workspace.
+struct AppendRopeWs {
+  int64_t k_rot;   // dtype [bh][max_new][d]
+  int64_t append;  // AppendWs
+  int64_t total;
+};
+
+SPLA_HD AppendRopeWs append_rope_ws_layout(const Dims& m, int max_new) {
+  AppendRopeWs w;
+  w.k_rot = 0;
+  w.append = align_up((int64_t)m.bh * max_new * m.d * m.elem, SPLA_WORKSPACE_ALIGN);
+  w.total = w.append + append_ws_layout(m, max_new).total;
+  return w;
+}
+
+// ---- exact attention -------------------------------------------------------
+// The query rows of a (sequence, KV head), (position t, head g of the group) =
+// t G + g, in tiles of 16 (the columns of a matrix-core tile), one workgroup per
+// tile and split of the keys.
+constexpr int kAttendRows = 16;
+constexpr int kAttendFill = 768;      // workgroups to aim for (three per compute unit)
+constexpr int kAttendMaxSplit = 128;  // workgroups that share one tile's keys at most
+constexpr int kAttendMinSteps = 4;    // 32-token steps per workgroup at least: one per wavefront
+
+struct AttendWs {
+  int n_tiles;    // row tiles per (sequence, kv head)
+  int n_split;    // workgroups that may share a tile's keys
+  int64_t part;   // f32 [bh][n_tiles][n_split][rows][d]  unnormalised outputs
+  int64_t ml;     // f32 [bh][n_tiles][n_split][rows][2]  maximum (base 2) and sum
+  int64_t n_eff;  // i32 [bh][n_tiles]  splits with a record (1: none, the output is written)
+  int64_t total;
+};
+
+SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
+  AttendWs w;
+  w.n_tiles = (int)ceil_div((int64_t)n_tokens * m.group, kAttendRows);
+  const int64_t wgs = (int64_t)m.bh * w.n_tiles;
+  int64_t n = wgs > 0 ? ceil_div(kAttendFill, wgs) : 1;
+  const int64_t most = ceil_div(m.cap, kAttendMinSteps * kSubTokens);
+  n = n < most ? n : most;
+  w.n_split = (int)(n < kAttendMaxSplit ? n : kAttendMaxSplit);
+  int64_t off = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t o = off;
+    off = align_up(off + bytes, SPLA_WORKSPACE_ALIGN);
+    return o;
+  };
+  const int64_t rec = w.n_split > 1 ? wgs * w.n_split * kAttendRows : 0;
+  w.part = take(rec * m.d * 4);
+  w.ml = take(rec * 2 * 4);
+  w.n_eff = take(w.n_split > 1 ? wgs * 4 : 0);
+  w.total = off;
+  return w;
+}
+
 }  // namespace spla

@@ -8,9 +8,11 @@ The binding fails loudly when the HIP library has not been built.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
-from ctypes import POINTER, c_float, c_int32, c_size_t, c_uint32, c_void_p
+from ctypes import (POINTER, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32,
+                    c_void_p)
 from typing import Optional, Sequence
 
 import torch
@@ -26,6 +28,9 @@ MAX_GROUP, MAX_TOP_K, MAX_BLOCKS, WORKSPACE_ALIGN = 16, 256, 32768, 256
 PHASES = {"append": 0, "score": 1, "select": 2, "sparse": 3, "merge": 4, "decode": 5,
           "linear": 6}
 NUM_PHASES = 8
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+ROPE_MAX_PAIRS = 64
 STATUS = {0: "ok", -1: "invalid argument", -2: "unsupported shape",
           -3: "capacity or library limit exceeded", -4: "workspace missing, too small or misaligned",
           -5: "HIP runtime error"}
@@ -33,10 +38,12 @@ STATUS = {0: "ok", -1: "invalid argument", -2: "unsupported shape",
 # every symbol include/spla.h declares
 HOST_EXPORTS = ["spla_status_string", "spla_phase_name", "spla_validate", "spla_cache_bytes",
                 "spla_workspace_bytes", "spla_append_workspace_bytes", "spla_decode_phase_mask",
-                "spla_prefill_workspace_bytes"]
+                "spla_prefill_workspace_bytes", "spla_rope_init",
+                "spla_append_rope_workspace_bytes", "spla_attend_workspace_bytes"]
 EXPORTS = HOST_EXPORTS + ["spla_workspace_init", "spla_reset", "spla_append", "spla_decode",
                           "spla_decode_ex", "spla_step", "spla_step_ex", "spla_prefill",
-                          "spla_prefill_ex", "spla_decode_noalloc"]
+                          "spla_prefill_ex", "spla_decode_noalloc", "spla_rotate",
+                          "spla_append_rope", "spla_attend"]
 
 
 class SplaError(RuntimeError):
@@ -64,6 +71,23 @@ class SplaEvents(ctypes.Structure):
     _fields_ = [("start", c_void_p * NUM_PHASES), ("stop", c_void_p * NUM_PHASES)]
 
 
+class SplaRopeConfig(ctypes.Structure):
+    _fields_ = [("head_dim", c_int32), ("rot_dim", c_int32), ("layout", c_int32),
+                ("scaling", c_int32), ("base", c_double), ("factor", c_double),
+                ("orig_len", c_double), ("low", c_double), ("high", c_double),
+                ("gain", c_double)]
+
+
+class SplaRope(ctypes.Structure):
+    _fields_ = [("head_dim", c_int32), ("rot_dim", c_int32), ("layout", c_int32),
+                ("reserved", c_int32), ("gain", c_double), ("turns", c_double * ROPE_MAX_PAIRS)]
+
+
+class SplaAttendOpts(ctypes.Structure):
+    _fields_ = [("softcap", c_float), ("reserved", c_float), ("slopes", c_void_p),
+                ("first_key", c_void_p), ("prefix_len", c_void_p), ("n_new", c_void_p)]
+
+
 def _declare(lib, host_only=False):
     cfgp = POINTER(SplaConfig)
     cachep = POINTER(SplaCacheStruct)
@@ -83,8 +107,24 @@ def _declare(lib, host_only=False):
     lib.spla_decode_phase_mask.argtypes = [cfgp, POINTER(c_uint32)]
     lib.spla_prefill_workspace_bytes.restype = c_int32
     lib.spla_prefill_workspace_bytes.argtypes = [cfgp, c_int32, POINTER(c_size_t)]
+    lib.spla_rope_init.restype = c_int32
+    lib.spla_rope_init.argtypes = [POINTER(SplaRopeConfig), POINTER(SplaRope)]
+    lib.spla_append_rope_workspace_bytes.restype = c_int32
+    lib.spla_append_rope_workspace_bytes.argtypes = [cfgp, c_int32, POINTER(c_size_t)]
+    lib.spla_attend_workspace_bytes.restype = c_int32
+    lib.spla_attend_workspace_bytes.argtypes = [cfgp, c_int32, POINTER(c_size_t)]
     if host_only:
         return lib
+    lib.spla_rotate.restype = c_int32
+    lib.spla_rotate.argtypes = [cfgp, POINTER(SplaRope), c_int32, c_void_p, c_void_p,
+                                c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                c_int64, c_int32, c_void_p]
+    lib.spla_append_rope.restype = c_int32
+    lib.spla_append_rope.argtypes = [cfgp, cachep, POINTER(SplaRope), c_void_p, c_void_p, c_int32,
+                                     c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.spla_attend.restype = c_int32
+    lib.spla_attend.argtypes = [cfgp, cachep, c_int32, c_void_p, POINTER(SplaAttendOpts), c_void_p,
+                                c_void_p, c_void_p, c_size_t, c_void_p]
     lib.spla_workspace_init.restype = c_int32
     lib.spla_workspace_init.argtypes = [cfgp, c_void_p, c_size_t, c_void_p]
     lib.spla_reset.restype = c_int32
@@ -190,6 +230,35 @@ def prefill_workspace_bytes(cfg: SplaConfig, n_tokens: int, library=None) -> int
     return int(n.value)
 
 
+def append_rope_workspace_bytes(cfg: SplaConfig, max_new: int, library=None) -> int:
+    n = c_size_t(0)
+    _check((library or lib()).spla_append_rope_workspace_bytes(ctypes.byref(cfg), int(max_new),
+                                                               ctypes.byref(n)),
+           "spla_append_rope_workspace_bytes")
+    return int(n.value)
+
+
+def attend_workspace_bytes(cfg: SplaConfig, n_tokens: int, library=None) -> int:
+    n = c_size_t(0)
+    _check((library or lib()).spla_attend_workspace_bytes(ctypes.byref(cfg), int(n_tokens),
+                                                          ctypes.byref(n)),
+           "spla_attend_workspace_bytes")
+    return int(n.value)
+
+
+def make_rope(head_dim, rot_dim=None, layout="half", base=10000.0, scaling="none", factor=1.0,
+              orig_len=0.0, low=1.0, high=32.0, gain=1.0, library=None) -> SplaRope:
+    """A rotation of the leading rot_dim coordinates (default: all) for rotate and append_rope.
+    layout: "half" or "interleaved"; scaling: "none", "linear", "base" or "parts"."""
+    c = SplaRopeConfig(int(head_dim), int(head_dim if rot_dim is None else rot_dim),
+                       ROPE_LAYOUTS.get(layout, layout), ROPE_SCALINGS.get(scaling, scaling),
+                       float(base), float(factor), float(orig_len), float(low), float(high),
+                       float(gain))
+    r = SplaRope()
+    _check((library or lib()).spla_rope_init(ctypes.byref(c), ctypes.byref(r)), "spla_rope_init")
+    return r
+
+
 def decode_phases(cfg: SplaConfig, library=None) -> list:
     """Names of the phases whose events spla_decode_ex records for cfg."""
     mask = c_uint32(0)
@@ -215,6 +284,69 @@ def _aligned_workspace(nbytes: int, device) -> torch.Tensor:
     t = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
     assert t.data_ptr() % WORKSPACE_ALIGN == 0
     return t
+
+
+def _on(device):
+    """A context in which `device` is the current one (the library launches there)."""
+    if device.type != "cuda" or device.index in (None, torch.cuda.current_device()):
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
+def _row_stride(x: torch.Tensor) -> int:
+    """Elements between the rows (t, b), (t, b + 1) of x [T, batch, heads, d], whose heads and
+    coordinates lie one after the other and whose rows are evenly spaced."""
+    T, b, h, d = x.shape
+    if x.is_contiguous():
+        return h * d
+    row = x.stride(1) if b > 1 else x.stride(0) if T > 1 else h * d
+    ok = x.stride(3) == 1 and (h == 1 or x.stride(2) == d)
+    if not ok or (b > 1 and T > 1 and x.stride(0) != b * row):
+        raise ValueError("rows of heads one after the other, evenly spaced, are needed")
+    return row
+
+
+def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_lens=None,
+           q_out=None, k_out=None, transpose=False):
+    """Rotates q [T, batch, Hq, d] and / or k [T, batch, Hkv, d] (or without T: one position)
+    into q_out, k_out (new tensors by default; q_out=q rotates in place) and returns the two.
+    Rows may be slices of wider ones (a fused projection's). positions int32 [T, batch];
+    without it row (t, b) stands at seq_lens[b] + t (seq_lens int32 [batch], or zeros).
+    transpose: the transposed map (the gradient)."""
+    outs, args, lead, device = [], [], None, None
+    for name, x, y, heads in (("q", q, q_out, cfg.n_q_heads), ("k", k, k_out, cfg.n_kv_heads)):
+        if x is None:
+            if y is not None:
+                raise ValueError(f"{name}_out without {name}")
+            outs.append(None)
+            args += [None, 0, None, 0]
+            continue
+        if x.shape[-2:] != (heads, cfg.head_dim) or x.dim() not in (3, 4):
+            raise ValueError(f"{name}: [T, batch, {heads}, {cfg.head_dim}] is needed")
+        if x.shape[-3] != cfg.batch or (lead is not None and x.shape[:-2] != lead):
+            raise ValueError(f"{name}: the leading dimensions do not match")
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if y.shape != x.shape or y.dtype != x.dtype or x.dtype != torch_dtype(cfg):
+            raise ValueError(f"{name}: the config's dtype, and an output of the same shape")
+        if y.device != x.device or (device is not None and x.device != device):
+            raise ValueError("tensors on different devices")
+        lead, device = x.shape[:-2], x.device
+        x4, y4 = (t if t.dim() == 4 else t[None] for t in (x, y))
+        args += [_ptr(x), _row_stride(x4), _ptr(y), _row_stride(y4)]
+        outs.append(y)
+    if lead is None:
+        raise ValueError("q or k is needed")
+    T = lead[0] if len(lead) == 2 else 1
+    for name, t, n in (("positions", positions, T * cfg.batch), ("seq_lens", seq_lens, cfg.batch)):
+        if t is not None and (t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous()
+                              or t.device != device):
+            raise ValueError(f"{name}: {n} contiguous int32 values on the rows' device")
+    with _on(device):
+        _check(lib().spla_rotate(ctypes.byref(cfg), ctypes.byref(rope), T, _ptr(positions),
+                                 _ptr(seq_lens), *args, int(bool(transpose)), _stream(device)),
+               "spla_rotate")
+    return outs[0], outs[1]
 
 
 class SplaCache:
@@ -249,6 +381,9 @@ class SplaCache:
                "spla_workspace_init")
         self._append_ws = None
         self._prefill_ws = None
+        self._rope_ws = None
+        self._attend_ws = None
+        self._outgrown = []  # workspaces that captured graphs may still name
         self._struct = SplaCacheStruct(self.k.data_ptr(), self.v.data_ptr(),
                                        self.stats.data_ptr(), self.state.data_ptr(),
                                        self.norm.data_ptr(), self.seq_lens.data_ptr(),
@@ -379,6 +514,89 @@ class SplaCache:
                                      _ptr(sel), _ptr(ws), ws.numel(), ev,
                                      _stream(self.device)), "spla_prefill")
         return out, sel
+
+    def _grown(self, ws, need):
+        """The workspace ws, or a larger one in its place."""
+        if ws is None or ws.numel() < need:
+            if ws is not None:
+                self._outgrown.append(ws)
+            ws = _aligned_workspace(need, self.device)
+        return ws
+
+    def _given(self, name, t, shape, dtype):
+        if (t.shape != shape or t.dtype != dtype or not t.is_contiguous()
+                or t.device != self.seq_lens.device):
+            raise ValueError(f"{name}: a contiguous {dtype} tensor {list(shape)} on the cache's "
+                             "device is needed")
+
+    def rotate(self, rope: SplaRope, q=None, k=None, positions=None, q_out=None, k_out=None,
+               transpose=False):
+        """rotate() of rows that stand at the positions after the tokens the cache holds (the
+        queries and keys that the next append, step or prefill brings), or at `positions`."""
+        return rotate(self.cfg, rope, q, k, positions, None if positions is not None
+                      else self.seq_lens, q_out, k_out, transpose)
+
+    def append_rope(self, rope: SplaRope, k_new: torch.Tensor, v_new: torch.Tensor,
+                    n_new: Optional[torch.Tensor] = None,
+                    pos_shift: Optional[torch.Tensor] = None):
+        """append() with the keys rotated on the way, the token that lands at position p of the
+        cache by the angles of p (+ pos_shift[b], int32 [batch])."""
+        c = self.cfg
+        if k_new.dim() != 4:
+            raise ValueError("k_new: [batch, Hkv, max_new, d] is needed")
+        max_new = int(k_new.shape[2])
+        shape = (c.batch, c.n_kv_heads, max_new, c.head_dim)
+        self._given("k_new", k_new, shape, torch_dtype(c))
+        self._given("v_new", v_new, shape, torch_dtype(c))
+        for name, t in (("n_new", n_new), ("pos_shift", pos_shift)):
+            if t is not None:
+                self._given(name, t, (c.batch,), torch.int32)
+        self._rope_ws = self._grown(self._rope_ws, append_rope_workspace_bytes(c, max_new))
+        with _on(self.device):
+            _check(lib().spla_append_rope(ctypes.byref(c), ctypes.byref(self._struct),
+                                          ctypes.byref(rope), _ptr(k_new), _ptr(v_new), max_new,
+                                          _ptr(n_new), _ptr(pos_shift), _ptr(self._rope_ws),
+                                          self._rope_ws.numel(), _stream(self.device)),
+                   "spla_append_rope")
+
+    def attend(self, q: torch.Tensor, out=None, lse=None, softcap=0.0, slopes=None,
+               first_key=None, prefix_len=None, n_new=None):
+        """Exact attention of the last T tokens of every sequence over the cache, which holds
+        them already: q [T, batch, Hq, d] (or [batch, Hq, d]: one token) -> (out, lse), lse
+        fp32 [T, batch, Hq] (natural logarithm). softcap: scores x become softcap
+        tanh(x / softcap). slopes fp32 [Hq]: slopes[m] |p - j| is subtracted. first_key int32
+        [T, batch]: the first position each query sees. prefix_len int32 [batch]: positions
+        every query sees. n_new int32 [batch]: the queries each sequence really has; the
+        rows of out and lse past them are left as they are (zeros in tensors made here)."""
+        c = self.cfg
+        if q.dim() not in (3, 4):
+            raise ValueError("q: [T, batch, Hq, d] is needed")
+        T = 1 if q.dim() == 3 else int(q.shape[0])
+        lead = tuple(q.shape[:-2])
+        self._given("q", q, (lead[:-1] if q.dim() == 4 else ()) + (c.batch, c.n_q_heads,
+                                                                   c.head_dim), torch_dtype(c))
+        new = torch.empty if n_new is None else torch.zeros
+        if out is None:
+            out = new(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = new(q.shape[:-1], dtype=torch.float32, device=q.device)
+        self._given("out", out, tuple(q.shape), q.dtype)
+        self._given("lse", lse, tuple(q.shape[:-1]), torch.float32)
+        for name, t, shape, dt in (("slopes", slopes, (c.n_q_heads,), torch.float32),
+                                   ("first_key", first_key, lead, torch.int32),
+                                   ("prefix_len", prefix_len, (c.batch,), torch.int32),
+                                   ("n_new", n_new, (c.batch,), torch.int32)):
+            if t is not None:
+                self._given(name, t, shape, dt)
+        opts = SplaAttendOpts(float(softcap), 0.0, *(
+            None if t is None else t.data_ptr() for t in (slopes, first_key, prefix_len, n_new)))
+        self._attend_ws = self._grown(self._attend_ws, attend_workspace_bytes(c, T))
+        with _on(self.device):
+            _check(lib().spla_attend(ctypes.byref(c), ctypes.byref(self._struct), T, _ptr(q),
+                                     ctypes.byref(opts), _ptr(out), _ptr(lse),
+                                     _ptr(self._attend_ws), self._attend_ws.numel(),
+                                     _stream(self.device)), "spla_attend")
+        return out, lse
 
     # ---- layout views (for checks; pure indexing) ----
     def stats_logical(self):
