@@ -9,6 +9,8 @@
 // One pass over the keys with a running maximum and sum (in base 2: x log2 e):
 // per step the scores of the tile, the new maximum, the weights e^(x - max), and
 // the outputs scaled by e^(old max - new max) before the step's product is added.
+#include <type_traits>
+
 #include "spla_device.h"
 #include "spla_kernels.h"
 #include "spla_sparse.h"
@@ -23,7 +25,7 @@ struct AttendArgs {
   const int32_t *seq_lens, *table;
   spla_attend_opts o;
   float scale;  // softmax scale
-  int n_tokens, n_tiles, n_split;
+  int n_tokens, n_tiles, n_split, rows;  // rows per tile
   int tile0;  // first row tile of this launch
   float *part, *ml;
   int32_t* n_eff;
@@ -87,6 +89,31 @@ __device__ __forceinline__ int64_t attend_slot(const AttendArgs& a, int bh, int 
   if (!a.table) return (int64_t)bh * a.m.nb_cap + blk;
   const int p = block_page(a.m, a.table, bh, blk);
   return (int64_t)(p < 0 ? 0 : p) * a.m.hkv + bh % a.m.hkv;
+}
+
+// Infinities and NaN among values that some query does not see: a zero weight
+// times such a value is NaN. They are taken out of the product, and a product of
+// marks with the queries' visibility says which queries see which: 1 for each +
+// infinity, 128 for each - infinity, 129 for each NaN (fewer than 128 per product).
+// odd_marks: the marks of a pair of bf16 values, which lose their odd ones.
+__device__ __forceinline__ uint32_t odd_marks(uint32_t& w) {
+  uint32_t fin = 0u, mark = 0u;
+#pragma unroll
+  for (int k = 0; k < 32; k += 16) {
+    const uint32_t b = (w >> k) & 0xFFFFu, mag = b & 0x7FFFu;
+    const uint32_t x = mag > 0x7F80u ? 0x4301u : b == 0x7F80u ? 0x3F80u : b == 0xFF80u ? 0x4300u : 0u;
+    mark |= x << k;
+    fin |= (mag < 0x7F80u ? b : 0u) << k;
+  }
+  w = fin;
+  return mark;
+}
+// What the values counted in n add to a sum.
+__device__ __forceinline__ float odd_sum(float n) {
+  const float neg = floorf(n * (1.f / 128.f));
+  float x = neg > 0.f ? -INFINITY : 0.f;
+  if (n - 128.f * neg > 0.f) x += INFINITY;
+  return x;
 }
 
 // ---- operands of a 32-token step on 16 x 16 tiles, straight from the cache
@@ -154,8 +181,8 @@ struct StepOps<bf16_t, D> {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[t]), p.v, c, 0, 0,
                                                    0);
   }
-  // Whether any value is infinite or NaN; finite() zeroes those, and marks() gives
-  // 1 for the values that are NaN or the infinity of the sign asked for.
+  // Whether any value is infinite or NaN; marks() are the counts of odd_marks per query
+  // for value tile t, which loses them.
   __device__ __forceinline__ bool odd() const {
     bool bad = false;
 #pragma unroll
@@ -167,32 +194,14 @@ struct StepOps<bf16_t, D> {
     }
     return bad;
   }
-  __device__ __forceinline__ floatx4 marks(int t, bool neg, const P& seen) const {
-    const uint32_t w[4] = {v[t].x, v[t].y, v[t].z, v[t].w};
-    uint32_t r[4];
+  __device__ __forceinline__ floatx4 marks(int t, const P& seen) {
+    uint32_t w[4] = {v[t].x, v[t].y, v[t].z, v[t].w}, r[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      auto one = [&](uint32_t h) {
-        const bool nan = (h & 0x7FFFu) > 0x7F80u, inf = h == (neg ? 0xFF80u : 0x7F80u);
-        return nan || inf ? 0x3F80u : 0u;
-      };
-      r[i] = one(w[i] & 0xFFFFu) | one(w[i] >> 16) << 16;
-    }
+    for (int i = 0; i < 4; ++i) r[i] = odd_marks(w[i]);
+    v[t] = make_uint4(w[0], w[1], w[2], w[3]);
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(
         __builtin_bit_cast(bf16x8, make_uint4(r[0], r[1], r[2], r[3])), seen.v,
         floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-  }
-  __device__ __forceinline__ void finite() {
-#pragma unroll
-    for (int t = 0; t < D / 16; ++t) {
-      uint32_t w[4] = {v[t].x, v[t].y, v[t].z, v[t].w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if ((w[i] & 0x7F80u) == 0x7F80u) w[i] &= 0xFFFF0000u;
-        if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] &= 0xFFFFu;
-      }
-      v[t] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
   }
 };
 
@@ -260,25 +269,21 @@ struct StepOps<float, D> {
         bad |= odd1(v[t][s].x) || odd1(v[t][s].y) || odd1(v[t][s].z) || odd1(v[t][s].w);
     return bad;
   }
-  __device__ __forceinline__ floatx4 marks(int s, bool neg, const P& seen) const {
-    auto one = [&](float x) {
+  __device__ __forceinline__ floatx4 marks(int s, const P& seen) {
+    auto one = [](float& x) {
       const uint32_t h = __float_as_uint(x);
-      return (h & 0x7FFFFFFFu) > 0x7F800000u || h == (neg ? 0xFF800000u : 0x7F800000u) ? 1.f : 0.f;
+      if (!odd1(x)) return 0.f;
+      x = 0.f;
+      return (h & 0x7FFFFFu) != 0u ? 129.f : h >> 31 ? 128.f : 1.f;
     };
     floatx4 c{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-      c = dot4(make_float4(one(v[t][s].x), one(v[t][s].y), one(v[t][s].z), one(v[t][s].w)),
-               seen.v[t], c);
+    for (int t = 0; t < 2; ++t) {
+      float4& x = v[t][s];
+      const float a = one(x.x), b = one(x.y), d = one(x.z), e = one(x.w);
+      c = dot4(make_float4(a, b, d, e), seen.v[t], c);
+    }
     return c;
-  }
-  __device__ __forceinline__ void finite() {
-    auto f = [](float x) { return odd1(x) ? 0.f : x; };
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s)
-        v[t][s] = make_float4(f(v[t][s].x), f(v[t][s].y), f(v[t][s].z), f(v[t][s].w));
   }
 };
 
@@ -392,14 +397,10 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
       const auto seen = StepOps<T, D>::pack(see);
 #pragma unroll
       for (int t = 0; t < OT; ++t) {
-        const floatx4 up = ops.marks(t, false, seen), dn = ops.marks(t, true, seen);
+        const floatx4 n = ops.marks(t, seen);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (up[i] > 0.f) o[t][i] += INFINITY;
-          if (dn[i] > 0.f) o[t][i] -= INFINITY;
-        }
+        for (int i = 0; i < 4; ++i) o[t][i] += odd_sum(n[i]);
       }
-      ops.finite();
     }
     const auto pk = StepOps<T, D>::pack(p);
 #pragma unroll
@@ -437,7 +438,7 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
     const int64_t u = (int64_t)bh * a.n_tiles + tile;
     if (split == 0 && tid == 0) a.n_eff[u] = n_eff;
     if (n_eff > 1) {
-      const int64_t rec = (u * a.n_split + split) * kAttendRows + r;
+      const int64_t rec = (u * a.n_split + split) * a.rows + r;
 #pragma unroll
       for (int e = 0; e < E; e += 4)
         *reinterpret_cast<float4*>(a.part + rec * D + c0 + e) =
@@ -449,53 +450,398 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
   attend_write<T, D>(a, attend_row(a, (int64_t)tile * kAttendRows + r, bh, L), bh, c0, y, mt, lt);
 }
 
-// Joins the records of a tile's splits; thread (row, coordinates) as above.
+// Joins the records of 16 rows of a tile's splits; thread (row, coordinates) as above.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   constexpr int E = D / 16;
   const Dims& m = a.m;
-  const int bh = (int)(blockIdx.x % (unsigned)m.bh);
-  const int tile = a.tile0 + (int)(blockIdx.x / (unsigned)m.bh);
-  const int r = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * E;
+  const int bh = (int)(blockIdx.x % (unsigned)m.bh), part = (int)(blockIdx.x / (unsigned)m.bh);
+  const int per = a.rows / 16, tile = a.tile0 + part / per;
+  const int r = part % per * 16 + (int)(threadIdx.x >> 4), c0 = (threadIdx.x & 15) * E;
   const int64_t u = (int64_t)bh * a.n_tiles + tile;
   const int n = a.n_eff[u];
   if (n <= 1) return;  // written by the pass
-  const int64_t rec0 = u * a.n_split * kAttendRows + r;
-  float mt = -INFINITY;
-  for (int x = 0; x < n; ++x) mt = fmaxf(mt, a.ml[(rec0 + x * kAttendRows) * 2]);
-  const float ref = mt == -INFINITY ? 0.f : mt;
-  float lt = 0.f, y[E];
+  const AttendRow row = attend_row(a, (int64_t)tile * a.rows + r, bh, attend_length(a, bh));
+  const int64_t rec0 = u * a.n_split * a.rows + r;
+  float mt = -INFINITY, lt = 0.f, y[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) y[e] = 0.f;
-  for (int x = 0; x < n; ++x) {
-    const int64_t rec = rec0 + x * kAttendRows;
-    const float2 h = *reinterpret_cast<const float2*>(a.ml + rec * 2);
-    const float f = __builtin_amdgcn_exp2f(h.x - ref);
-    lt = fmaf(h.y, f, lt);
+  // records eight at a time, their loads in flight together
+  for (int x0 = 0; x0 < n; x0 += 8) {
+    float2 h[8];
+    float4 v[8][E / 4];
 #pragma unroll
-    for (int e = 0; e < E; e += 4) {
-      const float4 v = *reinterpret_cast<const float4*>(a.part + rec * D + c0 + e);
-      y[e] = fmaf(v.x, f, y[e]);
-      y[e + 1] = fmaf(v.y, f, y[e + 1]);
-      y[e + 2] = fmaf(v.z, f, y[e + 2]);
-      y[e + 3] = fmaf(v.w, f, y[e + 3]);
+    for (int x = 0; x < 8; ++x) {
+      const int64_t rec = rec0 + (int64_t)min(x0 + x, n - 1) * a.rows;
+      h[x] = *reinterpret_cast<const float2*>(a.ml + rec * 2);
+#pragma unroll
+      for (int e = 0; e < E / 4; ++e)
+        v[x][e] = *reinterpret_cast<const float4*>(a.part + rec * D + c0 + 4 * e);
+    }
+    float nm = mt;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) nm = fmaxf(nm, h[x].x);
+    const float ref = nm == -INFINITY ? 0.f : nm, alpha = __builtin_amdgcn_exp2f(mt - ref);
+    mt = nm;
+    lt *= alpha;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] *= alpha;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      if (x0 + x >= n) break;
+      const float f = __builtin_amdgcn_exp2f(h[x].x - ref);
+      lt = fmaf(h[x].y, f, lt);
+#pragma unroll
+      for (int e = 0; e < E / 4; ++e) {
+        y[4 * e] = fmaf(v[x][e].x, f, y[4 * e]);
+        y[4 * e + 1] = fmaf(v[x][e].y, f, y[4 * e + 1]);
+        y[4 * e + 2] = fmaf(v[x][e].z, f, y[4 * e + 2]);
+        y[4 * e + 3] = fmaf(v[x][e].w, f, y[4 * e + 3]);
+      }
     }
   }
-  attend_write<T, D>(a, attend_row(a, (int64_t)tile * kAttendRows + r, bh,
-                                   attend_length(a, bh)), bh, c0, y, mt, lt);
+  attend_write<T, D>(a, row, bh, c0, y, mt, lt);
 }
 
-template <typename T, int D>
-static hipError_t attend_td(AttendArgs a, hipStream_t st) {
-  // a grid holds 2^32 threads: very long calls take several launches
-  const int most = (int)((1 << 22) / a.m.bh) > 0 ? (1 << 22) / a.m.bh : 1;
-  const int n_tiles = a.n_tiles;
-  for (a.tile0 = 0; a.tile0 < n_tiles; a.tile0 += most) {
-    const int n = n_tiles - a.tile0 < most ? n_tiles - a.tile0 : most;
-    const dim3 grid((unsigned)a.m.bh * (unsigned)n, (unsigned)a.n_split);
-    hipLaunchKernelGGL((attend_stream_kernel<T, D>), grid, dim3(256), 0, st, a);
-    if (a.n_split > 1)
-      hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3(grid.x), dim3(256), 0, st, a);
+// ---------------------------------------------------------------- many rows
+// bf16 calls of many query rows are bound by the matrix cores: a workgroup takes
+// 128 rows, 32 per wavefront, and its keys and values pass through LDS once for
+// all four wavefronts, 64 tokens (two steps) at a time in two buffers, copied
+// there by the loads themselves (no registers) while the tile before is used.
+//
+// v_mfma_f32_32x32x16_bf16, scores transposed (rows = tokens, columns = queries).
+// The cache's step is an operand image for this shape too: row r = 16 mt + i of
+// the score tile is the token 8 (i / 4) + 4 mt + i % 4 whose 16-byte pieces lie
+// one after the other over i, and result register 4 (2 mt + e) + b of lane half h
+// is then token 16 e + 8 h + 4 mt + b: the eight weights of (e, h) are the operand
+// of tokens 16 e + 8 h .. + 7 of the second product, whose value pieces (token
+// group 2 e + h) lie one after the other over 16 coordinates. So LDS holds the
+// cache's bytes as they are, every operand read is runs of 512 bytes, and the
+// weights never leave their lane.
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+constexpr int kTileTokens = 64;
+
+template <int D>
+struct alignas(16) TileBuf {
+  uint4 k[2][D * 4];  // two steps of 32 D elements
+  uint4 v[2][D * 4];
+};
+
+// 16 bytes per lane from src (per lane) to dst (uniform) + 16 lane, without a
+// register in between; complete when vmcnt has counted it down.
+__device__ __forceinline__ void copy_to_lds(const void* src, void* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src,
+                                   (__attribute__((address_space(3))) uint32_t*)dst, 16, 0, 0);
+}
+
+template <int D, bool CAP, bool BIAS>
+struct TilePass {
+  static constexpr int KS = D / 16, CT = D / 32;
+  bf16x8 q[KS];
+  floatx16 o[CT];
+  float ref, l;       // reference of the weights (base 2), their sum (this lane's tokens)
+  int pos, lo, hi;    // this column's query
+  float mul, cap2, slope2;
+
+  // x[16 s2 + 4 (2 mt + e) + b]: score of token 32 s2 + 16 e + 8 h + 4 mt + b
+  static __device__ __forceinline__ int token(int i, int h) {
+    return 32 * (i >> 4) + 16 * ((i >> 2) & 1) + 8 * h + 4 * ((i >> 3) & 1) + (i & 3);
+  }
+
+  __device__ __forceinline__ void step(const TileBuf<D>& buf, int t0, bool inner, bool odd,
+                                       int lane) {
+    const int r = lane & 31, h = lane >> 5;
+    // pieces of this lane's score row and of its value coordinate: coordinates 16 s
+    // + 8 h .. + 7 at + 32 s, coordinate 32 c + r, tokens 16 e + 8 h .. at + 128 c + 32 e
+    const int at_k = (r >> 4) * (D * 2) + 16 * h + (r & 15), at_v = (r >> 4) * 64 + 16 * h + (r & 15);
+    floatx16 x[2];
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      x[s2] = floatx16{};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const uint4 a = buf.k[s2][at_k + 32 * s];
+        x[s2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), q[s], x[s2],
+                                                        0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (CAP || BIAS) {
+      const float base = (float)(pos - t0);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        float y = x[i >> 4][i & 15] * mul;
+        if constexpr (CAP) y = cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.f));
+        if constexpr (BIAS) y = fmaf(-slope2, fabsf(base - (float)token(i, h)), y);
+        x[i >> 4][i & 15] = y;
+      }
+    }
+    if (!inner) {
+      const uint32_t a = (uint32_t)(t0 + 8 * h - lo), n = (uint32_t)(hi - lo);
+#pragma unroll
+      for (int i = 0; i < 32; ++i)  // lo <= token < hi
+        x[i >> 4][i & 15] = a + (uint32_t)token(i, 0) < n ? x[i >> 4][i & 15] : -INFINITY;
+    }
+    float nm = x[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) nm = fmaxf(nm, x[i >> 4][i & 15]);
+    nm = fmaxf(nm, xor32(nm));
+    if constexpr (!(CAP || BIAS)) nm *= mul;
+    // the reference moves only when a score passes it by 2^8: weights up to there
+    // are as exact in bf16 and fp32, and the outputs are scaled a few times only
+    // (each query's by its own scores, so that no query's rounding hangs on another's)
+    const bool move = nm > ref + 8.f;
+    if (__any(move)) {
+      const float alpha = move ? __builtin_amdgcn_exp2f(ref - nm) : 1.f;
+      ref = move ? nm : ref;
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[c][i] *= alpha;
+    }
+    const float rf = ref == -INFINITY ? 0.f : ref;
+    bf16x8 p[4];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float y = x[i >> 4][i & 15];
+      const float w = __builtin_amdgcn_exp2f(CAP || BIAS ? y - rf : fmaf(y, mul, -rf));
+      sum += w;
+      // weights rounded to bf16 for the product (the sum keeps fp32)
+      p[2 * (i >> 4) + ((i >> 2) & 1)][4 * ((i >> 3) & 1) + (i & 3)] = (__bf16)w;
+    }
+    l += sum;
+    __builtin_amdgcn_sched_barrier(0);
+    if (__builtin_expect(odd && !inner, 0)) {
+      odd_values(buf, t0, lane, p);
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)  // tokens 16 e .. + 15 of the tile
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const uint4 a = buf.v[e >> 1][at_v + 128 * c + 32 * (e & 1)];
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), p[e], o[c], 0,
+                                                       0, 0);
+      }
+  }
+
+  // The product of a tile with infinities or NaN among its values, some of which
+  // some query of the wavefront does not see: taken out of the product and given
+  // to the queries that see them.
+  __device__ __forceinline__ void odd_values(const TileBuf<D>& buf, int t0, int lane,
+                                             const bf16x8 (&p)[4]) {
+    const int r = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      // per query, values it sees: 1 for each + infinity, 128 for each - infinity and
+      // 129 for each NaN (at most 64 of them)
+      floatx16 seen_odd = floatx16{};
+#pragma unroll 1
+      for (int e = 0; e < 4; ++e) {
+        const uint4 v = buf.v[e >> 1][(2 * c + (r >> 4)) * 64 + (2 * (e & 1) + h) * 16 + (r & 15)];
+        uint32_t w[4] = {v.x, v.y, v.z, v.w}, u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = odd_marks(w[i]);
+        bf16x8 seen;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int t = t0 + 16 * e + 8 * h + k;
+          seen[k] = (__bf16)(t >= lo && t < hi ? 1.f : 0.f);
+        }
+        const bf16x8 pe = e == 0 ? p[0] : e == 1 ? p[1] : e == 2 ? p[2] : p[3];
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3])), pe, o[c], 0, 0, 0);
+        seen_odd = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), seen, seen_odd, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[c][i] += odd_sum(seen_odd[i]);
+      asm volatile("" : "+v"(o[c]));  // done here, before the next coordinates' counts
+    }
+  }
+};
+
+// Maximum over the 32 columns (lanes l % 32) of the wavefront.
+__device__ __forceinline__ int cols32_max(int v) {
+#pragma unroll
+  for (int s = 1; s < 32; s *= 2) v = max(v, __shfl_xor(v, s, 64));
+  return v;
+}
+
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
+  __shared__ TileBuf<D> buf0, buf1;
+  __shared__ int4 s_range[4];
+  __shared__ int s_odd[2][4];
+  const Dims& m = a.m;
+  const int bh = (int)(blockIdx.x % (unsigned)m.bh);
+  // tiles of late queries, which see the most keys, first
+  const int tile = a.n_tiles - 1 - (a.tile0 + (int)(blockIdx.x / (unsigned)m.bh));
+  const int split = (int)blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int L = attend_length(a, bh);
+  const int rr = w * 32 + (lane & 31), h = lane >> 5;  // this lane's row of the tile
+  const AttendRow row = attend_row(a, (int64_t)tile * kTileRows + rr, bh, L);
+  const bool any = row.hi > row.lo;
+  // keys of this wavefront's queries, and those that all of its (non-empty) ones see
+  const int lo_min = -cols32_max(any ? -row.lo : -INT32_MAX), hi_max = cols32_max(row.hi);
+  const int lo_max = cols32_max(any ? row.lo : 0);
+  const int hi_min = -cols32_max(any ? -row.hi : -INT32_MAX);
+  if (lane == 0) s_range[w] = make_int4(lo_min, hi_max, lo_max, hi_min);
+  __syncthreads();
+  int4 g = s_range[0];  // of the workgroup's
+#pragma unroll
+  for (int i = 1; i < 4; ++i) {
+    const int4 x = s_range[i];
+    g = make_int4(min(g.x, x.x), max(g.y, x.y), max(g.z, x.z), min(g.w, x.w));
+  }
+  const int g_lo = __builtin_amdgcn_readfirstlane(g.x), g_hi = __builtin_amdgcn_readfirstlane(g.y);
+  const int g_lo_max = __builtin_amdgcn_readfirstlane(g.z);
+  const int g_hi_min = __builtin_amdgcn_readfirstlane(g.w);
+  const int step0 = g_hi > 0 ? g_lo / 32 : 0;
+  const int step_end = g_hi > 0 ? (g_hi + 31) / 32 : 0;
+  const int n_kt = (step_end - step0 + 1) / 2;  // tiles of keys
+  const int per = max((n_kt + a.n_split - 1) / a.n_split, kTileMinSplit);
+  const int n_eff = (n_kt + per - 1) / per;
+  if (split > 0 && split >= n_eff) return;
+  const int first = split * per, last = min(first + per, n_kt);
+
+  TilePass<D, CAP, BIAS> ps;
+  const int64_t qrow = row.valid ? ((int64_t)row.t * m.batch + bh / m.hkv) * m.hq + row.head : 0;
+  const bf16_t* qp = static_cast<const bf16_t*>(a.q) + qrow * D + 8 * h;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    uint4 x = *reinterpret_cast<const uint4*>(qp + 16 * s);
+    if (!row.valid) x = make_uint4(0u, 0u, 0u, 0u);
+    ps.q[s] = __builtin_bit_cast(bf16x8, x);
+  }
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) ps.o[c] = floatx16{};
+  const ScoreMap map(a, row.valid ? row.head : 0);
+  ps.mul = map.mul;
+  ps.cap2 = map.cap2;
+  ps.slope2 = map.slope2;
+  ps.ref = -INFINITY;
+  ps.l = 0.f;
+  ps.pos = row.pos;
+  ps.lo = row.lo;
+  ps.hi = row.hi;
+
+  // wavefront w copies pieces w, w + 4, ... (1 KiB each) of the tile's two key
+  // steps and two value steps; a step past the last is the last again (masked)
+  const int sh = m.B == 32 ? 0 : m.B == 64 ? 1 : 2;  // log2 of the steps per block
+  auto load = [&](TileBuf<D>& buf, int kt) {
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      const int st = min(step0 + 2 * kt + s2, step_end - 1);
+      const int64_t o = (attend_slot(a, bh, st >> sh) * m.B + (st & ((1 << sh) - 1)) * 32) * D;
+      const char* kp = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.k) + o) + lane * 16;
+      const char* vp = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.v) + o) + lane * 16;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const int pc = w + 4 * i;
+        copy_to_lds(kp + pc * 1024, &buf.k[s2][pc * 64]);
+        copy_to_lds(vp + pc * 1024, &buf.v[s2][pc * 64]);
+      }
+    }
+  };
+  auto use = [&](TileBuf<D>& buf, TileBuf<D>& other, int kt, int par) {
+    const int t0 = (step0 + 2 * kt) * 32;
+    wait_memory();  // this wavefront's copies of tile kt are in LDS
+    // values that some query may not see (the same for all wavefronts): every
+    // wavefront looks through the pieces it copied
+    const bool g_inner = t0 >= g_lo_max && t0 + kTileTokens <= g_hi_min;
+    if (!g_inner) {
+      uint32_t bad = 0u;
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          const uint4 v = buf.v[s2][(w + 4 * i) * 64 + lane];
+          const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            bad |= ((x[k] & 0x7F80u) == 0x7F80u || (x[k] & 0x7F800000u) == 0x7F800000u) ? 1u : 0u;
+        }
+      const bool one = __any(bad != 0u);
+      if (lane == 0) s_odd[par][w] = one;
+    }
+    __syncthreads();
+    if (kt + 1 < last) load(other, kt + 1);
+    if (t0 >= hi_max || t0 + kTileTokens <= lo_min) return;  // nothing here for this wavefront
+    const bool inner = t0 >= lo_max && t0 + kTileTokens <= hi_min;
+    const bool odd = !inner && (s_odd[par][0] | s_odd[par][1] | s_odd[par][2] | s_odd[par][3]);
+    ps.step(buf, t0, inner, odd, lane);
+  };
+  if (first < last) load(buf0, first);
+#pragma unroll 1
+  for (int kt = first; kt < last; kt += 2) {
+    use(buf0, buf1, kt, 0);
+    if (kt + 1 < last) use(buf1, buf0, kt + 1, 1);
+  }
+
+  const float l = ps.l + xor32(ps.l);
+  const int64_t u = (int64_t)bh * a.n_tiles + tile;
+  if (a.n_split > 1 && split == 0 && tid == 0) a.n_eff[u] = n_eff;
+  if (n_eff > 1) {  // (only where the keys may be split)
+    const int64_t rec = (u * a.n_split + split) * kTileRows + rr;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(a.part + rec * D + 32 * c + 8 * i + 4 * h) = make_float4(
+            ps.o[c][4 * i], ps.o[c][4 * i + 1], ps.o[c][4 * i + 2], ps.o[c][4 * i + 3]);
+    if (h == 0) *reinterpret_cast<float2*>(a.ml + rec * 2) = make_float2(ps.ref, l);
+    return;
+  }
+  if (!row.valid) return;
+  const int64_t orow = ((int64_t)row.t * m.batch + bh / m.hkv) * m.hq + row.head;
+  const float inv = any ? 1.f / l : 0.f;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = any ? ps.o[c][4 * i + k] * inv : 0.f;
+      Elem<bf16_t>::store4(static_cast<bf16_t*>(a.out), orow * D + 32 * c + 8 * i + 4 * h, y);
+    }
+  if (a.lse && h == 0) a.lse[orow] = any ? (ps.ref + log2f(l)) * kLn2 : -INFINITY;
+}
+
+static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
+  const auto go = [&](auto kern, auto join) {
+    // a grid holds 2^32 threads: very long calls take several launches
+    const int most = (int)((1 << 20) / a.m.bh) > 0 ? (1 << 20) / a.m.bh : 1;
+    for (a.tile0 = 0; a.tile0 < a.n_tiles; a.tile0 += most) {
+      const int n = a.n_tiles - a.tile0 < most ? a.n_tiles - a.tile0 : most;
+      const unsigned wgs = (unsigned)a.m.bh * (unsigned)n;
+      hipLaunchKernelGGL(kern, dim3(wgs, (unsigned)a.n_split), dim3(256), 0, st, a);
+      if (a.n_split > 1)
+        hipLaunchKernelGGL(join, dim3(wgs * (unsigned)(a.rows / 16)), dim3(256), 0, st, a);
+    }
+  };
+  const bool cap = a.o.softcap > 0.f, bias = a.o.slopes != nullptr;
+  const auto tile = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    const auto join = attend_join_kernel<bf16_t, D>;
+    if (cap && bias) go(attend_tile_kernel<D, true, true>, join);
+    else if (cap) go(attend_tile_kernel<D, true, false>, join);
+    else if (bias) go(attend_tile_kernel<D, false, true>, join);
+    else go(attend_tile_kernel<D, false, false>, join);
+  };
+  if (a.rows == kTileRows) {
+    if (a.m.d == 64) tile(std::integral_constant<int, 64>{});
+    else tile(std::integral_constant<int, 128>{});
+  } else if (a.m.elem == 4) {
+    if (a.m.d == 64) go(attend_stream_kernel<float, 64>, attend_join_kernel<float, 64>);
+    else go(attend_stream_kernel<float, 128>, attend_join_kernel<float, 128>);
+  } else {
+    if (a.m.d == 64) go(attend_stream_kernel<bf16_t, 64>, attend_join_kernel<bf16_t, 64>);
+    else go(attend_stream_kernel<bf16_t, 128>, attend_join_kernel<bf16_t, 128>);
   }
   return hipGetLastError();
 }
@@ -517,12 +863,12 @@ hipError_t launch_attend(const Dims& m, const spla_config& cfg, const spla_cache
   a.n_tokens = n_tokens;
   a.n_tiles = ws.n_tiles;
   a.n_split = ws.n_split;
+  a.rows = ws.rows;
   a.tile0 = 0;
   a.part = reinterpret_cast<float*>(base + ws.part);
   a.ml = reinterpret_cast<float*>(base + ws.ml);
   a.n_eff = reinterpret_cast<int32_t*>(base + ws.n_eff);
-  if (m.elem == 4) return m.d == 64 ? attend_td<float, 64>(a, st) : attend_td<float, 128>(a, st);
-  return m.d == 64 ? attend_td<bf16_t, 64>(a, st) : attend_td<bf16_t, 128>(a, st);
+  return attend_launches(a, st);
 }
 
 }  // namespace spla

@@ -422,37 +422,49 @@ SPLA_HD AppendRopeWs append_rope_ws_layout(const Dims& m, int max_new) {
 
 // ---- exact attention -------------------------------------------------------
 // The query rows of a (sequence, KV head), (position t, head g of the group) =
-// t G + g, in tiles of 16 (the columns of a matrix-core tile), one workgroup per
-// tile and split of the keys.
+// t G + g, in tiles: of 16 rows (the columns of one matrix-core tile; keys and
+// values straight from the cache), or of 128 (through LDS, bf16 only). One
+// workgroup per tile and split of the keys.
 constexpr int kAttendRows = 16;
+constexpr int kTileRows = 128;
 constexpr int kAttendFill = 768;      // workgroups to aim for (three per compute unit)
+constexpr int kTileFill = 512;        // ... of tiles of 128 rows (two)
 constexpr int kAttendMaxSplit = 128;  // workgroups that share one tile's keys at most
 constexpr int kAttendMinSteps = 4;    // 32-token steps per workgroup at least: one per wavefront
+constexpr int kTileMinSplit = 4;      // 64-token key tiles per workgroup at least
+
+SPLA_HD bool attend_wide(const Dims& m, int n_tokens) {
+  return m.elem == 2 && (int64_t)n_tokens * m.group > 64;
+}
 
 struct AttendWs {
+  int rows;       // query rows per tile
   int n_tiles;    // row tiles per (sequence, kv head)
   int n_split;    // workgroups that may share a tile's keys
   int64_t part;   // f32 [bh][n_tiles][n_split][rows][d]  unnormalised outputs
-  int64_t ml;     // f32 [bh][n_tiles][n_split][rows][2]  maximum (base 2) and sum
+  int64_t ml;     // f32 [bh][n_tiles][n_split][rows][2]  reference (base 2) and sum of the weights
   int64_t n_eff;  // i32 [bh][n_tiles]  splits with a record (1: none, the output is written)
   int64_t total;
 };
 
 SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
   AttendWs w;
-  w.n_tiles = (int)ceil_div((int64_t)n_tokens * m.group, kAttendRows);
+  const bool wide = attend_wide(m, n_tokens);
+  w.rows = wide ? kTileRows : kAttendRows;
+  w.n_tiles = (int)ceil_div((int64_t)n_tokens * m.group, w.rows);
   const int64_t wgs = (int64_t)m.bh * w.n_tiles;
-  int64_t n = wgs > 0 ? ceil_div(kAttendFill, wgs) : 1;
-  const int64_t most = ceil_div(m.cap, kAttendMinSteps * kSubTokens);
+  int64_t n = wgs > 0 ? (wide ? kTileFill / wgs : ceil_div(kAttendFill, wgs)) : 1;
+  const int64_t most = ceil_div(m.cap, wide ? kTileMinSplit * 64 : kAttendMinSteps * kSubTokens);
   n = n < most ? n : most;
-  w.n_split = (int)(n < kAttendMaxSplit ? n : kAttendMaxSplit);
+  n = n < kAttendMaxSplit ? n : kAttendMaxSplit;
+  w.n_split = (int)(n > 1 ? n : 1);
   int64_t off = 0;
   auto take = [&](int64_t bytes) {
     const int64_t o = off;
     off = align_up(off + bytes, SPLA_WORKSPACE_ALIGN);
     return o;
   };
-  const int64_t rec = w.n_split > 1 ? wgs * w.n_split * kAttendRows : 0;
+  const int64_t rec = w.n_split > 1 ? wgs * w.n_split * w.rows : 0;
   w.part = take(rec * m.d * 4);
   w.ml = take(rec * 2 * 4);
   w.n_eff = take(w.n_split > 1 ? wgs * 4 : 0);
