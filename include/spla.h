@@ -329,9 +329,11 @@ int32_t spla_append_rope_workspace_bytes(const spla_config* cfg, int32_t max_new
                                          size_t* out_bytes);
 
 /* Device workspace that spla_attend needs for n_tokens queries per sequence
- * (host-only query): the partial results of sequences whose keys are split over
- * several workgroups. It does not grow monotonically with n_tokens (few queries
- * split more). */
+ * (host-only query): arrival counters and the partial results of sequences whose
+ * keys are split over several workgroups. It does not grow monotonically with
+ * n_tokens (few queries split more). Zero-fill the workspace once before its first
+ * use, or after other data was in it: the counters, its first bytes for every
+ * shape, must be zero when a call starts, and every call leaves them so. */
 int32_t spla_attend_workspace_bytes(const spla_config* cfg, int32_t n_tokens,
                                     size_t* out_bytes);
 
@@ -507,7 +509,7 @@ int32_t spla_append_rope(const spla_config* cfg, const spla_cache* cache, const 
  *  lse:  device fp32 [n_tokens][batch][Hq] or NULL (natural logarithm; -inf for a
  *        query that sees no key).
  *  workspace: device, at least spla_attend_workspace_bytes(cfg, n_tokens),
- *        256-byte aligned (no preparation needed).
+ *        256-byte aligned, zero-filled before its first use.
  * Keys and values that a query does not see do not change its result, whatever
  * they hold (infinities and NaN included). Sums and softmax statistics are fp32;
  * for bf16 caches the weights e^(x_j - m) are rounded to bf16 before the product

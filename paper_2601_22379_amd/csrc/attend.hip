@@ -28,8 +28,12 @@ struct AttendArgs {
   int n_tokens, n_tiles, n_split, rows;  // rows per tile
   int tile0;  // first row tile of this launch
   float *part, *ml;
-  int32_t* n_eff;
+  int32_t *n_eff, *count;
 };
+
+__device__ __forceinline__ uint64_t pack_f32x2(float a, float b) {
+  return __float_as_uint(a) | (uint64_t)__float_as_uint(b) << 32;
+}
 
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -133,13 +137,10 @@ struct StepOps<bf16_t, D> {
   bf16x8 q[KS];
   uint4 k[2][KS], v[D / 16];
   static __device__ __forceinline__ int token(int a, int i) { return 8 * a + i; }
-  __device__ __forceinline__ void load_q(const bf16_t* row, int g, bool ok) {
+  __device__ __forceinline__ void load_q(const bf16_t* row, int g) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      uint4 x = *reinterpret_cast<const uint4*>(row + 32 * s + 8 * g);
-      if (!ok) x = make_uint4(0u, 0u, 0u, 0u);
-      q[s] = __builtin_bit_cast(bf16x8, x);
-    }
+    for (int s = 0; s < KS; ++s)
+      q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + 32 * s + 8 * g));
   }
   // k, v: the buffers; slot of the block, step tb / 32 of it
   __device__ __forceinline__ void load_kv(const Dims& m, const void* kc, const void* vc,
@@ -212,12 +213,9 @@ struct StepOps<float, D> {
   static __device__ __forceinline__ int token(int a, int i) {
     return 16 * (i >> 2) + 4 * a + (i & 3);
   }
-  __device__ __forceinline__ void load_q(const float* row, int g, bool ok) {
+  __device__ __forceinline__ void load_q(const float* row, int g) {
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      q[s] = *reinterpret_cast<const float4*>(row + 16 * s + 4 * g);
-      if (!ok) q[s] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
+    for (int s = 0; s < D / 16; ++s) q[s] = *reinterpret_cast<const float4*>(row + 16 * s + 4 * g);
   }
   __device__ __forceinline__ void load_kv(const Dims& m, const void* kc, const void* vc,
                                           int64_t slot, int tb, int lane) {
@@ -320,10 +318,20 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
   constexpr int OT = D / 16;
   __shared__ float s_m[4][16], s_l[4][16];
   __shared__ __align__(16) float s_o[4][16][D + 4];
+  __shared__ int s_last;
   const Dims& m = a.m;
   const int bh = (int)(blockIdx.x % (unsigned)m.bh);
   const int tile = a.tile0 + (int)(blockIdx.x / (unsigned)m.bh), split = (int)blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, j = lane & 15, g = lane >> 4;
+  // the queries first: their loads wait for nothing. A column past the call's rows
+  // reads its last one: the columns of a product are independent of each other
+  StepOps<T, D> ops;
+  {
+    const int64_t r = min((int64_t)tile * kAttendRows + j, (int64_t)a.n_tokens * m.group - 1);
+    const int64_t t = r / m.group;
+    ops.load_q(static_cast<const T*>(a.q) + ((t * m.batch + bh / m.hkv) * m.hq +
+               (bh % m.hkv) * m.group + (r - t * m.group)) * D, g);
+  }
   const int L = attend_length(a, bh);
   const AttendRow row = attend_row(a, (int64_t)tile * kAttendRows + j, bh, L);
   const bool any = row.hi > row.lo;
@@ -337,19 +345,18 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
   if (split > 0 && split >= n_eff) return;
   const int first = step0 + split * per, last = min(first + per, step0 + n_steps);
 
-  StepOps<T, D> ops;
-  // (a row past the call's queries reads the first one's)
-  const int64_t qrow = row.valid ? ((int64_t)row.t * m.batch + bh / m.hkv) * m.hq + row.head : 0;
-  ops.load_q(static_cast<const T*>(a.q) + qrow * D, g, row.valid);
   const ScoreMap map(a, row.valid ? row.head : 0);
   float mx = -INFINITY, l = 0.f;
   floatx4 o[OT];
 #pragma unroll
   for (int t = 0; t < OT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const int spb = m.B / 32;  // steps per block
+  const int sh = m.B == 32 ? 0 : m.B == 64 ? 1 : 2;  // log2 of the steps per block
+  // the next step's page is looked up while this one's rows are used
+  int64_t slot = first + w < last ? attend_slot(a, bh, (first + w) >> sh) : 0;
   for (int st = first + w; st < last; st += 4) {
     const int t0 = st * 32;
-    ops.load_kv(m, a.k, a.v, attend_slot(a, bh, st / spb), (st % spb) * 32, lane);
+    ops.load_kv(m, a.k, a.v, slot, (st & ((1 << sh) - 1)) * 32, lane);
+    if (st + 4 < last) slot = attend_slot(a, bh, (st + 4) >> sh);
     float x[8];
     ops.scores(x);
 #pragma unroll
@@ -434,24 +441,92 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
 #pragma unroll
     for (int e = 0; e < E; ++e) y[e] = fmaf(s_o[x][r][c0 + e], f, y[e]);
   }
-  if (a.n_split > 1) {
-    const int64_t u = (int64_t)bh * a.n_tiles + tile;
-    if (split == 0 && tid == 0) a.n_eff[u] = n_eff;
-    if (n_eff > 1) {
-      const int64_t rec = (u * a.n_split + split) * a.rows + r;
+  const AttendRow out_row = attend_row(a, (int64_t)tile * kAttendRows + r, bh, L);
+  if (n_eff <= 1) {
+    attend_write<T, D>(a, out_row, bh, c0, y, mt, lt);
+    return;
+  }
+  // the tile's last workgroup to arrive joins the records of all (device-coherent:
+  // other workgroups of this launch wrote them), in the order of the splits
+  const int64_t u = (int64_t)bh * a.n_tiles + tile, rec0 = u * a.n_split * kAttendRows;
+  if (out_row.valid) {
+    const int64_t rec = rec0 + (int64_t)split * kAttendRows + r;
 #pragma unroll
-      for (int e = 0; e < E; e += 4)
-        *reinterpret_cast<float4*>(a.part + rec * D + c0 + e) =
-            make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
-      if (c0 == 0) *reinterpret_cast<float2*>(a.ml + rec * 2) = make_float2(mt, lt);
-      return;
+    for (int e = 0; e < E; e += 2)
+      Mem<true>::st(reinterpret_cast<uint64_t*>(a.part + rec * D + c0 + e), pack_f32x2(y[e], y[e + 1]));
+    if (c0 == 0) Mem<true>::st(reinterpret_cast<uint64_t*>(a.ml + rec * 2), pack_f32x2(mt, lt));
+  }
+  int32_t* ctr = a.count + u * kSyncLine;
+  if (!arrive_last(ctr, n_eff, &s_last)) return;
+  if (tid == 0) store_agent(ctr, 0);  // zero again for the next call
+  // the valid rows are the first ones: R of them (a power of two) by 16 threads
+  // each, in P = 16 / R parts that take every P-th record
+  const int nv = __popcll(__ballot(row.valid && lane < 16));
+  int R = 1;
+  while (R < nv) R *= 2;
+  const int P = 16 / R, p = tid / (16 * R), jr = (tid >> 4) % R;
+  float jm = -INFINITY, jl = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] = 0.f;
+  for (int x0 = p; x0 < n_eff; x0 += 8 * P) {  // eight records in flight
+    float2 hd[8];
+    float4 v[8][E / 4];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const int64_t rec = rec0 + (int64_t)min(x0 + x * P, n_eff - 1) * kAttendRows + jr;
+      hd[x] = Mem<true>::ld2(a.ml + rec * 2);
+#pragma unroll
+      for (int e = 0; e < E / 4; ++e) v[x][e] = Mem<true>::ld4(a.part + rec * D + c0 + 4 * e);
+    }
+    float nm = jm;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) nm = fmaxf(nm, hd[x].x);
+    const float rf = nm == -INFINITY ? 0.f : nm, alpha = __builtin_amdgcn_exp2f(jm - rf);
+    jm = nm;
+    jl *= alpha;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] *= alpha;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      if (x0 + x * P >= n_eff) break;
+      const float f = __builtin_amdgcn_exp2f(hd[x].x - rf);
+      jl = fmaf(hd[x].y, f, jl);
+#pragma unroll
+      for (int e = 0; e < E / 4; ++e) {
+        y[4 * e] = fmaf(v[x][e].x, f, y[4 * e]);
+        y[4 * e + 1] = fmaf(v[x][e].y, f, y[4 * e + 1]);
+        y[4 * e + 2] = fmaf(v[x][e].z, f, y[4 * e + 2]);
+        y[4 * e + 3] = fmaf(v[x][e].w, f, y[4 * e + 3]);
+      }
     }
   }
-  attend_write<T, D>(a, attend_row(a, (int64_t)tile * kAttendRows + r, bh, L), bh, c0, y, mt, lt);
+  if (P > 1) {  // uniform
+    if ((tid & 15) == 0) {
+      s_m[0][p * R + jr] = jm;
+      s_l[0][p * R + jr] = jl;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_o[0][p * R + jr][c0 + e] = y[e];
+    __syncthreads();
+    if (p > 0) return;
+    for (int x = 1; x < P; ++x) jm = fmaxf(jm, s_m[0][x * R + jr]);
+    const float rf = jm == -INFINITY ? 0.f : jm;
+    jl = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = 0.f;
+    for (int x = 0; x < P; ++x) {
+      const float f = __builtin_amdgcn_exp2f(s_m[0][x * R + jr] - rf);
+      jl = fmaf(s_l[0][x * R + jr], f, jl);
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = fmaf(s_o[0][x * R + jr][c0 + e], f, y[e]);
+    }
+  }
+  attend_write<T, D>(a, attend_row(a, (int64_t)tile * kAttendRows + jr, bh, L), bh, c0, y, jm, jl);
 }
 
-// Joins the records of 16 rows of a tile's splits; thread (row, coordinates) as above.
-template <typename T, int D>
+// Joins the records of 16 rows of a tile's splits (tiles of 128 rows); thread (row,
+// coordinates) as above.
+template <int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   constexpr int E = D / 16;
   const Dims& m = a.m;
@@ -500,7 +575,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
       }
     }
   }
-  attend_write<T, D>(a, row, bh, c0, y, mt, lt);
+  attend_write<bf16_t, D>(a, row, bh, c0, y, mt, lt);
 }
 
 // ---------------------------------------------------------------- many rows
@@ -813,21 +888,22 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
 }
 
 static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
-  const auto go = [&](auto kern, auto join) {
+  using Kernel = void (*)(AttendArgs);
+  const auto go = [&](Kernel kern, Kernel join = nullptr) {
     // a grid holds 2^32 threads: very long calls take several launches
     const int most = (int)((1 << 20) / a.m.bh) > 0 ? (1 << 20) / a.m.bh : 1;
     for (a.tile0 = 0; a.tile0 < a.n_tiles; a.tile0 += most) {
       const int n = a.n_tiles - a.tile0 < most ? a.n_tiles - a.tile0 : most;
       const unsigned wgs = (unsigned)a.m.bh * (unsigned)n;
       hipLaunchKernelGGL(kern, dim3(wgs, (unsigned)a.n_split), dim3(256), 0, st, a);
-      if (a.n_split > 1)
+      if (a.n_split > 1 && join)
         hipLaunchKernelGGL(join, dim3(wgs * (unsigned)(a.rows / 16)), dim3(256), 0, st, a);
     }
   };
   const bool cap = a.o.softcap > 0.f, bias = a.o.slopes != nullptr;
   const auto tile = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    const auto join = attend_join_kernel<bf16_t, D>;
+    const auto join = attend_join_kernel<D>;
     if (cap && bias) go(attend_tile_kernel<D, true, true>, join);
     else if (cap) go(attend_tile_kernel<D, true, false>, join);
     else if (bias) go(attend_tile_kernel<D, false, true>, join);
@@ -837,11 +913,11 @@ static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
     if (a.m.d == 64) tile(std::integral_constant<int, 64>{});
     else tile(std::integral_constant<int, 128>{});
   } else if (a.m.elem == 4) {
-    if (a.m.d == 64) go(attend_stream_kernel<float, 64>, attend_join_kernel<float, 64>);
-    else go(attend_stream_kernel<float, 128>, attend_join_kernel<float, 128>);
+    if (a.m.d == 64) go(attend_stream_kernel<float, 64>);
+    else go(attend_stream_kernel<float, 128>);
   } else {
-    if (a.m.d == 64) go(attend_stream_kernel<bf16_t, 64>, attend_join_kernel<bf16_t, 64>);
-    else go(attend_stream_kernel<bf16_t, 128>, attend_join_kernel<bf16_t, 128>);
+    if (a.m.d == 64) go(attend_stream_kernel<bf16_t, 64>);
+    else go(attend_stream_kernel<bf16_t, 128>);
   }
   return hipGetLastError();
 }
@@ -868,6 +944,7 @@ hipError_t launch_attend(const Dims& m, const spla_config& cfg, const spla_cache
   a.part = reinterpret_cast<float*>(base + ws.part);
   a.ml = reinterpret_cast<float*>(base + ws.ml);
   a.n_eff = reinterpret_cast<int32_t*>(base + ws.n_eff);
+  a.count = reinterpret_cast<int32_t*>(base);
   return attend_launches(a, st);
 }
 

@@ -441,9 +441,12 @@ struct AttendWs {
   int rows;       // query rows per tile
   int n_tiles;    // row tiles per (sequence, kv head)
   int n_split;    // workgroups that may share a tile's keys
+  // the arrival counters of split tiles of 16 rows lie first, one per line, wherever
+  // the rest ends: zero between calls of any shape (i32 [kAttendFill][kSyncLine])
   int64_t part;   // f32 [bh][n_tiles][n_split][rows][d]  unnormalised outputs
   int64_t ml;     // f32 [bh][n_tiles][n_split][rows][2]  reference (base 2) and sum of the weights
-  int64_t n_eff;  // i32 [bh][n_tiles]  splits with a record (1: none, the output is written)
+  int64_t n_eff;  // i32 [bh][n_tiles]  tiles of 128 rows: splits with a record (1: none, the
+                  //   output is written)
   int64_t total;
 };
 
@@ -465,9 +468,10 @@ SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
     return o;
   };
   const int64_t rec = w.n_split > 1 ? wgs * w.n_split * w.rows : 0;
+  if (rec) take((int64_t)kAttendFill * kSyncLine * 4);  // (split tiles are fewer than that)
   w.part = take(rec * m.d * 4);
   w.ml = take(rec * 2 * 4);
-  w.n_eff = take(w.n_split > 1 ? wgs * 4 : 0);
+  w.n_eff = take(rec && wide ? wgs * 4 : 0);
   w.total = off;
   return w;
 }

@@ -289,8 +289,11 @@ def _aligned_workspace(nbytes: int, device) -> torch.Tensor:
 def _on(device):
     """A context in which `device` is the current one (the library launches there)."""
     if device.type != "cuda" or device.index in (None, torch.cuda.current_device()):
-        return contextlib.nullcontext()
+        return _HERE_ALREADY
     return torch.cuda.device(device)
+
+
+_HERE_ALREADY = contextlib.nullcontext()
 
 
 def _row_stride(x: torch.Tensor) -> int:
@@ -516,11 +519,11 @@ class SplaCache:
         return out, sel
 
     def _grown(self, ws, need):
-        """The workspace ws, or a larger one in its place."""
+        """The workspace ws, or a larger one in its place (zeros: its counters)."""
         if ws is None or ws.numel() < need:
             if ws is not None:
                 self._outgrown.append(ws)
-            ws = _aligned_workspace(need, self.device)
+            ws = _aligned_workspace(need, self.device).zero_()
         return ws
 
     def _given(self, name, t, shape, dtype):
