@@ -286,27 +286,51 @@ def _aligned_workspace(nbytes: int, device) -> torch.Tensor:
     return t
 
 
-def _on(device):
-    """A context in which `device` is the current one (the library launches there)."""
-    if device.type != "cuda" or device.index in (None, torch.cuda.current_device()):
-        return _HERE_ALREADY
-    return torch.cuda.device(device)
+# The handle of a device's current stream by its index: torch's own short cut for launchers,
+# where it has one (a Stream object costs 2 us, a third of a small call).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-_HERE_ALREADY = contextlib.nullcontext()
+def _launch(fn, where, device, args):
+    """fn(*args, current stream of device), with that device the current one."""
+    index = device.index
+    if index is None or index == torch.cuda.current_device():
+        status = fn(*args, _raw_stream(torch.cuda.current_device()))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
+    if status != 0:
+        raise SplaError(status, where)
 
 
 def _row_stride(x: torch.Tensor) -> int:
-    """Elements between the rows (t, b), (t, b + 1) of x [T, batch, heads, d], whose heads and
-    coordinates lie one after the other and whose rows are evenly spaced."""
-    T, b, h, d = x.shape
+    """Elements between the rows (t, b), (t, b + 1) of x [T, batch, heads, d] or [batch, heads,
+    d], whose heads and coordinates lie one after the other and whose rows are evenly spaced."""
+    b, h, d = x.shape[-3:]
     if x.is_contiguous():
         return h * d
-    row = x.stride(1) if b > 1 else x.stride(0) if T > 1 else h * d
-    ok = x.stride(3) == 1 and (h == 1 or x.stride(2) == d)
+    T = x.shape[0] if x.dim() == 4 else 1
+    row = x.stride(-3) if b > 1 else x.stride(0) if T > 1 else h * d
+    ok = x.stride(-1) == 1 and (h == 1 or x.stride(-2) == d)
     if not ok or (b > 1 and T > 1 and x.stride(0) != b * row):
         raise ValueError("rows of heads one after the other, evenly spaced, are needed")
     return row
+
+
+def _rows(name, x, y, lead, heads, cfg, dtype, device):
+    """y, or a new output of the rows x [*lead, heads, d]; both checked."""
+    shape = x.shape
+    if shape[:-2] != lead or shape[-2:] != (heads, cfg.head_dim) or x.dtype is not dtype:
+        raise ValueError(f"{name}: a {dtype} tensor [T, {cfg.batch}, {heads}, {cfg.head_dim}] is "
+                         "needed, T the same for q and k")
+    if y is None:
+        y = torch.empty(shape, dtype=dtype, device=device)
+    elif y.shape != shape or y.dtype is not dtype:
+        raise ValueError(f"{name}_out: a {dtype} tensor of {name}'s shape is needed")
+    if x.device != device or y.device != device:
+        raise ValueError("tensors on different devices")
+    return y
 
 
 def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_lens=None,
@@ -316,40 +340,33 @@ def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_
     Rows may be slices of wider ones (a fused projection's). positions int32 [T, batch];
     without it row (t, b) stands at seq_lens[b] + t (seq_lens int32 [batch], or zeros).
     transpose: the transposed map (the gradient)."""
-    outs, args, lead, device = [], [], None, None
-    for name, x, y, heads in (("q", q, q_out, cfg.n_q_heads), ("k", k, k_out, cfg.n_kv_heads)):
-        if x is None:
-            if y is not None:
-                raise ValueError(f"{name}_out without {name}")
-            outs.append(None)
-            args += [None, 0, None, 0]
-            continue
-        if x.shape[-2:] != (heads, cfg.head_dim) or x.dim() not in (3, 4):
-            raise ValueError(f"{name}: [T, batch, {heads}, {cfg.head_dim}] is needed")
-        if x.shape[-3] != cfg.batch or (lead is not None and x.shape[:-2] != lead):
-            raise ValueError(f"{name}: the leading dimensions do not match")
-        if y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if y.shape != x.shape or y.dtype != x.dtype or x.dtype != torch_dtype(cfg):
-            raise ValueError(f"{name}: the config's dtype, and an output of the same shape")
-        if y.device != x.device or (device is not None and x.device != device):
-            raise ValueError("tensors on different devices")
-        lead, device = x.shape[:-2], x.device
-        x4, y4 = (t if t.dim() == 4 else t[None] for t in (x, y))
-        args += [_ptr(x), _row_stride(x4), _ptr(y), _row_stride(y4)]
-        outs.append(y)
-    if lead is None:
-        raise ValueError("q or k is needed")
+    x = k if q is None else q
+    if x is None or (q is None and q_out is not None) or (k is None and k_out is not None):
+        raise ValueError("q or k is needed, and no output without its input")
+    lead, device, dtype = x.shape[:-2], x.device, torch_dtype(cfg)
+    if len(lead) not in (1, 2) or lead[-1] != cfg.batch:
+        raise ValueError(f"rows of [T, {cfg.batch}] or [{cfg.batch}] positions are needed")
     T = lead[0] if len(lead) == 2 else 1
+    qp = qs = op = os_ = kp = ks = tp = ts = 0
+    if q is not None:
+        q_out = _rows("q", q, q_out, lead, cfg.n_q_heads, cfg, dtype, device)
+        qp, qs, op, os_ = q.data_ptr(), _row_stride(q), q_out.data_ptr(), _row_stride(q_out)
+    if k is not None:
+        k_out = _rows("k", k, k_out, lead, cfg.n_kv_heads, cfg, dtype, device)
+        kp, ks, tp, ts = k.data_ptr(), _row_stride(k), k_out.data_ptr(), _row_stride(k_out)
+    at = []
     for name, t, n in (("positions", positions, T * cfg.batch), ("seq_lens", seq_lens, cfg.batch)):
-        if t is not None and (t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous()
-                              or t.device != device):
+        if t is None:
+            at.append(None)
+            continue
+        if (t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous()
+                or t.device != device):
             raise ValueError(f"{name}: {n} contiguous int32 values on the rows' device")
-    with _on(device):
-        _check(lib().spla_rotate(ctypes.byref(cfg), ctypes.byref(rope), T, _ptr(positions),
-                                 _ptr(seq_lens), *args, int(bool(transpose)), _stream(device)),
-               "spla_rotate")
-    return outs[0], outs[1]
+        at.append(t.data_ptr())
+    _launch(lib().spla_rotate, "spla_rotate", device,
+            (ctypes.byref(cfg), ctypes.byref(rope), T, at[0], at[1], qp, qs, op, os_, kp, ks, tp,
+             ts, 1 if transpose else 0))
+    return q_out, k_out
 
 
 class SplaCache:
@@ -387,6 +404,7 @@ class SplaCache:
         self._rope_ws = None
         self._attend_ws = None
         self._outgrown = []  # workspaces that captured graphs may still name
+        self._ws_sizes = {}
         self._struct = SplaCacheStruct(self.k.data_ptr(), self.v.data_ptr(),
                                        self.stats.data_ptr(), self.state.data_ptr(),
                                        self.norm.data_ptr(), self.seq_lens.data_ptr(),
@@ -518,8 +536,12 @@ class SplaCache:
                                      _stream(self.device)), "spla_prefill")
         return out, sel
 
-    def _grown(self, ws, need):
-        """The workspace ws, or a larger one in its place (zeros: its counters)."""
+    def _workspace(self, kind, n, sizes, ws):
+        """The workspace ws, or a larger one in its place (zeros: its counters), for a call of
+        n tokens; the sizes of earlier calls are remembered."""
+        need = self._ws_sizes.get((kind, n))
+        if need is None:
+            need = self._ws_sizes[kind, n] = sizes(self.cfg, n)
         if ws is None or ws.numel() < need:
             if ws is not None:
                 self._outgrown.append(ws)
@@ -527,10 +549,12 @@ class SplaCache:
         return ws
 
     def _given(self, name, t, shape, dtype):
-        if (t.shape != shape or t.dtype != dtype or not t.is_contiguous()
+        """The address of t, checked."""
+        if (t.shape != shape or t.dtype is not dtype or not t.is_contiguous()
                 or t.device != self.seq_lens.device):
             raise ValueError(f"{name}: a contiguous {dtype} tensor {list(shape)} on the cache's "
                              "device is needed")
+        return t.data_ptr()
 
     def rotate(self, rope: SplaRope, q=None, k=None, positions=None, q_out=None, k_out=None,
                transpose=False):
@@ -547,20 +571,18 @@ class SplaCache:
         c = self.cfg
         if k_new.dim() != 4:
             raise ValueError("k_new: [batch, Hkv, max_new, d] is needed")
-        max_new = int(k_new.shape[2])
-        shape = (c.batch, c.n_kv_heads, max_new, c.head_dim)
-        self._given("k_new", k_new, shape, torch_dtype(c))
-        self._given("v_new", v_new, shape, torch_dtype(c))
-        for name, t in (("n_new", n_new), ("pos_shift", pos_shift)):
-            if t is not None:
-                self._given(name, t, (c.batch,), torch.int32)
-        self._rope_ws = self._grown(self._rope_ws, append_rope_workspace_bytes(c, max_new))
-        with _on(self.device):
-            _check(lib().spla_append_rope(ctypes.byref(c), ctypes.byref(self._struct),
-                                          ctypes.byref(rope), _ptr(k_new), _ptr(v_new), max_new,
-                                          _ptr(n_new), _ptr(pos_shift), _ptr(self._rope_ws),
-                                          self._rope_ws.numel(), _stream(self.device)),
-                   "spla_append_rope")
+        max_new = k_new.shape[2]
+        shape, dtype = (c.batch, c.n_kv_heads, max_new, c.head_dim), torch_dtype(c)
+        kp = self._given("k_new", k_new, shape, dtype)
+        vp = self._given("v_new", v_new, shape, dtype)
+        np_ = None if n_new is None else self._given("n_new", n_new, (c.batch,), torch.int32)
+        sp = (None if pos_shift is None
+              else self._given("pos_shift", pos_shift, (c.batch,), torch.int32))
+        ws = self._rope_ws = self._workspace("rope", max_new, append_rope_workspace_bytes,
+                                             self._rope_ws)
+        _launch(lib().spla_append_rope, "spla_append_rope", self.device,
+                (ctypes.byref(c), ctypes.byref(self._struct), ctypes.byref(rope), kp, vp, max_new,
+                 np_, sp, ws.data_ptr(), ws.numel()))
 
     def attend(self, q: torch.Tensor, out=None, lse=None, softcap=0.0, slopes=None,
                first_key=None, prefix_len=None, n_new=None):
@@ -571,34 +593,33 @@ class SplaCache:
         [T, batch]: the first position each query sees. prefix_len int32 [batch]: positions
         every query sees. n_new int32 [batch]: the queries each sequence really has; the
         rows of out and lse past them are left as they are (zeros in tensors made here)."""
-        c = self.cfg
-        if q.dim() not in (3, 4):
+        c, shape, dtype = self.cfg, q.shape, torch_dtype(self.cfg)
+        if len(shape) not in (3, 4):
             raise ValueError("q: [T, batch, Hq, d] is needed")
-        T = 1 if q.dim() == 3 else int(q.shape[0])
-        lead = tuple(q.shape[:-2])
-        self._given("q", q, (lead[:-1] if q.dim() == 4 else ()) + (c.batch, c.n_q_heads,
-                                                                   c.head_dim), torch_dtype(c))
+        T = shape[0] if len(shape) == 4 else 1
+        lead = (T, c.batch) if len(shape) == 4 else (c.batch,)
+        qp = self._given("q", q, lead + (c.n_q_heads, c.head_dim), dtype)
         new = torch.empty if n_new is None else torch.zeros
         if out is None:
-            out = new(q.shape, dtype=q.dtype, device=q.device)
+            out = new(shape, dtype=dtype, device=q.device)
         if lse is None:
-            lse = new(q.shape[:-1], dtype=torch.float32, device=q.device)
-        self._given("out", out, tuple(q.shape), q.dtype)
-        self._given("lse", lse, tuple(q.shape[:-1]), torch.float32)
-        for name, t, shape, dt in (("slopes", slopes, (c.n_q_heads,), torch.float32),
-                                   ("first_key", first_key, lead, torch.int32),
-                                   ("prefix_len", prefix_len, (c.batch,), torch.int32),
-                                   ("n_new", n_new, (c.batch,), torch.int32)):
-            if t is not None:
-                self._given(name, t, shape, dt)
-        opts = SplaAttendOpts(float(softcap), 0.0, *(
-            None if t is None else t.data_ptr() for t in (slopes, first_key, prefix_len, n_new)))
-        self._attend_ws = self._grown(self._attend_ws, attend_workspace_bytes(c, T))
-        with _on(self.device):
-            _check(lib().spla_attend(ctypes.byref(c), ctypes.byref(self._struct), T, _ptr(q),
-                                     ctypes.byref(opts), _ptr(out), _ptr(lse),
-                                     _ptr(self._attend_ws), self._attend_ws.numel(),
-                                     _stream(self.device)), "spla_attend")
+            lse = new(shape[:-1], dtype=torch.float32, device=q.device)
+        op = self._given("out", out, shape, dtype)
+        lp = self._given("lse", lse, shape[:-1], torch.float32)
+        opts = SplaAttendOpts(softcap)
+        if slopes is not None:
+            opts.slopes = self._given("slopes", slopes, (c.n_q_heads,), torch.float32)
+        if first_key is not None:
+            opts.first_key = self._given("first_key", first_key, lead, torch.int32)
+        if prefix_len is not None:
+            opts.prefix_len = self._given("prefix_len", prefix_len, (c.batch,), torch.int32)
+        if n_new is not None:
+            opts.n_new = self._given("n_new", n_new, (c.batch,), torch.int32)
+        ws = self._attend_ws = self._workspace("attend", T, attend_workspace_bytes,
+                                               self._attend_ws)
+        _launch(lib().spla_attend, "spla_attend", self.device,
+                (ctypes.byref(c), ctypes.byref(self._struct), T, qp, ctypes.byref(opts), op, lp,
+                 ws.data_ptr(), ws.numel()))
         return out, lse
 
     # ---- layout views (for checks; pure indexing) ----
