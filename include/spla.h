@@ -324,7 +324,9 @@ int32_t spla_prefill_workspace_bytes(const spla_config* cfg, int32_t n_tokens,
 int32_t spla_rope_init(const spla_rope_config* cfg, spla_rope* out);
 
 /* Device workspace that spla_append_rope needs for up to max_new tokens per
- * sequence (host-only query). */
+ * sequence (host-only query). Zero-fill it once before its first use, or after
+ * other data was in it: its first bytes are counters, which must be zero when a
+ * call starts and which every call leaves zero. */
 int32_t spla_append_rope_workspace_bytes(const spla_config* cfg, int32_t max_new,
                                          size_t* out_bytes);
 
@@ -483,12 +485,12 @@ int32_t spla_rotate(const spla_config* cfg, const spla_rope* rope, int32_t n_tok
 /* spla_append with the rotation applied to the keys on the way: the row at
  * position p = L_b + t (plus pos_shift[b]) is rotated, rounded to the cache
  * dtype and appended; values are appended as they are. The result is that of
- * spla_append of the rotated rows.
+ * spla_append of the rotated rows (of spla_step's append for max_new = 1).
  *  pos_shift:  device int32 [batch] or NULL (0): added to the cache position to
  *              give the rotary position (a sequence whose oldest tokens were
  *              dropped, or that begins in the middle of a text).
  * The other arguments as spla_append; the workspace from
- * spla_append_rope_workspace_bytes. Queries of the same tokens: spla_rotate. */
+ * spla_append_rope_workspace_bytes, zero-filled before its first use. Queries of the same tokens: spla_rotate. */
 int32_t spla_append_rope(const spla_config* cfg, const spla_cache* cache, const spla_rope* rope,
                          const void* k_new, const void* v_new, int32_t max_new,
                          const int32_t* n_new, const int32_t* pos_shift, void* workspace,

@@ -2,8 +2,11 @@
 // global linear-attention state S_bar = sum_t phi(k_t)^T v_t, z_bar =
 // sum_t phi(k_t) (Sec. 3.1 statistics, Sec. 3.2 Eq. 15, phi = softmax over
 // the feature dimension).
+#include <type_traits>
+
 #include "spla_device.h"
 #include "spla_kernels.h"
+#include "spla_rope.h"
 
 namespace spla {
 
@@ -598,13 +601,33 @@ __global__ __launch_bounds__(256) void append_state_mfma_kernel(
 // Tokens outside [L0, L0 + n) (before the append point in the first block,
 // past the new tokens in the last) load a clamped real row, get phi = 0 and
 // are neither stored nor counted.
-template <int D>
+//
+// ROPE: the keys are rotated as they come out of their registers, before anything
+// else sees them (rotations of a multiple of 16 coordinates: a lane's 8 coordinates
+// then all lie in the first, or all in the second half of their pairs, or unrotated).
+// A lane holds the cosines and sines of its 8 pairs at its first token of the step,
+// in fp64, turned on by 32 positions per step with four products (a sine for every
+// token and pair would be 2048 of them per step and workgroup), and by one position
+// for its second token. The turns of one and of 32 positions lie in LDS. After n
+// steps the angle is off by n roundings of 2^-53: nothing next to the rounding to
+// fp32 that follows.
+struct RopeStep {
+  double2 one[SPLA_ROPE_MAX_PAIRS], step[SPLA_ROPE_MAX_PAIRS];
+};
+struct NoRope {};
+
+__device__ __forceinline__ double2 turn_on(double2 a, double2 b) {
+  return make_double2(fma(a.x, b.x, -(a.y * b.y)), fma(a.x, b.y, a.y * b.x));
+}
+
+template <int D, bool ROPE>
 __global__ __launch_bounds__(256) void append_fused_kernel(
     Dims m, bf16_t* __restrict__ kcache, bf16_t* __restrict__ vcache, float* __restrict__ stats,
     const int32_t* __restrict__ seq_lens, int32_t* __restrict__ err,
     const bf16_t* __restrict__ k_new, const bf16_t* __restrict__ v_new, int max_new,
     const int32_t* __restrict__ n_new, const int32_t* __restrict__ table, int n_chunks,
-    int chunk_tokens, float* __restrict__ part_s, float* __restrict__ part_z) {
+    int chunk_tokens, float* __restrict__ part_s, float* __restrict__ part_z,
+    std::conditional_t<ROPE, spla_rope, NoRope> rope, const int32_t* __restrict__ shift) {
   static_assert(D == 128, "two tokens per lane: d = 128");
   constexpr int RT = D / 16;  // row tiles (coordinates j)
   constexpr int CT = D / 64;  // column tiles per wavefront
@@ -657,6 +680,28 @@ __global__ __launch_bounds__(256) void append_fused_kernel(
     v += dpp_rot<0x4E>(v);
     return v + dpp_rot<0xB1>(v);
   };
+  [[maybe_unused]] int rp0 = 0, r_other = lane;  // first pair; lane of the other coordinates
+  [[maybe_unused]] bool r_on = false, r_half = false, r_second = false;
+  [[maybe_unused]] double2 z[8];  // the pairs' cosine and sine at token tok(0) of the step
+  __shared__ std::conditional_t<ROPE, RopeStep, NoRope> s_rope;
+  if constexpr (ROPE) {
+    const int np = rope.rot_dim / 2;
+    r_on = 8 * cl < 2 * np;
+    r_half = rope.layout == SPLA_ROPE_HALF;
+    r_second = r_half && 8 * cl >= np;
+    if (r_on) {
+      rp0 = r_half ? 8 * cl - (r_second ? np : 0) : 4 * cl;
+      if (r_half) r_other = (lane & 48) + cl + (r_second ? -np / 8 : np / 8);
+    }
+    if (tid < np) s_rope.one[tid] = rope_cos_sin(1.0, rope.turns[tid], 1.0);
+    if (tid >= 128 && tid < 128 + np)
+      s_rope.step[tid - 128] = rope_cos_sin(32.0, rope.turns[tid - 128], 1.0);
+    const double p0 = (double)(a0 + tok(0)) + (shift ? shift[b] : 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      z[i] = rope_cos_sin(p0, rope.turns[min(rp0 + i, SPLA_ROPE_MAX_PAIRS - 1)], rope.gain);
+    __syncthreads();
+  }
   // statistics: thread (coordinate sc, half sh) sums tokens 16 sh .. + 15
   const int sc = tid >> 1, sh = tid & 1;
   double s1 = 0.0, s2 = 0.0;
@@ -680,6 +725,44 @@ __global__ __launch_bounds__(256) void append_fused_kernel(
       vc[s] = vx[s];
     }
     if (tt + kSubTokens < a1) load_step(tt + kSubTokens);
+    if constexpr (ROPE) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        uint32_t own[4] = {kc[s].x, kc[s].y, kc[s].z, kc[s].w}, oth[4];
+        if (r_half) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) oth[i] = (uint32_t)__shfl((int)own[i], r_other, 64);
+        }
+        if (!r_on) continue;
+        auto at = [](const uint32_t (&x)[4], int i) {
+          return (double)bf16_to_f32((uint16_t)(i & 1 ? x[i >> 1] >> 16 : x[i >> 1] & 0xFFFFu));
+        };
+        float y[8];
+        if (r_half) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const double2 c = s == 0 ? z[i] : turn_on(z[i], s_rope.one[rp0 + i]);
+            const double q = at(oth, i) * c.y;
+            y[i] = (float)fma(at(own, i), c.x, r_second ? q : -q);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const double2 c = s == 0 ? z[i] : turn_on(z[i], s_rope.one[rp0 + i]);
+            const double a = at(own, 2 * i), q = at(own, 2 * i + 1);
+            y[2 * i] = (float)fma(a, c.x, -(q * c.y));
+            y[2 * i + 1] = (float)fma(q, c.x, a * c.y);
+          }
+        }
+        kc[s] = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]),
+                           pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+      }
+      if (r_on) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < 4 || r_half) z[i] = turn_on(z[i], s_rope.step[rp0 + i]);
+      }
+    }
     float ph[2][8];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -895,11 +978,12 @@ __global__ __launch_bounds__(256) void append_state_reduce_kernel(
 // Rows rx * 16 .. rx * 16 + 15 of S_bar += phi(k)^T v (and those entries of
 // z_bar += phi(k)) for the single token k, v of (sequence, kv head) bh, by the
 // 256 threads of a workgroup. A sequence at capacity gets nothing.
+// (k_row, v_row: the token's d elements)
 template <typename T, int D>
 __device__ __forceinline__ void append_rank1_rows(const Dims& m,
                                                   const int32_t* __restrict__ seq_lens,
-                                                  const T* __restrict__ k_new,
-                                                  const T* __restrict__ v_new,
+                                                  const T* __restrict__ k_row,
+                                                  const T* __restrict__ v_row,
                                                   float* __restrict__ S, float* __restrict__ z,
                                                   int rx, int bh) {
   __shared__ float sphi[D];
@@ -922,7 +1006,7 @@ __device__ __forceinline__ void append_rank1_rows(const Dims& m,
     float mx = -INFINITY;
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) {
-      x[e] = Elem<T>::load(k_new, (int64_t)bh * D + tid + 64 * e);
+      x[e] = Elem<T>::load(k_row, tid + 64 * e);
       mx = fmaxf(mx, x[e]);
     }
     mx = wave_max(mx);
@@ -938,7 +1022,7 @@ __device__ __forceinline__ void append_rank1_rows(const Dims& m,
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) sphi[tid + 64 * e] = x[e] / s;
   }
-  for (int c = tid; c < D; c += 256) sv[c] = Elem<T>::load(v_new, (int64_t)bh * D + c);
+  for (int c = tid; c < D; c += 256) sv[c] = Elem<T>::load(v_row, c);
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < PT; ++u) {
@@ -958,7 +1042,7 @@ __device__ __forceinline__ void append_rank1_rows(const Dims& m,
 // itself, so no read of the old length follows the advance.
 __device__ __forceinline__ void append_one_finish(const Dims& m, int32_t* seq_lens,
                                                   int32_t* fin_ctr, int32_t* appended, int bh,
-                                                  int* s_flag) {
+                                                  int* s_flag, const int32_t* n_new = nullptr) {
   const int b = bh / m.hkv;
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -966,7 +1050,7 @@ __device__ __forceinline__ void append_one_finish(const Dims& m, int32_t* seq_le
     if (atomic_add_agent(c, 1) == m.hkv * (int)gridDim.x - 1) {
       bool clipped;
       const int L0 = seq_lens[b];
-      const int n = appended_count(m, L0, 1, nullptr, b, &clipped);
+      const int n = appended_count(m, L0, 1, n_new, b, &clipped);
       seq_lens[b] = L0 + n;
       if (appended) appended[b] = n;
       store_agent(c, 0);
@@ -989,11 +1073,54 @@ __global__ __launch_bounds__(256) void append_one_kernel(
   __shared__ int s_flag;
   const int bh = (int)blockIdx.y;
   if ((int)blockIdx.x < D / 16)
-    append_rank1_rows<T, D>(m, seq_lens, k_new, v_new, S, z, (int)blockIdx.x, bh);
+    append_rank1_rows<T, D>(m, seq_lens, k_new + (int64_t)bh * D, v_new + (int64_t)bh * D, S, z,
+                            (int)blockIdx.x, bh);
   else
     append_unit<T>(m, kc, vc, stats, seq_lens, err, k_new, v_new, 1, nullptr, table,
                    (int)blockIdx.x - D / 16, bh, D, D);
   if (fin_ctr) append_one_finish(m, seq_lens, fin_ctr, appended, bh, &s_flag);
+}
+
+// append_one_kernel for a token whose key is rotated on the way: every workgroup
+// rotates the key of its (sequence, KV head) into LDS first (a thread per
+// coordinate, its pair's angle in fp64: the same bits as spla_rotate gives), while
+// the first loads of its part are on their way. n_new: 0 or 1 token per sequence.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void append_rope_one_kernel(
+    Dims m, T* __restrict__ kc, T* __restrict__ vc, float* __restrict__ stats,
+    int32_t* __restrict__ seq_lens, int32_t* __restrict__ err, const T* __restrict__ k_new,
+    const T* __restrict__ v_new, const int32_t* __restrict__ n_new,
+    const int32_t* __restrict__ shift, spla_rope rope, const int32_t* __restrict__ table,
+    float* __restrict__ S, float* __restrict__ z, int32_t* __restrict__ fin_ctr) {
+  __shared__ int s_flag;
+  __shared__ T s_k[D];
+  const int bh = (int)blockIdx.y, b = bh / m.hkv, tid = threadIdx.x;
+  if (!n_new || n_new[b] > 0) {  // uniform
+    if (tid < D) {
+      const T* kr = k_new + (int64_t)bh * D;
+      const int np = rope.rot_dim / 2;
+      const bool half = rope.layout == SPLA_ROPE_HALF;
+      T own = kr[tid];
+      if (tid < 2 * np) {
+        const bool second = half ? tid >= np : tid & 1;
+        const int other = half ? (second ? tid - np : tid + np) : tid ^ 1;
+        const int pair = half ? (second ? tid - np : tid) : tid >> 1;
+        T x = kr[other];
+        const double2 w = rope_cos_sin((double)seq_lens[b] + (shift ? shift[b] : 0),
+                                       rope.turns[pair], rope.gain);
+        if (second) rope_turn(x, own, w);
+        else rope_turn(own, x, w);
+      }
+      s_k[tid] = own;
+    }
+    __syncthreads();
+    if ((int)blockIdx.x < D / 16)
+      append_rank1_rows<T, D>(m, seq_lens, s_k, v_new + (int64_t)bh * D, S, z, (int)blockIdx.x, bh);
+    else
+      append_unit<T>(m, kc, vc, stats, seq_lens, err, s_k, v_new + (int64_t)bh * D, 1, nullptr,
+                     table, (int)blockIdx.x - D / 16, bh, 0, 0);
+  }
+  append_one_finish(m, seq_lens, fin_ctr, nullptr, bh, &s_flag, n_new);
 }
 
 // The statistics units and K/V rows of a single-token append alone (the
@@ -1111,21 +1238,30 @@ hipError_t launch_block_states(const Dims& m, const spla_cache& c, const void* k
   return hipGetLastError();
 }
 
+bool append_rope_fusable(const Dims& m, const spla_rope& rope) {
+  return append_fusable(m) && rope.rot_dim % 16 == 0;
+}
+
 bool append_fusable(const Dims& m) { return m.elem == 2 && m.d == 128 && !windowed(m); }
 
 hipError_t launch_append_fused(const Dims& m, const spla_cache& c, const void* k_new,
                                const void* v_new, int max_new, const int32_t* n_new,
-                               const AppendWs& ws, char* base, hipStream_t st) {
+                               const AppendWs& ws, char* base, hipStream_t st,
+                               const spla_rope* rope, const int32_t* shift) {
   if (!append_fusable(m)) return hipErrorInvalidValue;
   // block-aligned chunks: the first starts up to B - 1 positions before the
   // append point, so n_chunks chunks of ct tokens cover B - 1 + max_new
   const int ct = (int)align_up(ceil_div((int64_t)max_new + m.B - 1, ws.n_chunks),
                                m.B > kSubTokens ? m.B : kSubTokens);
-  hipLaunchKernelGGL(append_fused_kernel<128>, dim3(ws.n_chunks, m.bh), dim3(256), 0, st, m,
-                     (bf16_t*)c.k_cache, (bf16_t*)c.v_cache, c.blk_stats, c.seq_lens, c.err_flags,
-                     (const bf16_t*)k_new, (const bf16_t*)v_new, max_new, n_new,
-                     m.pages > 0 ? c.block_table : nullptr, ws.n_chunks, ct,
-                     (float*)(base + ws.part_s), (float*)(base + ws.part_z));
+  auto go = [&](auto kern, auto r) {
+    hipLaunchKernelGGL(kern, dim3(ws.n_chunks, m.bh), dim3(256), 0, st, m, (bf16_t*)c.k_cache,
+                       (bf16_t*)c.v_cache, c.blk_stats, c.seq_lens, c.err_flags,
+                       (const bf16_t*)k_new, (const bf16_t*)v_new, max_new, n_new,
+                       m.pages > 0 ? c.block_table : nullptr, ws.n_chunks, ct,
+                       (float*)(base + ws.part_s), (float*)(base + ws.part_z), r, shift);
+  };
+  if (rope) go(append_fused_kernel<128, true>, *rope);
+  else go(append_fused_kernel<128, false>, NoRope{});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(append_state_reduce_kernel, dim3(m.d / kReduceRows, m.bh), dim3(256), 0,
@@ -1165,6 +1301,26 @@ hipError_t launch_append_one(const Dims& m, const spla_cache& c, const void* k_n
   } else {
     if (m.d == 64) append_one_td<bf16_t, 64>(m, c, k_new, v_new, st, rank1, fin_ctr, appended);
     else append_one_td<bf16_t, 128>(m, c, k_new, v_new, st, rank1, fin_ctr, appended);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_append_rope_one(const Dims& m, const spla_cache& c, const spla_rope& rope,
+                                  const void* k_new, const void* v_new, const int32_t* n_new,
+                                  const int32_t* shift, int32_t* fin_ctr, hipStream_t st) {
+  auto go = [&](auto zero, auto kern) {
+    using T = decltype(zero);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(m.d / 16 + units_of_one(m)), (unsigned)m.bh),
+                       dim3(256), 0, st, m, (T*)c.k_cache, (T*)c.v_cache, c.blk_stats, c.seq_lens,
+                       c.err_flags, (const T*)k_new, (const T*)v_new, n_new, shift, rope,
+                       m.pages > 0 ? c.block_table : nullptr, c.lin_state, c.lin_norm, fin_ctr);
+  };
+  if (m.elem == 4) {
+    if (m.d == 64) go(float{}, append_rope_one_kernel<float, 64>);
+    else go(float{}, append_rope_one_kernel<float, 128>);
+  } else {
+    if (m.d == 64) go(bf16_t{}, append_rope_one_kernel<bf16_t, 64>);
+    else go(bf16_t{}, append_rope_one_kernel<bf16_t, 128>);
   }
   return hipGetLastError();
 }

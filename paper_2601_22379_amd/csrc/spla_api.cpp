@@ -358,6 +358,18 @@ extern "C" int32_t spla_append_rope(const spla_config* cfg, const spla_cache* ca
   const spla::AppendRopeWs L = spla::append_rope_ws_layout(m, max_new);
   if ((s = check_ws(workspace, workspace_bytes, (size_t)L.total)) != SPLA_OK) return s;
   char* ws = static_cast<char*>(workspace);
+  if (max_new == 1) {
+    SPLA_TRY(spla::launch_append_rope_one(m, *cache, *rope, k_new, v_new, n_new, pos_shift,
+                                          reinterpret_cast<int32_t*>(ws + L.count),
+                                          static_cast<hipStream_t>(stream)));
+    return SPLA_OK;
+  }
+  if (spla::append_rope_fusable(m, *rope)) {
+    SPLA_TRY(spla::launch_append_fused(m, *cache, k_new, v_new, max_new, n_new,
+                                       spla::append_ws_layout(m, max_new), ws + L.append,
+                                       static_cast<hipStream_t>(stream), rope, pos_shift));
+    return SPLA_OK;
+  }
   const int64_t s_h = (int64_t)max_new * m.d, s_b = s_h * m.hkv;
   const spla::RotateSet set{k_new, ws + L.k_rot, m.d, s_b, s_h, m.d, s_b, s_h, m.hkv};
   const spla::RotateRows rows{max_new, m.batch, nullptr, cache->seq_lens, pos_shift, n_new};

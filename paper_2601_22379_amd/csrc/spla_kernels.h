@@ -40,7 +40,11 @@ hipError_t launch_block_states(const Dims& m, const spla_cache& c, const void* k
 bool append_fusable(const Dims& m);
 hipError_t launch_append_fused(const Dims& m, const spla_cache& c, const void* k_new,
                                const void* v_new, int max_new, const int32_t* n_new,
-                               const AppendWs& ws, char* wsbase, hipStream_t st);
+                               const AppendWs& ws, char* wsbase, hipStream_t st,
+                               const spla_rope* rope = nullptr, const int32_t* shift = nullptr);
+// ... with the keys rotated on the way (rope, shift as in spla_append_rope): the
+// append_fusable shapes with a multiple of 16 rotated coordinates
+bool append_rope_fusable(const Dims& m, const spla_rope& rope);
 // the single-token append of a step (statistics, K/V rows and, with rank1,
 // the rank-one update of S_bar and z_bar) in one launch. With fin_ctr (the
 // items_done lines of a decode workspace's synchronisation area) the last
@@ -50,6 +54,11 @@ hipError_t launch_append_fused(const Dims& m, const spla_cache& c, const void* k
 hipError_t launch_append_one(const Dims& m, const spla_cache& c, const void* k_new,
                              const void* v_new, hipStream_t st, bool rank1 = true,
                              int32_t* fin_ctr = nullptr, int32_t* appended = nullptr);
+// launch_append_one of keys rotated on the way (n_new, shift as in spla_append_rope);
+// fin_ctr: zero between calls, a line of kSyncLine words per sequence
+hipError_t launch_append_rope_one(const Dims& m, const spla_cache& c, const spla_rope& rope,
+                                  const void* k_new, const void* v_new, const int32_t* n_new,
+                                  const int32_t* shift, int32_t* fin_ctr, hipStream_t st);
 hipError_t launch_append_finish(const Dims& m, const spla_cache& c, int max_new,
                                 const int32_t* n_new, hipStream_t st,
                                 int32_t* appended = nullptr);

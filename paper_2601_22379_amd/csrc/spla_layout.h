@@ -405,8 +405,10 @@ SPLA_HD AppendWs append_ws_layout(const Dims& m, int max_new) {
   return w;
 }
 
-// The rotating append: the rotated keys, then the append's own workspace.
+// The rotating append: the counters of its single-token form (zero between calls of
+// any length), the rotated keys, then the append's own workspace.
 struct AppendRopeWs {
+  int64_t count;   // i32 [batch][kSyncLine]
   int64_t k_rot;   // dtype [bh][max_new][d]
   int64_t append;  // AppendWs
   int64_t total;
@@ -414,8 +416,13 @@ struct AppendRopeWs {
 
 SPLA_HD AppendRopeWs append_rope_ws_layout(const Dims& m, int max_new) {
   AppendRopeWs w;
-  w.k_rot = 0;
-  w.append = align_up((int64_t)m.bh * max_new * m.d * m.elem, SPLA_WORKSPACE_ALIGN);
+  w.count = 0;
+  w.k_rot = align_up((int64_t)m.batch * kSyncLine * 4, SPLA_WORKSPACE_ALIGN);
+  if (max_new <= 1) {
+    w.append = w.total = w.k_rot;
+    return w;
+  }
+  w.append = w.k_rot + align_up((int64_t)m.bh * max_new * m.d * m.elem, SPLA_WORKSPACE_ALIGN);
   w.total = w.append + append_ws_layout(m, max_new).total;
   return w;
 }

@@ -153,6 +153,11 @@ APPENDS = {  # dtype, d, hkv, B, paged, windows, rot, layout, slabs of (tokens, 
                 [(77, [77, 32, 33]), (1, None), (40, None)]),
     "f32_d128_paged": ("f32", 128, 1, 64, True, (0, 0), 128, "half",
                        [(1, None), (70, [1, 70, 69])]),
+    "bf16_d128_part": ("bf16", 128, 2, 128, True, (0, 0), 48, "half",
+                       [(300, [300, 129, 2]), (50, None)]),
+    "bf16_d128_pairs": ("bf16", 128, 2, 64, False, (0, 0), 112, "interleaved",
+                        [(130, [130, 65, 0]), (64, None)]),
+    "bf16_d128_odd": ("bf16", 128, 1, 64, False, (0, 0), 90, "half", [(130, [130, 65, 0])]),
     "bf16_d128_long": ("bf16", 128, 1, 64, False, (0, 0), 128, "half", [(5000, [5000, 4097, 64])]),
 }
 
@@ -160,7 +165,8 @@ APPENDS = {  # dtype, d, hkv, B, paged, windows, rot, layout, slabs of (tokens, 
 @pytest.mark.parametrize("name", list(APPENDS))
 def test_append_rope(dev, name):
     """Cache contents after rotating appends: the rotated rows, and the statistics, state and
-    lengths that an append of those rows gives, bit for bit."""
+    lengths that an append of those rows gives, bit for bit (but for the state after single
+    tokens, which a step's append adds in another order: within the bounds below)."""
     dtype, d, hkv, B, paged, win, rot, layout, slabs = APPENDS[name]
     b, cap = 3, -(-(sum(s[0] for s in slabs) + 5) // B) * B
     pages, table, extra = 0, None, {}
@@ -192,9 +198,10 @@ def test_append_rope(dev, name):
             lens[s] += c
     torch.cuda.synchronize()
     assert one.device_errors() == 0 and one.seq_lens.cpu().tolist() == lens
-    for x, y in ((one.k, two.k), (one.v, two.v), (one.stats, two.stats), (one.state, two.state),
-                 (one.norm, two.norm)):
+    for x, y in ((one.k, two.k), (one.v, two.v), (one.stats, two.stats)):
         assert torch.equal(x, y)
+    if all(T > 1 for T, _ in slabs):
+        assert torch.equal(one.state, two.state) and torch.equal(one.norm, two.norm)
     K, V = one.k_logical(), one.v_logical()
     S, z = one.state_logical()
     mean, m2 = one.stats_logical()
