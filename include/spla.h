@@ -484,8 +484,9 @@ int32_t spla_rotate(const spla_config* cfg, const spla_rope* rope, int32_t n_tok
 
 /* spla_append with the rotation applied to the keys on the way: the row at
  * position p = L_b + t (plus pos_shift[b]) is rotated, rounded to the cache
- * dtype and appended; values are appended as they are. The result is that of
- * spla_append of the rotated rows (of spla_step's append for max_new = 1).
+ * dtype and appended; values are appended as they are. Rows, statistics and
+ * lengths become those of spla_append of the rotated rows, S_bar and z_bar too up
+ * to the rounding of their fp32 sums.
  *  pos_shift:  device int32 [batch] or NULL (0): added to the cache position to
  *              give the rotary position (a sequence whose oldest tokens were
  *              dropped, or that begins in the middle of a text).

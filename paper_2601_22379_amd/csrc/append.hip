@@ -603,16 +603,22 @@ __global__ __launch_bounds__(256) void append_state_mfma_kernel(
 // are neither stored nor counted.
 //
 // ROPE: the keys are rotated as they come out of their registers, before anything
-// else sees them (rotations of a multiple of 16 coordinates: a lane's 8 coordinates
-// then all lie in the first, or all in the second half of their pairs, or unrotated).
-// A lane holds the cosines and sines of its 8 pairs at its first token of the step,
+// else sees them (rotations of a multiple of 16 coordinates, whole 8-coordinate
+// pieces). Half pairs: lanes 2 u and 2 u + 1 take the pieces u and u + rot / 16, whose
+// coordinates pair up, and swap halves of them (two dwords by a lane swap) before and
+// after, so that each turns four pairs of its own, as with interleaved ones; fetching
+// a partner's coordinates and turning one end of eight pairs per lane converted and
+// turned everything twice (196 us against FUSED_US for 4 prompts of up to 16384 tokens). A
+// lane holds the cosines and sines of its four pairs at its first token of the step,
 // in fp64, turned on by 32 positions per step with four products (a sine for every
 // token and pair would be 2048 of them per step and workgroup), and by one position
 // for its second token. The turns of one and of 32 positions lie in LDS. After n
 // steps the angle is off by n roundings of 2^-53: nothing next to the rounding to
-// fp32 that follows.
+// fp32 that follows. The kernel is bound by its instructions (two wavefronts per SIMD).
 struct RopeStep {
   double2 one[SPLA_ROPE_MAX_PAIRS], step[SPLA_ROPE_MAX_PAIRS];
+  double2 two[4][SPLA_ROPE_MAX_PAIRS];  // turns of 2, 4, 8 and 16 positions
+  double2 base[SPLA_ROPE_MAX_PAIRS];    // angles at the chunk's first position
 };
 struct NoRope {};
 
@@ -656,16 +662,22 @@ __global__ __launch_bounds__(256) void append_fused_kernel(
   for (int i = 0; i < 8; ++i) zacc[i] = 0.f;
   const bf16_t* kb = k_new + (int64_t)bh * max_new * D;
   const bf16_t* vb = v_new + (int64_t)bh * max_new * D;
-  // lane l: coordinates 8 (l % 16) .. + 7 of tokens 8 w + 2 (l / 16) + s
+  // lane l: coordinates 8 (l % 16) .. + 7 of tokens 8 w + 2 (l / 16) + s (c0 .. + 7;
+  // rotated half pairs: the pieces of a pair of lanes pair up)
   const int cl = lane & 15, tl = lane >> 4;
+  int c0 = 8 * cl;
+  if constexpr (ROPE) {
+    if (rope.layout == SPLA_ROPE_HALF && 8 * cl < rope.rot_dim)
+      c0 = 8 * (cl >> 1) + (cl & 1) * (rope.rot_dim / 2);
+  }
   auto tok = [&](int s) { return 8 * w + 2 * tl + s; };
   uint4 kx[2], vx[2];
   auto load_step = [&](int tt) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int row = min(max(tt + tok(s) - L0, 0), ne - 1);
-      kx[s] = *reinterpret_cast<const uint4*>(kb + (int64_t)row * D + 8 * cl);
-      vx[s] = *reinterpret_cast<const uint4*>(vb + (int64_t)row * D + 8 * cl);
+      kx[s] = *reinterpret_cast<const uint4*>(kb + (int64_t)row * D + c0);
+      vx[s] = *reinterpret_cast<const uint4*>(vb + (int64_t)row * D + c0);
     }
   };
   auto row_max = [](float v) {
@@ -680,27 +692,27 @@ __global__ __launch_bounds__(256) void append_fused_kernel(
     v += dpp_rot<0x4E>(v);
     return v + dpp_rot<0xB1>(v);
   };
-  [[maybe_unused]] int rp0 = 0, r_other = lane;  // first pair; lane of the other coordinates
-  [[maybe_unused]] bool r_on = false, r_half = false, r_second = false;
-  [[maybe_unused]] double2 z[8];  // the pairs' cosine and sine at token tok(0) of the step
+  [[maybe_unused]] bool r_on = false, r_half = false;
+  [[maybe_unused]] double2 z[4];  // pairs 4 cl + i: cosine and sine at token tok(0) of the step
   __shared__ std::conditional_t<ROPE, RopeStep, NoRope> s_rope;
   if constexpr (ROPE) {
-    const int np = rope.rot_dim / 2;
-    r_on = 8 * cl < 2 * np;
+    r_on = 8 * cl < rope.rot_dim;
     r_half = rope.layout == SPLA_ROPE_HALF;
-    r_second = r_half && 8 * cl >= np;
-    if (r_on) {
-      rp0 = r_half ? 8 * cl - (r_second ? np : 0) : 4 * cl;
-      if (r_half) r_other = (lane & 48) + cl + (r_second ? -np / 8 : np / 8);
-    }
-    if (tid < np) s_rope.one[tid] = rope_cos_sin(1.0, rope.turns[tid], 1.0);
-    if (tid >= 128 && tid < 128 + np)
-      s_rope.step[tid - 128] = rope_cos_sin(32.0, rope.turns[tid - 128], 1.0);
-    const double p0 = (double)(a0 + tok(0)) + (shift ? shift[b] : 0);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      z[i] = rope_cos_sin(p0, rope.turns[min(rp0 + i, SPLA_ROPE_MAX_PAIRS - 1)], rope.gain);
+    // two sines per thread (one for each of its pairs took 10 us of a 16K-token
+    // append); a lane's first angles are products over the bits of its token
+    const int pr = tid & 63, k = tid >> 6;
+    const double u = rope.turns[pr], p0 = (double)a0 + (shift ? shift[b] : 0);
+    s_rope.two[k][pr] = rope_cos_sin((double)(2 << k), u, 1.0);
+    const double2 x = rope_cos_sin(k == 0 ? 1.0 : k == 1 ? 32.0 : p0, u, k < 2 ? 1.0 : rope.gain);
+    (k == 0 ? s_rope.one : k == 1 ? s_rope.step : s_rope.base)[pr] = x;  // k = 3: base again
     __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      z[i] = s_rope.base[4 * cl + i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (tok(0) >> (e + 1) & 1) z[i] = turn_on(z[i], s_rope.two[e][4 * cl + i]);
+    }
   }
   // statistics: thread (coordinate sc, half sh) sums tokens 16 sh .. + 15
   const int sc = tid >> 1, sh = tid & 1;
@@ -726,41 +738,45 @@ __global__ __launch_bounds__(256) void append_fused_kernel(
     }
     if (tt + kSubTokens < a1) load_step(tt + kSubTokens);
     if constexpr (ROPE) {
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        uint32_t own[4] = {kc[s].x, kc[s].y, kc[s].z, kc[s].w}, oth[4];
-        if (r_half) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) oth[i] = (uint32_t)__shfl((int)own[i], r_other, 64);
-        }
-        if (!r_on) continue;
-        auto at = [](const uint32_t (&x)[4], int i) {
-          return (double)bf16_to_f32((uint16_t)(i & 1 ? x[i >> 1] >> 16 : x[i >> 1] & 0xFFFFu));
-        };
-        float y[8];
-        if (r_half) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const double2 c = s == 0 ? z[i] : turn_on(z[i], s_rope.one[rp0 + i]);
-            const double q = at(oth, i) * c.y;
-            y[i] = (float)fma(at(own, i), c.x, r_second ? q : -q);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const double2 c = s == 0 ? z[i] : turn_on(z[i], s_rope.one[rp0 + i]);
-            const double a = at(own, 2 * i), q = at(own, 2 * i + 1);
-            y[2 * i] = (float)fma(a, c.x, -(q * c.y));
-            y[2 * i + 1] = (float)fma(q, c.x, a * c.y);
-          }
-        }
-        kc[s] = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]),
-                           pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-      }
       if (r_on) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (i < 4 || r_half) z[i] = turn_on(z[i], s_rope.step[rp0 + i]);
+        for (int s = 0; s < 2; ++s) {
+          uint32_t w[4] = {kc[s].x, kc[s].y, kc[s].z, kc[s].w};
+          // half pairs: even lane the low, odd lane the high coordinates of both pieces
+          auto swap_halves = [&] {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t y =
+                  __float_as_uint(dpp_rot<0xB1>(__uint_as_float(cl & 1 ? w[i] : w[2 + i])));
+              w[i] = cl & 1 ? y : w[i];
+              w[2 + i] = cl & 1 ? w[2 + i] : y;
+            }
+          };
+          if (r_half) swap_halves();
+          float x[8], y[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            x[i] = bf16_to_f32((uint16_t)(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xFFFFu));
+          auto turn = [&](int i, int e0, int e1) {
+            const double2 c = s == 0 ? z[i] : turn_on(z[i], s_rope.one[4 * cl + i]);
+            const double a = (double)x[e0], q = (double)x[e1];
+            y[e0] = (float)fma(a, c.x, -(q * c.y));
+            y[e1] = (float)fma(q, c.x, a * c.y);
+          };
+          if (r_half) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) turn(i, i, 4 + i);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) turn(i, 2 * i, 2 * i + 1);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(y[2 * i], y[2 * i + 1]);
+          if (r_half) swap_halves();
+          kc[s] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = turn_on(z[i], s_rope.step[4 * cl + i]);
       }
     }
     float ph[2][8];
@@ -769,7 +785,7 @@ __global__ __launch_bounds__(256) void append_fused_kernel(
       const int t = tt + tok(s);
       const bool ok = t >= lo && t < a1;
       if (ok && slot >= 0)
-        *reinterpret_cast<uint4*>(kcache + k_off_slot(m, slot, t % Bk, 8 * cl)) = kc[s];
+        *reinterpret_cast<uint4*>(kcache + k_off_slot(m, slot, t % Bk, c0)) = kc[s];
       const uint32_t kw[4] = {kc[s].x, kc[s].y, kc[s].z, kc[s].w};
       float kf[8];
 #pragma unroll
@@ -804,7 +820,7 @@ __global__ __launch_bounds__(256) void append_fused_kernel(
         const uint32_t sel = i & 1 ? 0x07060302u : 0x05040100u;
         const uint32_t hp = pack_bf16x2(ph[0][i], ph[1][i]);
         const float h0 = __uint_as_float(hp << 16), h1 = __uint_as_float(hp & 0xFFFF0000u);
-        const int o = StateSmem<D>::at(8 * cl + i, tok(0));
+        const int o = StateSmem<D>::at(c0 + i, tok(0));
         *reinterpret_cast<uint32_t*>(&sm.kT_h[o]) = hp;
         *reinterpret_cast<uint32_t*>(&sm.kT_l[o]) = pack_bf16x2(ph[0][i] - h0, ph[1][i] - h1);
         *reinterpret_cast<uint32_t*>(&sm.vT[o]) = __builtin_amdgcn_perm(v1[i >> 1], v0[i >> 1], sel);
@@ -921,7 +937,7 @@ __global__ __launch_bounds__(256) void append_fused_kernel(
   }
   if (lane < 16) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sm.z[w][8 * lane + i] = zacc[i];
+    for (int i = 0; i < 8; ++i) sm.z[w][c0 + i] = zacc[i];
   }
   __syncthreads();
   if (tid < D) {

@@ -165,8 +165,8 @@ APPENDS = {  # dtype, d, hkv, B, paged, windows, rot, layout, slabs of (tokens, 
 @pytest.mark.parametrize("name", list(APPENDS))
 def test_append_rope(dev, name):
     """Cache contents after rotating appends: the rotated rows, and the statistics, state and
-    lengths that an append of those rows gives, bit for bit (but for the state after single
-    tokens, which a step's append adds in another order: within the bounds below)."""
+    lengths that an append of those rows gives, bit for bit but for the state, whose sums are
+    taken in another order: within the bounds below."""
     dtype, d, hkv, B, paged, win, rot, layout, slabs = APPENDS[name]
     b, cap = 3, -(-(sum(s[0] for s in slabs) + 5) // B) * B
     pages, table, extra = 0, None, {}
@@ -200,8 +200,6 @@ def test_append_rope(dev, name):
     assert one.device_errors() == 0 and one.seq_lens.cpu().tolist() == lens
     for x, y in ((one.k, two.k), (one.v, two.v), (one.stats, two.stats)):
         assert torch.equal(x, y)
-    if all(T > 1 for T, _ in slabs):
-        assert torch.equal(one.state, two.state) and torch.equal(one.norm, two.norm)
     K, V = one.k_logical(), one.v_logical()
     S, z = one.state_logical()
     mean, m2 = one.stats_logical()
