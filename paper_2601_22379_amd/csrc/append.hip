@@ -386,12 +386,26 @@ struct alignas(16) StateSmem {
   float z[4][D];              // per-wavefront sums of phi(k)
 };
 
+// EX (the rotating append): phi as three terms, all 24 bits of it. Two leave 2^-17 of
+// each product, 2.4e-6 of the state where fp32 sums of few tokens are 6e-8 off; the
+// third costs half as many products again, a twentieth of the kernel's time.
+template <int D>
+struct alignas(16) ThirdSmem {
+  uint16_t kT[StateSmem<D>::N];  // laid out as kT_h
+};
+struct NoThird {};
+
+// What two bf16 (packed in lo) leave of a and b, as two bf16.
+__device__ __forceinline__ uint32_t third_bf16x2(float a, float b, uint32_t lo) {
+  return pack_bf16x2(a - __uint_as_float(lo << 16), b - __uint_as_float(lo & 0xFFFF0000u));
+}
+
 //
 // Chunk x holds new tokens x chunk_tokens .. + chunk_tokens - 1; with aligned,
 // those of the x-th block of the sequence from the append point's on (the
 // chunked prefill's partial of every block; chunk_tokens = B). New row r of
 // bh is element bh s_bh + r s_row of k_new and v_new, as in append_unit.
-template <int D>
+template <int D, bool EX>
 __global__ __launch_bounds__(256) void append_state_mfma_kernel(
     Dims m, const int32_t* __restrict__ seq_lens, const bf16_t* __restrict__ k_new,
     const bf16_t* __restrict__ v_new, int max_new, const int32_t* __restrict__ n_new, int n_chunks,
@@ -400,6 +414,7 @@ __global__ __launch_bounds__(256) void append_state_mfma_kernel(
   constexpr int RT = D / 16;        // row tiles (coordinates j)
   constexpr int CT = D / 64;        // column tiles per wavefront
   __shared__ StateSmem<D> sm;
+  __shared__ std::conditional_t<EX, ThirdSmem<D>, NoThird> s3;
   const int bh = blockIdx.y;
   const int b = bh / m.hkv;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
@@ -512,6 +527,9 @@ __global__ __launch_bounds__(256) void append_state_mfma_kernel(
         const uint32_t hp = pack_bf16x2(ph[0][i], ph[1][i]);
         const float h0 = __uint_as_float(hp << 16), h1 = __uint_as_float(hp & 0xFFFF0000u);
         const uint32_t lp = pack_bf16x2(ph[0][i] - h0, ph[1][i] - h1);
+        if constexpr (EX)
+          *reinterpret_cast<uint32_t*>(&s3.kT[StateSmem<D>::at(8 * cl + i, tok(0))]) =
+              third_bf16x2(ph[0][i] - h0, ph[1][i] - h1, lp);
         const uint32_t vp =
             __builtin_amdgcn_perm(v1[i >> 1], v0[i >> 1], i & 1 ? 0x07060302u : 0x05040100u);
         const int o = StateSmem<D>::at(8 * cl + i, tok(0));
@@ -528,6 +546,8 @@ __global__ __launch_bounds__(256) void append_state_mfma_kernel(
         const int o = StateSmem<D>::at(8 * cl + i, tok(0));
         sm.kT_h[o] = __builtin_bit_cast(uint16_t, hi);
         sm.kT_l[o] = __builtin_bit_cast(uint16_t, lo);
+        if constexpr (EX)
+          s3.kT[o] = __builtin_bit_cast(uint16_t, (__bf16)(ph[0][i] - (float)hi - (float)lo));
         sm.vT[o] = (uint16_t)(i & 1 ? vw[i >> 1] >> 16 : vw[i >> 1] & 0xFFFFu);
       }
     }
@@ -546,6 +566,10 @@ __global__ __launch_bounds__(256) void append_state_mfma_kernel(
             abf16x8, *reinterpret_cast<const uint4*>(&sm.vT[StateSmem<D>::at(col, 8 * lg)]));
         acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ah, bv, acc[r][c], 0, 0, 0);
         acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(al, bv, acc[r][c], 0, 0, 0);
+        if constexpr (EX)
+          acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              __builtin_bit_cast(abf16x8, *reinterpret_cast<const uint4*>(&s3.kT[oa])), bv,
+              acc[r][c], 0, 0, 0);
       }
     }
     __syncthreads();
@@ -638,6 +662,7 @@ __global__ __launch_bounds__(256) void append_fused_kernel(
   constexpr int RT = D / 16;  // row tiles (coordinates j)
   constexpr int CT = D / 64;  // column tiles per wavefront
   __shared__ StateSmem<D> sm;
+  __shared__ std::conditional_t<ROPE, ThirdSmem<D>, NoThird> s3;
   __shared__ __align__(16) uint16_t kR[StateSmem<D>::N];  // keys of the step, transposed
   const int bh = blockIdx.y;
   const int b = bh / m.hkv;
@@ -822,7 +847,10 @@ __global__ __launch_bounds__(256) void append_fused_kernel(
         const float h0 = __uint_as_float(hp << 16), h1 = __uint_as_float(hp & 0xFFFF0000u);
         const int o = StateSmem<D>::at(c0 + i, tok(0));
         *reinterpret_cast<uint32_t*>(&sm.kT_h[o]) = hp;
-        *reinterpret_cast<uint32_t*>(&sm.kT_l[o]) = pack_bf16x2(ph[0][i] - h0, ph[1][i] - h1);
+        const uint32_t lp = pack_bf16x2(ph[0][i] - h0, ph[1][i] - h1);
+        *reinterpret_cast<uint32_t*>(&sm.kT_l[o]) = lp;
+        if constexpr (ROPE)
+          *reinterpret_cast<uint32_t*>(&s3.kT[o]) = third_bf16x2(ph[0][i] - h0, ph[1][i] - h1, lp);
         *reinterpret_cast<uint32_t*>(&sm.vT[o]) = __builtin_amdgcn_perm(v1[i >> 1], v0[i >> 1], sel);
         *reinterpret_cast<uint32_t*>(&kR[o]) = __builtin_amdgcn_perm(k1[i >> 1], k0[i >> 1], sel);
       }
@@ -842,6 +870,10 @@ __global__ __launch_bounds__(256) void append_fused_kernel(
             abf16x8, *reinterpret_cast<const uint4*>(&sm.vT[StateSmem<D>::at(col, 8 * lg)]));
         acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ah, bv, acc[r][c], 0, 0, 0);
         acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(al, bv, acc[r][c], 0, 0, 0);
+        if constexpr (ROPE)
+          acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              __builtin_bit_cast(abf16x8, *reinterpret_cast<const uint4*>(&s3.kT[oa])), bv,
+              acc[r][c], 0, 0, 0);
       }
     }
     // value pieces: piece p = (c >> 4, token group g, c & 15), the order of
@@ -1211,9 +1243,10 @@ hipError_t launch_append_blocks(const Dims& m, const spla_cache& c, const void* 
 template <typename T, int D>
 static void state_partial(const Dims& m, const spla_cache& c, const void* k_new, const void* v_new,
                           int max_new, const int32_t* n_new, const AppendWs& ws, char* base,
-                          hipStream_t st) {
+                          hipStream_t st, bool exact) {
   if constexpr (sizeof(T) == 2)
-    hipLaunchKernelGGL((append_state_mfma_kernel<D>), dim3(ws.n_chunks, m.bh), dim3(256), 0, st,
+    hipLaunchKernelGGL((exact ? append_state_mfma_kernel<D, true>
+                              : append_state_mfma_kernel<D, false>), dim3(ws.n_chunks, m.bh), dim3(256), 0, st,
                        m, c.seq_lens, (const bf16_t*)k_new, (const bf16_t*)v_new, max_new, n_new,
                        ws.n_chunks, ws.chunk_tokens, (float*)(base + ws.part_s),
                        (float*)(base + ws.part_z), false, (int64_t)max_new * D, (int64_t)D);
@@ -1226,36 +1259,33 @@ static void state_partial(const Dims& m, const spla_cache& c, const void* k_new,
 
 hipError_t launch_append_state(const Dims& m, const spla_cache& c, const void* k_new,
                                const void* v_new, int max_new, const int32_t* n_new,
-                               const AppendWs& ws, char* base, hipStream_t st) {
+                               const AppendWs& ws, char* base, hipStream_t st, bool exact,
+                               bool advance) {
   if (m.elem == 4) {
-    if (m.d == 64) state_partial<float, 64>(m, c, k_new, v_new, max_new, n_new, ws, base, st);
-    else state_partial<float, 128>(m, c, k_new, v_new, max_new, n_new, ws, base, st);
+    if (m.d == 64) state_partial<float, 64>(m, c, k_new, v_new, max_new, n_new, ws, base, st, exact);
+    else state_partial<float, 128>(m, c, k_new, v_new, max_new, n_new, ws, base, st, exact);
   } else {
-    if (m.d == 64) state_partial<bf16_t, 64>(m, c, k_new, v_new, max_new, n_new, ws, base, st);
-    else state_partial<bf16_t, 128>(m, c, k_new, v_new, max_new, n_new, ws, base, st);
+    if (m.d == 64) state_partial<bf16_t, 64>(m, c, k_new, v_new, max_new, n_new, ws, base, st, exact);
+    else state_partial<bf16_t, 128>(m, c, k_new, v_new, max_new, n_new, ws, base, st, exact);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(append_state_reduce_kernel, dim3(m.d / kReduceRows, m.bh), dim3(256), 0,
                      st, m, ws.n_chunks, (const float*)(base + ws.part_s),
-                     (const float*)(base + ws.part_z), c.lin_state, c.lin_norm, nullptr, 0,
-                     nullptr);
+                     (const float*)(base + ws.part_z), c.lin_state, c.lin_norm,
+                     advance ? c.seq_lens : nullptr, max_new, n_new);
   return hipGetLastError();
 }
 
 hipError_t launch_block_states(const Dims& m, const spla_cache& c, const void* k_new,
                                const void* v_new, int T, int n_blk, float* part_s, float* part_z,
                                hipStream_t st) {
-  auto kern = m.d == 64 ? append_state_mfma_kernel<64> : append_state_mfma_kernel<128>;
+  auto kern = m.d == 64 ? append_state_mfma_kernel<64, false> : append_state_mfma_kernel<128, false>;
   hipLaunchKernelGGL(kern, dim3((unsigned)n_blk, (unsigned)m.bh), dim3(256), 0, st, m,
                      (const int32_t*)c.seq_lens, (const bf16_t*)k_new, (const bf16_t*)v_new, T,
                      (const int32_t*)nullptr, n_blk, m.B, part_s, part_z, true, (int64_t)m.d,
                      (int64_t)m.bh * m.d);
   return hipGetLastError();
-}
-
-bool append_rope_fusable(const Dims& m, const spla_rope& rope) {
-  return append_fusable(m) && rope.rot_dim % 16 == 0;
 }
 
 bool append_fusable(const Dims& m) { return m.elem == 2 && m.d == 128 && !windowed(m); }

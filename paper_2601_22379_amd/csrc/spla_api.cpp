@@ -364,19 +364,29 @@ extern "C" int32_t spla_append_rope(const spla_config* cfg, const spla_cache* ca
                                           static_cast<hipStream_t>(stream)));
     return SPLA_OK;
   }
-  if (spla::append_rope_fusable(m, *rope)) {
-    SPLA_TRY(spla::launch_append_fused(m, *cache, k_new, v_new, max_new, n_new,
-                                       spla::append_ws_layout(m, max_new), ws + L.append,
-                                       static_cast<hipStream_t>(stream), rope, pos_shift));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const spla::AppendWs A = spla::append_ws_layout(m, max_new);
+  const bool one_pass = spla::append_fusable(m);
+  if (one_pass && rope->rot_dim % 16 == 0) {
+    SPLA_TRY(spla::launch_append_fused(m, *cache, k_new, v_new, max_new, n_new, A, ws + L.append,
+                                       st, rope, pos_shift));
     return SPLA_OK;
   }
   const int64_t s_h = (int64_t)max_new * m.d, s_b = s_h * m.hkv;
   const spla::RotateSet set{k_new, ws + L.k_rot, m.d, s_b, s_h, m.d, s_b, s_h, m.hkv};
   const spla::RotateRows rows{max_new, m.batch, nullptr, cache->seq_lens, pos_shift, n_new};
-  SPLA_TRY(spla::launch_rotate(m, *rope, rows, set, spla::RotateSet{}, false,
-                               static_cast<hipStream_t>(stream)));
-  return spla_append(cfg, cache, ws + L.k_rot, v_new, max_new, n_new, ws + L.append,
-                     (size_t)(L.total - L.append), stream);
+  SPLA_TRY(spla::launch_rotate(m, *rope, rows, set, spla::RotateSet{}, false, st));
+  const void* kr = ws + L.k_rot;
+  if (one_pass) {
+    const spla_rope none{};
+    SPLA_TRY(spla::launch_append_fused(m, *cache, kr, v_new, max_new, n_new, A, ws + L.append, st,
+                                       &none));
+    return SPLA_OK;
+  }
+  SPLA_TRY(spla::launch_append_blocks(m, *cache, kr, v_new, max_new, n_new, st));
+  SPLA_TRY(spla::launch_append_state(m, *cache, kr, v_new, max_new, n_new, A, ws + L.append, st,
+                                     true, true));
+  return SPLA_OK;
 }
 
 extern "C" int32_t spla_attend(const spla_config* cfg, const spla_cache* cache, int32_t n_tokens,

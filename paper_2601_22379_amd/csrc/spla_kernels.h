@@ -26,7 +26,10 @@ hipError_t launch_append_blocks(const Dims& m, const spla_cache& c, const void* 
                                 hipStream_t st, bool position_major = false);
 hipError_t launch_append_state(const Dims& m, const spla_cache& c, const void* k_new,
                                const void* v_new, int max_new, const int32_t* n_new,
-                               const AppendWs& ws, char* wsbase, hipStream_t st);
+                               const AppendWs& ws, char* wsbase, hipStream_t st,
+                               bool exact = false, bool advance = false);
+// (exact: bf16 phi in three terms instead of two; advance: its last kernel also
+// advances seq_lens, and launch_append_finish must not be called)
 // phi(K)^T V (part_s [bh][n_blk][d][d]) and the sums of phi(K) (part_z
 // [bh][n_blk][d]) of the new tokens of each block that T new position-major
 // rows touch, from the block of the append point on (bf16)
@@ -42,9 +45,8 @@ hipError_t launch_append_fused(const Dims& m, const spla_cache& c, const void* k
                                const void* v_new, int max_new, const int32_t* n_new,
                                const AppendWs& ws, char* wsbase, hipStream_t st,
                                const spla_rope* rope = nullptr, const int32_t* shift = nullptr);
-// ... with the keys rotated on the way (rope, shift as in spla_append_rope): the
-// append_fusable shapes with a multiple of 16 rotated coordinates
-bool append_rope_fusable(const Dims& m, const spla_rope& rope);
+// (rope, shift as in spla_append_rope: the keys are rotated on the way, a multiple of
+// 16 coordinates, or none for rows rotated before)
 // the single-token append of a step (statistics, K/V rows and, with rank1,
 // the rank-one update of S_bar and z_bar) in one launch. With fin_ctr (the
 // items_done lines of a decode workspace's synchronisation area) the last
