@@ -609,6 +609,13 @@ __device__ __forceinline__ void copy_to_lds(const void* src, void* dst) {
                                    (__attribute__((address_space(3))) uint32_t*)dst, 16, 0, 0);
 }
 
+// Waits for this wavefront's copies to LDS: the builtin, which the compiler counts (it
+// would otherwise wait for them, and for those issued since, at the reads).
+__device__ __forceinline__ void wait_copies() {
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt 0, the other counts open
+  asm volatile("" ::: "memory");
+}
+
 template <int D, bool CAP, bool BIAS>
 struct TilePass {
   static constexpr int KS = D / 16, CT = D / 32;
@@ -738,6 +745,39 @@ struct TilePass {
   }
 };
 
+// A lane's half of its column's outputs (unnormalised, o[c][4 i + k]: coordinate 32 c +
+// 8 i + 4 h + k) written out, or as record rec where the keys are split.
+template <int D>
+__device__ __forceinline__ void tile_write(const AttendArgs& a, const AttendRow& row, int bh, int h,
+                                           const floatx16 (&o)[D / 32], float ref, float lane_sum,
+                                           int n_eff, int64_t rec) {
+  const float l = lane_sum + xor32(lane_sum);
+  if (n_eff > 1) {
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(a.part + rec * D + 32 * c + 8 * i + 4 * h) =
+            make_float4(o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]);
+    if (h == 0) *reinterpret_cast<float2*>(a.ml + rec * 2) = make_float2(ref, l);
+    return;
+  }
+  if (!row.valid) return;
+  const bool any = row.hi > row.lo;
+  const int64_t at = ((int64_t)row.t * a.m.batch + bh / a.m.hkv) * a.m.hq + row.head;
+  const float inv = any ? 1.f / l : 0.f;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = any ? o[c][4 * i + k] * inv : 0.f;
+      Elem<bf16_t>::store4(static_cast<bf16_t*>(a.out), at * D + 32 * c + 8 * i + 4 * h, y);
+    }
+  if (a.lse && h == 0) a.lse[at] = any ? (ref + log2f(l)) * kLn2 : -INFINITY;
+}
+
 // Maximum over the 32 columns (lanes l % 32) of the wavefront.
 __device__ __forceinline__ int cols32_max(int v) {
 #pragma unroll
@@ -825,7 +865,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
   };
   auto use = [&](TileBuf<D>& buf, TileBuf<D>& other, int kt, int par) {
     const int t0 = (step0 + 2 * kt) * 32;
-    wait_memory();  // this wavefront's copies of tile kt are in LDS
+    wait_copies();  // this wavefront's copies of tile kt are in LDS
     // values that some query may not see (the same for all wavefronts): every
     // wavefront looks through the pieces it copied
     const bool g_inner = t0 >= g_lo_max && t0 + kTileTokens <= g_hi_min;
@@ -858,33 +898,332 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
     if (kt + 1 < last) use(buf1, buf0, kt + 1, 1);
   }
 
-  const float l = ps.l + xor32(ps.l);
   const int64_t u = (int64_t)bh * a.n_tiles + tile;
   if (a.n_split > 1 && split == 0 && tid == 0) a.n_eff[u] = n_eff;
-  if (n_eff > 1) {  // (only where the keys may be split)
-    const int64_t rec = (u * a.n_split + split) * kTileRows + rr;
+  tile_write<D>(a, row, bh, h, ps.o, ps.ref, ps.l, n_eff,
+                (u * a.n_split + split) * kTileRows + rr);
+}
+
+// ------------------------------------------------- overlapped within a wavefront
+// As above with eight wavefronts of 32 rows to a workgroup (256 rows, two wavefronts per
+// SIMD), each of which overlaps by itself: while the vector unit forms the weights of a
+// 32-token step, the matrix cores form the scores of the next and then use the weights,
+// in one run of instructions without a branch (the reference is moved, if it must be,
+// before that run). A step's scores are taken one step ahead and the loads a tile (64
+// tokens) ahead of that: three tiles of keys and values in LDS, which are objects of
+// their own so that the compiler can tell a read of one from the loads into another.
+template <int D>
+struct alignas(16) WideTile {
+  uint4 k[2][D * 4], v[2][D * 4];
+};
+
+enum { kPlain = 0, kCapped = 1, kGeneral = 2 };
+
+// Order of a run's instructions: a few pieces read ahead, then N times a product, the V
+// vector instructions that fit beside it, and the next piece.
+template <int N, int V>
+__device__ __forceinline__ void wide_order() {
+  __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);  // LDS read
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(a.part + rec * D + 32 * c + 8 * i + 4 * h) = make_float4(
-            ps.o[c][4 * i], ps.o[c][4 * i + 1], ps.o[c][4 * i + 2], ps.o[c][4 * i + 3]);
-    if (h == 0) *reinterpret_cast<float2*>(a.ml + rec * 2) = make_float2(ps.ref, l);
-    return;
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix
+    __builtin_amdgcn_sched_group_barrier(0x002, V, 0);  // vector
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
   }
-  if (!row.valid) return;
-  const int64_t orow = ((int64_t)row.t * m.batch + bh / m.hkv) * m.hq + row.head;
-  const float inv = any ? 1.f / l : 0.f;
+}
+
+template <int D, int KIND>
+struct WidePass {
+  static constexpr int KS = D / 16, CT = D / 32;
+  bf16x8 q[KS];
+  floatx16 o[CT], x;  // outputs; scores of the step at hand
+  float ref, l, slope2;
+  int pos, lo, hi;
+  float mul, cap2;
+
+  // x[4 (2 mt + e) + b]: score of token 16 e + 8 h + 4 mt + b of the step
+  static __device__ __forceinline__ int token(int i, int h) {
+    return 16 * ((i >> 2) & 1) + 8 * h + 4 * (i >> 3) + (i & 3);
+  }
+
+  __device__ __forceinline__ floatx16 scores(const uint4* k) const {
+    floatx16 y = floatx16{};
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c)
+    for (int s = 0; s < KS; ++s)
+      y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[32 * s]), q[s], y, 0,
+                                                  0, 0);
+    return y;
+  }
+
+  // Weights of the scores against the reference (which bounds them); their sum to l.
+  // MASK: none for the tokens (of the step at t0) that a query does not see.
+  template <bool MASK>
+  __device__ __forceinline__ void weights(bf16x8 (&p)[2], int t0 = 0, int h = 0) {
+    [[maybe_unused]] const uint32_t a = (uint32_t)(t0 + 8 * h - lo), n = (uint32_t)(hi - lo);
+    const float rf = ref == -INFINITY ? 0.f : ref;
+    float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float y[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) y[k] = any ? ps.o[c][4 * i + k] * inv : 0.f;
-      Elem<bf16_t>::store4(static_cast<bf16_t*>(a.out), orow * D + 32 * c + 8 * i + 4 * h, y);
+    for (int i = 0; i < 16; ++i) {
+      float w;
+      if constexpr (KIND == kPlain) {
+        w = __builtin_amdgcn_exp2f(fmaf(x[i], mul, -rf));
+      } else if constexpr (KIND == kCapped) {
+        const float e = __builtin_amdgcn_exp2f(x[i] * mul) + 1.f;
+        w = __builtin_amdgcn_exp2f(fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(e), cap2));
+        if constexpr (MASK) w = a + (uint32_t)token(i, 0) < n ? w : 0.f;
+      } else {
+        w = __builtin_amdgcn_exp2f(x[i] - rf);
+      }
+      sum += w;
+      // weights rounded to bf16 for the product (the sum keeps fp32)
+      p[(i >> 2) & 1][4 * (i >> 3) + (i & 3)] = (__bf16)w;
     }
-  if (a.lse && h == 0) a.lse[orow] = any ? (ps.ref + log2f(l)) * kLn2 : -INFINITY;
+    l += sum;
+  }
+
+  __device__ __forceinline__ void product(const uint4* v, const bf16x8 (&p)[2]) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+        o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, v[128 * ct + 32 * e]), p[e], o[ct], 0, 0, 0);
+  }
+
+  // What the infinities and NaN among a step's values add to the queries that see them
+  // (see odd_marks), ahead of the product with the values without them.
+  __device__ __forceinline__ void odd_values(const uint4* v, int t0, int h) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      floatx16 n = floatx16{};
+#pragma unroll 1
+      for (int e = 0; e < 2; ++e) {
+        const uint4 y = v[128 * ct + 32 * e];
+        uint32_t w[4] = {y.x, y.y, y.z, y.w}, u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = odd_marks(w[i]);
+        bf16x8 seen;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int t = t0 + 16 * e + 8 * h + k;
+          seen[k] = (__bf16)(t >= lo && t < hi ? 1.f : 0.f);
+        }
+        n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), seen, n, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[ct][i] += odd_sum(n[i]);
+      asm volatile("" : "+v"(o[ct]));  // done here, before the next coordinates' counts
+    }
+  }
+
+  // Scores of the step at t0 made ready: bias and cap (general), - infinity for keys that
+  // a query does not see, and the reference moved where a score passes it by 2^8 (each
+  // query's by its own scores). The scores of a bounded cap need none of it.
+  __device__ __forceinline__ void ready(int t0, bool inner, int h) {
+    if constexpr (KIND == kCapped) return;
+    if constexpr (KIND == kGeneral) {
+      const float base = (float)(pos - t0);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float y = x[i] * mul;
+        if (cap2 > 0.f)
+          y = cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.f));
+        x[i] = fmaf(-slope2, fabsf(base - (float)token(i, h)), y);
+      }
+    }
+    if (!inner) {
+      const uint32_t a = (uint32_t)(t0 + 8 * h - lo), n = (uint32_t)(hi - lo);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)  // lo <= token < hi
+        x[i] = a + (uint32_t)token(i, 0) < n ? x[i] : -INFINITY;
+    }
+    float nm = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) nm = fmaxf(nm, x[i]);
+    nm = fmaxf(nm, xor32(nm));
+    if constexpr (KIND == kPlain) nm *= mul;
+    const bool move = nm > ref + 8.f;
+    if (__any(move)) {
+      // (never zero: an infinity that odd_values left would become NaN)
+      const float alpha = move ? __builtin_amdgcn_exp2f(fmaxf(ref - nm, -126.f)) : 1.f;
+      ref = move ? nm : ref;
+      l *= alpha;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[ct][i] *= alpha;
+    }
+  }
+};
+
+template <int D, int KIND>
+__global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a) {
+  __shared__ WideTile<D> tile0, tile1, tile2;
+  __shared__ int4 s_range[8];
+  __shared__ __align__(16) int s_odd[3][8];
+  const Dims& m = a.m;
+  const int bh = (int)(blockIdx.x % (unsigned)m.bh);
+  // tiles of late queries, which see the most keys, first
+  const int tile = a.n_tiles - 1 - (a.tile0 + (int)(blockIdx.x / (unsigned)m.bh));
+  const int split = (int)blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, h = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int L = attend_length(a, bh);
+  const AttendRow row = attend_row(a, (int64_t)tile * kWideRows + w * 32 + r, bh, L);
+  const bool any = row.hi > row.lo;
+  WidePass<D, KIND> ps;
+  {
+    const int64_t at = row.valid ? ((int64_t)row.t * m.batch + bh / m.hkv) * m.hq + row.head : 0;
+    const bf16_t* qp = static_cast<const bf16_t*>(a.q) + at * D + 8 * h;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      ps.q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + 16 * s));
+#pragma unroll
+    for (int ct = 0; ct < D / 32; ++ct) ps.o[ct] = floatx16{};
+    const ScoreMap map(a, row.valid ? row.head : 0);
+    ps.mul = map.mul;
+    ps.cap2 = map.cap2;
+    ps.slope2 = map.slope2;
+    ps.ref = KIND == kCapped ? 0.f : -INFINITY;
+    ps.l = 0.f;
+    ps.pos = row.pos;
+    ps.lo = row.lo;
+    ps.hi = row.hi;
+  }
+  // keys of this wavefront's queries, and those that all of its (non-empty) ones see
+  int lo_min = -cols32_max(any ? -row.lo : -INT32_MAX), hi_max = cols32_max(row.hi);
+  int lo_max = cols32_max(any ? row.lo : 0), hi_min = -cols32_max(any ? -row.hi : -INT32_MAX);
+  if (lane == 0) s_range[w] = make_int4(lo_min, hi_max, lo_max, hi_min);
+  __syncthreads();
+  int4 g = s_range[0];  // of the workgroup's
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    const int4 x = s_range[i];
+    g = make_int4(min(g.x, x.x), max(g.y, x.y), max(g.z, x.z), min(g.w, x.w));
+  }
+  const int g_lo = __builtin_amdgcn_readfirstlane(g.x), g_hi = __builtin_amdgcn_readfirstlane(g.y);
+  const int g_lo_max = __builtin_amdgcn_readfirstlane(g.z);
+  const int g_hi_min = __builtin_amdgcn_readfirstlane(g.w);
+  lo_min = __builtin_amdgcn_readfirstlane(lo_min);
+  hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+  lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+  hi_min = __builtin_amdgcn_readfirstlane(hi_min);
+  const int step0 = g_hi > 0 ? g_lo / 32 : 0, step_end = g_hi > 0 ? (g_hi + 31) / 32 : 0;
+  const int n_kt = (step_end - step0 + 1) / 2;  // tiles of keys
+  const int per = max((n_kt + a.n_split - 1) / a.n_split, kTileMinSplit);
+  const int n_eff = (n_kt + per - 1) / per;
+  if (split > 0 && split >= n_eff) return;
+  const int first = split * per, last = min(first + per, n_kt);
+
+  // wavefront w copies pieces w, w + 8, ... (1 KiB each) of a tile's two steps; a step
+  // past the last is the last again (masked)
+  const int sh = m.B == 32 ? 0 : m.B == 64 ? 1 : 2;  // log2 of the steps per block
+  constexpr int PPS = D / 16;  // pieces per step
+  auto load = [&](const void* src, uint4 (&dst)[2][D * 4], int kt) {
+#pragma unroll
+    for (int i = 0; i < 2 * PPS; i += 8) {
+      const int s2 = (i + w) / PPS, pc = (i + w) % PPS;
+      const int st = min(step0 + 2 * kt + s2, step_end - 1);
+      const int64_t at = (attend_slot(a, bh, st >> sh) * m.B + (st & ((1 << sh) - 1)) * 32) * D;
+      copy_to_lds(reinterpret_cast<const char*>(static_cast<const bf16_t*>(src) + at) + pc * 1024 +
+                      lane * 16,
+                  &dst[s2][pc * 64]);
+    }
+  };
+  const int at_k = (r >> 4) * (D * 2) + 16 * h + (r & 15), at_v = (r >> 4) * 64 + 16 * h + (r & 15);
+  auto none = [&](int t0) { return t0 >= hi_max || t0 + 32 <= lo_min; };  // of this wavefront
+  // tile kt in `cur`: the keys of kt + 1 are in `nxt`, whose values are on their way
+  auto use = [&](WideTile<D>& cur, WideTile<D>& nxt, WideTile<D>& far, int kt, int* odd) {
+    wait_copies();  // this wavefront's copies: values of tile kt, keys of kt + 1
+    const int tile_t0 = (step0 + 2 * kt) * 32;
+    const bool g_inner = tile_t0 >= g_lo_max && tile_t0 + kTileTokens <= g_hi_min;
+    if (!g_inner) {  // every wavefront looks through the values it copied
+      uint32_t bad = 0u;
+#pragma unroll
+      for (int i = 0; i < 2 * PPS; i += 8) {
+        const uint4 v = cur.v[(i + w) / PPS][(i + w) % PPS * 64 + lane];
+        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          bad |= ((x[k] & 0x7F80u) == 0x7F80u || (x[k] & 0x7F800000u) == 0x7F800000u) ? 1u : 0u;
+      }
+      const bool one = __any(bad != 0u);
+      if (lane == 0) odd[w] = one;
+    }
+    __syncthreads();
+    if (kt + 2 < last) load(a.k, far.k, kt + 2);
+    if (kt + 1 < last) load(a.v, nxt.v, kt + 1);
+    const int4* of = reinterpret_cast<const int4*>(odd);
+    if (__builtin_expect(!g_inner && (of[0].x | of[0].y | of[0].z | of[0].w | of[1].x | of[1].y |
+                                      of[1].z | of[1].w), 0)) {
+#pragma unroll 1
+      for (int s2 = 0; s2 < 2; ++s2) ps.odd_values(&cur.v[s2][at_v], tile_t0 + 32 * s2, h);
+      __syncthreads();  // (the same for all wavefronts) then they leave the values
+#pragma unroll
+      for (int i = 0; i < 2 * PPS; i += 8) {
+        uint4& v = cur.v[(i + w) / PPS][(i + w) % PPS * 64 + lane];
+        uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) odd_marks(x[k]);
+        v = make_uint4(x[0], x[1], x[2], x[3]);
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      const int t0 = tile_t0 + 32 * s2;
+      const uint4* kp = s2 == 0 ? &cur.k[1][at_k] : &nxt.k[0][at_k];  // of the next step
+      const bool now = !none(t0), next = (s2 == 0 || kt + 1 < last) && !none(t0 + 32);
+      if (!now && !next) continue;
+      // one path for every step, so that the outputs keep their registers: a step of which
+      // this wavefront sees nothing has weights of zero, scores past the last are not used
+      const bool inner = t0 >= lo_max && t0 + 32 <= hi_min;
+      ps.ready(t0, inner, h);
+      bf16x8 p[2];
+      floatx16 y;
+      if constexpr (KIND == kCapped) {
+        if (inner) {
+          __builtin_amdgcn_sched_barrier(0);
+          y = ps.scores(kp);
+          ps.template weights<false>(p);
+          wide_order<D / 16, 6>();
+        } else {
+          ps.template weights<true>(p, t0, h);
+          y = ps.scores(kp);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        ps.product(&cur.v[s2][at_v], p);
+      } else {
+        __builtin_amdgcn_sched_barrier(0);
+        y = ps.scores(kp);
+        ps.template weights<false>(p);
+        ps.product(&cur.v[s2][at_v], p);
+        wide_order<D / 16 + 2 * (D / 32), 5>();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      ps.x = y;
+    }
+  };
+  if (first < last) {
+    load(a.k, tile0.k, first);
+    load(a.v, tile0.v, first);
+    if (first + 1 < last) load(a.k, tile1.k, first + 1);
+    wait_copies();
+    __syncthreads();
+    if (!none((step0 + 2 * first) * 32)) ps.x = ps.scores(&tile0.k[0][at_k]);
+  }
+#pragma unroll 1
+  for (int kt = first; kt < last; kt += 3) {
+    use(tile0, tile1, tile2, kt, s_odd[0]);
+    if (kt + 1 < last) use(tile1, tile2, tile0, kt + 1, s_odd[1]);
+    if (kt + 2 < last) use(tile2, tile0, tile1, kt + 2, s_odd[2]);
+  }
+
+  const int64_t u = (int64_t)bh * a.n_tiles + tile;
+  if (a.n_split > 1 && split == 0 && tid == 0) a.n_eff[u] = n_eff;
+  tile_write<D>(a, row, bh, h, ps.o, ps.ref, ps.l, n_eff,
+                (u * a.n_split + split) * kWideRows + w * 32 + r);
 }
 
 static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
@@ -895,7 +1234,8 @@ static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
     for (a.tile0 = 0; a.tile0 < a.n_tiles; a.tile0 += most) {
       const int n = a.n_tiles - a.tile0 < most ? a.n_tiles - a.tile0 : most;
       const unsigned wgs = (unsigned)a.m.bh * (unsigned)n;
-      hipLaunchKernelGGL(kern, dim3(wgs, (unsigned)a.n_split), dim3(256), 0, st, a);
+      hipLaunchKernelGGL(kern, dim3(wgs, (unsigned)a.n_split), dim3(a.rows == kWideRows ? 512 : 256), 0,
+                         st, a);
       if (a.n_split > 1 && join)
         hipLaunchKernelGGL(join, dim3(wgs * (unsigned)(a.rows / 16)), dim3(256), 0, st, a);
     }
@@ -909,7 +1249,19 @@ static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
     else if (bias) go(attend_tile_kernel<D, false, true>, join);
     else go(attend_tile_kernel<D, false, false>, join);
   };
-  if (a.rows == kTileRows) {
+  // a cap this small bounds every score: weights against a reference of 0 stay in range
+  const bool bounded = cap && !bias && a.o.softcap * kLog2e <= 60.f;
+  const auto wide = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    const auto join = attend_join_kernel<D>;
+    if (bounded) go(attend_wide_kernel<D, kCapped>, join);
+    else if (cap || bias) go(attend_wide_kernel<D, kGeneral>, join);
+    else go(attend_wide_kernel<D, kPlain>, join);
+  };
+  if (a.rows == kWideRows) {
+    if (a.m.d == 64) wide(std::integral_constant<int, 64>{});
+    else wide(std::integral_constant<int, 128>{});
+  } else if (a.rows == kTileRows) {
     if (a.m.d == 64) tile(std::integral_constant<int, 64>{});
     else tile(std::integral_constant<int, 128>{});
   } else if (a.m.elem == 4) {
