@@ -48,9 +48,9 @@ struct AttendRow {
 __device__ __forceinline__ AttendRow attend_row(const AttendArgs& a, int64_t r, int bh, int L) {
   const int b = bh / a.m.hkv, G = a.m.group;
   AttendRow w;
-  const int64_t t = r / G;
-  w.t = (int)t;
-  w.head = (bh % a.m.hkv) * G + (int)(r - t * G);
+  const int t = (int)r / G;  // (tokens of a call times group: below 2^27)
+  w.t = t;
+  w.head = (bh % a.m.hkv) * G + (int)r - t * G;
   int n = a.o.n_new ? a.o.n_new[b] : a.n_tokens;
   n = n < 0 ? 0 : n > a.n_tokens ? a.n_tokens : n;
   w.valid = t < n;
@@ -61,7 +61,7 @@ __device__ __forceinline__ AttendRow attend_row(const AttendArgs& a, int64_t r, 
     if (a.o.prefix_len) hi = max(hi, a.o.prefix_len[b]);
     hi = min(hi, L);
     int lo = 0;
-    if (a.o.first_key) lo = max(0, a.o.first_key[t * a.m.batch + b]);
+    if (a.o.first_key) lo = max(0, a.o.first_key[(int64_t)t * a.m.batch + b]);
     if (lo < hi) {
       w.lo = lo;
       w.hi = hi;
@@ -285,11 +285,16 @@ struct StepOps<float, D> {
   }
 };
 
-// Maximum / minimum over the 16 columns (lanes l % 16) of the wavefront.
+// Maximum over the columns of the wavefront's rows, lanes l % 16 (or l % 32), which the
+// other lanes repeat; the same in every lane, so kept in a scalar register.
+template <int COLS>
 __device__ __forceinline__ int cols_max(int v) {
-#pragma unroll
-  for (int s = 1; s < 16; s *= 2) v = max(v, __shfl_xor(v, s, 64));
-  return v;
+  v = max(v, (int)dpp_u32<0x128, 0xF>(0u, (uint32_t)v));  // row_ror:8
+  v = max(v, (int)dpp_u32<0x124, 0xF>(0u, (uint32_t)v));  // row_ror:4
+  v = max(v, (int)dpp_u32<0x4E, 0xF>(0u, (uint32_t)v));   // quad_perm [2,3,0,1]
+  v = max(v, (int)dpp_u32<0xB1, 0xF>(0u, (uint32_t)v));   // quad_perm [1,0,3,2]
+  if (COLS == 32) v = max(v, (int)lane_xor16((uint32_t)v));
+  return __builtin_amdgcn_readfirstlane(v);
 }
 
 // Row r of a tile written out: c0 .. of its output from unnormalised o, sum l and
@@ -336,8 +341,8 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
   const AttendRow row = attend_row(a, (int64_t)tile * kAttendRows + j, bh, L);
   const bool any = row.hi > row.lo;
   // the tile's keys, and those that all of its (non-empty) queries see
-  const int lo_min = -cols_max(any ? -row.lo : -INT32_MAX), hi_max = cols_max(row.hi);
-  const int lo_max = cols_max(any ? row.lo : 0), hi_min = -cols_max(any ? -row.hi : -INT32_MAX);
+  const int lo_min = -cols_max<16>(any ? -row.lo : -INT32_MAX), hi_max = cols_max<16>(row.hi);
+  const int lo_max = cols_max<16>(any ? row.lo : 0), hi_min = -cols_max<16>(any ? -row.hi : -INT32_MAX);
   const int step0 = hi_max > 0 ? lo_min / 32 : 0;
   const int n_steps = hi_max > 0 ? (hi_max + 31) / 32 - step0 : 0;
   const int per = max((n_steps + a.n_split - 1) / a.n_split, kAttendMinSteps);
@@ -616,7 +621,10 @@ __device__ __forceinline__ void wait_copies() {
   asm volatile("" ::: "memory");
 }
 
-template <int D, bool CAP, bool BIAS>
+// kCapped: a cap that bounds all scores, no bias; kGeneral: any cap, and a bias
+enum { kPlain = 0, kCapped = 1, kBiased = 2, kGeneral = 3 };
+
+template <int D, int KIND>
 struct TilePass {
   static constexpr int KS = D / 16, CT = D / 32;
   bf16x8 q[KS];
@@ -625,13 +633,17 @@ struct TilePass {
   int pos, lo, hi;    // this column's query
   float mul, cap2, slope2;
 
+  // c log2 e tanh(z / 2) of a product z scaled to 2 log2 e / c (see ScoreMap)
+  __device__ __forceinline__ float capped(float z) const {
+    return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z) + 1.f), cap2);
+  }
+
   // x[16 s2 + 4 (2 mt + e) + b]: score of token 32 s2 + 16 e + 8 h + 4 mt + b
   static __device__ __forceinline__ int token(int i, int h) {
     return 32 * (i >> 4) + 16 * ((i >> 2) & 1) + 8 * h + 4 * ((i >> 3) & 1) + (i & 3);
   }
 
-  __device__ __forceinline__ void step(const TileBuf<D>& buf, int t0, bool inner, bool odd,
-                                       int lane) {
+  __device__ __forceinline__ void step(const TileBuf<D>& buf, int t0, bool inner, int lane) {
     const int r = lane & 31, h = lane >> 5;
     // pieces of this lane's score row and of its value coordinate: coordinates 16 s
     // + 8 h .. + 7 at + 32 s, coordinate 32 c + r, tokens 16 e + 8 h .. at + 128 c + 32 e
@@ -648,15 +660,18 @@ struct TilePass {
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (CAP || BIAS) {
-      const float base = (float)(pos - t0);
+    if constexpr (KIND == kBiased || KIND == kGeneral) {
+      const float base = (float)(pos - t0 - 8 * h);
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
         float y = x[i >> 4][i & 15] * mul;
-        if constexpr (CAP) y = cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.f));
-        if constexpr (BIAS) y = fmaf(-slope2, fabsf(base - (float)token(i, h)), y);
-        x[i >> 4][i & 15] = y;
+        if constexpr (KIND == kGeneral) y = capped(y);
+        x[i >> 4][i & 15] = fmaf(-slope2, fabsf(base - (float)token(i, 0)), y);
       }
+    }
+    if constexpr (KIND == kCapped) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i >> 4][i & 15] = capped(x[i >> 4][i & 15] * mul);
     }
     if (!inner) {
       const uint32_t a = (uint32_t)(t0 + 8 * h - lo), n = (uint32_t)(hi - lo);
@@ -664,23 +679,26 @@ struct TilePass {
       for (int i = 0; i < 32; ++i)  // lo <= token < hi
         x[i >> 4][i & 15] = a + (uint32_t)token(i, 0) < n ? x[i >> 4][i & 15] : -INFINITY;
     }
-    float nm = x[0][0];
+    if constexpr (KIND != kCapped) {
+      float nm = x[0][0];
 #pragma unroll
-    for (int i = 1; i < 32; ++i) nm = fmaxf(nm, x[i >> 4][i & 15]);
-    nm = fmaxf(nm, xor32(nm));
-    if constexpr (!(CAP || BIAS)) nm *= mul;
-    // the reference moves only when a score passes it by 2^8: weights up to there
-    // are as exact in bf16 and fp32, and the outputs are scaled a few times only
-    // (each query's by its own scores, so that no query's rounding hangs on another's)
-    const bool move = nm > ref + 8.f;
-    if (__any(move)) {
-      const float alpha = move ? __builtin_amdgcn_exp2f(ref - nm) : 1.f;
-      ref = move ? nm : ref;
-      l *= alpha;
+      for (int i = 1; i < 32; ++i) nm = fmaxf(nm, x[i >> 4][i & 15]);
+      nm = fmaxf(nm, xor32(nm));
+      if constexpr (KIND == kPlain) nm *= mul;
+      // the reference moves only when a score passes it by 2^8: weights up to there are as
+      // exact in bf16 and fp32, and the outputs are scaled a few times only (each query's
+      // by its own scores, so that no query's rounding hangs on another's)
+      const bool move = nm > ref + 8.f;
+      if (__any(move)) {
+        // (never zero: an infinity that odd_values left would become NaN)
+        const float alpha = move ? __builtin_amdgcn_exp2f(fmaxf(ref - nm, -126.f)) : 1.f;
+        ref = move ? nm : ref;
+        l *= alpha;
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
+        for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[c][i] *= alpha;
+          for (int i = 0; i < 16; ++i) o[c][i] *= alpha;
+      }
     }
     const float rf = ref == -INFINITY ? 0.f : ref;
     bf16x8 p[4];
@@ -688,17 +706,14 @@ struct TilePass {
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
       const float y = x[i >> 4][i & 15];
-      const float w = __builtin_amdgcn_exp2f(CAP || BIAS ? y - rf : fmaf(y, mul, -rf));
+      const float w = __builtin_amdgcn_exp2f(KIND == kPlain ? fmaf(y, mul, -rf)
+                                             : KIND == kCapped ? y : y - rf);
       sum += w;
       // weights rounded to bf16 for the product (the sum keeps fp32)
       p[2 * (i >> 4) + ((i >> 2) & 1)][4 * ((i >> 3) & 1) + (i & 3)] = (__bf16)w;
     }
     l += sum;
     __builtin_amdgcn_sched_barrier(0);
-    if (__builtin_expect(odd && !inner, 0)) {
-      odd_values(buf, t0, lane, p);
-      return;
-    }
 #pragma unroll
     for (int e = 0; e < 4; ++e)  // tokens 16 e .. + 15 of the tile
 #pragma unroll
@@ -709,20 +724,17 @@ struct TilePass {
       }
   }
 
-  // The product of a tile with infinities or NaN among its values, some of which
-  // some query of the wavefront does not see: taken out of the product and given
-  // to the queries that see them.
-  __device__ __forceinline__ void odd_values(const TileBuf<D>& buf, int t0, int lane,
-                                             const bf16x8 (&p)[4]) {
+  // What the infinities and NaN among a tile's values add to the queries that see them
+  // (see odd_marks), ahead of the product with the values without them.
+  __device__ __forceinline__ void odd_values(const TileBuf<D>& buf, int t0, int lane) {
     const int r = lane & 31, h = lane >> 5;
+    const int at_v = (r >> 4) * 64 + 16 * h + (r & 15);
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-      // per query, values it sees: 1 for each + infinity, 128 for each - infinity and
-      // 129 for each NaN (at most 64 of them)
-      floatx16 seen_odd = floatx16{};
+      floatx16 n = floatx16{};
 #pragma unroll 1
       for (int e = 0; e < 4; ++e) {
-        const uint4 v = buf.v[e >> 1][(2 * c + (r >> 4)) * 64 + (2 * (e & 1) + h) * 16 + (r & 15)];
+        const uint4 v = buf.v[e >> 1][at_v + 128 * c + 32 * (e & 1)];
         uint32_t w[4] = {v.x, v.y, v.z, v.w}, u[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = odd_marks(w[i]);
@@ -732,14 +744,11 @@ struct TilePass {
           const int t = t0 + 16 * e + 8 * h + k;
           seen[k] = (__bf16)(t >= lo && t < hi ? 1.f : 0.f);
         }
-        const bf16x8 pe = e == 0 ? p[0] : e == 1 ? p[1] : e == 2 ? p[2] : p[3];
-        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3])), pe, o[c], 0, 0, 0);
-        seen_odd = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), seen, seen_odd, 0, 0, 0);
+        n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), seen, n, 0, 0, 0);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[c][i] += odd_sum(seen_odd[i]);
+      for (int i = 0; i < 16; ++i) o[c][i] += odd_sum(n[i]);
       asm volatile("" : "+v"(o[c]));  // done here, before the next coordinates' counts
     }
   }
@@ -778,14 +787,7 @@ __device__ __forceinline__ void tile_write(const AttendArgs& a, const AttendRow&
   if (a.lse && h == 0) a.lse[at] = any ? (ref + log2f(l)) * kLn2 : -INFINITY;
 }
 
-// Maximum over the 32 columns (lanes l % 32) of the wavefront.
-__device__ __forceinline__ int cols32_max(int v) {
-#pragma unroll
-  for (int s = 1; s < 32; s *= 2) v = max(v, __shfl_xor(v, s, 64));
-  return v;
-}
-
-template <int D, bool CAP, bool BIAS>
+template <int D, int KIND>
 __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
   __shared__ TileBuf<D> buf0, buf1;
   __shared__ int4 s_range[4];
@@ -802,9 +804,9 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
   const AttendRow row = attend_row(a, (int64_t)tile * kTileRows + rr, bh, L);
   const bool any = row.hi > row.lo;
   // keys of this wavefront's queries, and those that all of its (non-empty) ones see
-  const int lo_min = -cols32_max(any ? -row.lo : -INT32_MAX), hi_max = cols32_max(row.hi);
-  const int lo_max = cols32_max(any ? row.lo : 0);
-  const int hi_min = -cols32_max(any ? -row.hi : -INT32_MAX);
+  const int lo_min = -cols_max<32>(any ? -row.lo : -INT32_MAX), hi_max = cols_max<32>(row.hi);
+  const int lo_max = cols_max<32>(any ? row.lo : 0);
+  const int hi_min = -cols_max<32>(any ? -row.hi : -INT32_MAX);
   if (lane == 0) s_range[w] = make_int4(lo_min, hi_max, lo_max, hi_min);
   __syncthreads();
   int4 g = s_range[0];  // of the workgroup's
@@ -824,7 +826,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
   if (split > 0 && split >= n_eff) return;
   const int first = split * per, last = min(first + per, n_kt);
 
-  TilePass<D, CAP, BIAS> ps;
+  TilePass<D, KIND> ps;
   const int64_t qrow = row.valid ? ((int64_t)row.t * m.batch + bh / m.hkv) * m.hq + row.head : 0;
   const bf16_t* qp = static_cast<const bf16_t*>(a.q) + qrow * D + 8 * h;
 #pragma unroll
@@ -839,7 +841,7 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
   ps.mul = map.mul;
   ps.cap2 = map.cap2;
   ps.slope2 = map.slope2;
-  ps.ref = -INFINITY;
+  ps.ref = KIND == kCapped ? 0.f : -INFINITY;
   ps.l = 0.f;
   ps.pos = row.pos;
   ps.lo = row.lo;
@@ -886,10 +888,24 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
     }
     __syncthreads();
     if (kt + 1 < last) load(other, kt + 1);
+    if (__builtin_expect(!g_inner && (s_odd[par][0] | s_odd[par][1] | s_odd[par][2] | s_odd[par][3]),
+                         0)) {  // the same for all wavefronts
+      ps.odd_values(buf, t0, lane);
+      __syncthreads();  // then they leave the values
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+          uint4& v = buf.v[s2][(w + 4 * i) * 64 + lane];
+          uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) odd_marks(x[k]);
+          v = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+      __syncthreads();
+    }
     if (t0 >= hi_max || t0 + kTileTokens <= lo_min) return;  // nothing here for this wavefront
-    const bool inner = t0 >= lo_max && t0 + kTileTokens <= hi_min;
-    const bool odd = !inner && (s_odd[par][0] | s_odd[par][1] | s_odd[par][2] | s_odd[par][3]);
-    ps.step(buf, t0, inner, odd, lane);
+    ps.step(buf, t0, t0 >= lo_max && t0 + kTileTokens <= hi_min, lane);
   };
   if (first < last) load(buf0, first);
 #pragma unroll 1
@@ -904,328 +920,6 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
                 (u * a.n_split + split) * kTileRows + rr);
 }
 
-// ------------------------------------------------- overlapped within a wavefront
-// As above with eight wavefronts of 32 rows to a workgroup (256 rows, two wavefronts per
-// SIMD), each of which overlaps by itself: while the vector unit forms the weights of a
-// 32-token step, the matrix cores form the scores of the next and then use the weights,
-// in one run of instructions without a branch (the reference is moved, if it must be,
-// before that run). A step's scores are taken one step ahead and the loads a tile (64
-// tokens) ahead of that: three tiles of keys and values in LDS, which are objects of
-// their own so that the compiler can tell a read of one from the loads into another.
-template <int D>
-struct alignas(16) WideTile {
-  uint4 k[2][D * 4], v[2][D * 4];
-};
-
-enum { kPlain = 0, kCapped = 1, kGeneral = 2 };
-
-// Order of a run's instructions: a few pieces read ahead, then N times a product, the V
-// vector instructions that fit beside it, and the next piece.
-template <int N, int V>
-__device__ __forceinline__ void wide_order() {
-  __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);  // LDS read
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix
-    __builtin_amdgcn_sched_group_barrier(0x002, V, 0);  // vector
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-  }
-}
-
-template <int D, int KIND>
-struct WidePass {
-  static constexpr int KS = D / 16, CT = D / 32;
-  bf16x8 q[KS];
-  floatx16 o[CT], x;  // outputs; scores of the step at hand
-  float ref, l, slope2;
-  int pos, lo, hi;
-  float mul, cap2;
-
-  // x[4 (2 mt + e) + b]: score of token 16 e + 8 h + 4 mt + b of the step
-  static __device__ __forceinline__ int token(int i, int h) {
-    return 16 * ((i >> 2) & 1) + 8 * h + 4 * (i >> 3) + (i & 3);
-  }
-
-  __device__ __forceinline__ floatx16 scores(const uint4* k) const {
-    floatx16 y = floatx16{};
-#pragma unroll
-    for (int s = 0; s < KS; ++s)
-      y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[32 * s]), q[s], y, 0,
-                                                  0, 0);
-    return y;
-  }
-
-  // Weights of the scores against the reference (which bounds them); their sum to l.
-  // MASK: none for the tokens (of the step at t0) that a query does not see.
-  template <bool MASK>
-  __device__ __forceinline__ void weights(bf16x8 (&p)[2], int t0 = 0, int h = 0) {
-    [[maybe_unused]] const uint32_t a = (uint32_t)(t0 + 8 * h - lo), n = (uint32_t)(hi - lo);
-    const float rf = ref == -INFINITY ? 0.f : ref;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float w;
-      if constexpr (KIND == kPlain) {
-        w = __builtin_amdgcn_exp2f(fmaf(x[i], mul, -rf));
-      } else if constexpr (KIND == kCapped) {
-        const float e = __builtin_amdgcn_exp2f(x[i] * mul) + 1.f;
-        w = __builtin_amdgcn_exp2f(fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(e), cap2));
-        if constexpr (MASK) w = a + (uint32_t)token(i, 0) < n ? w : 0.f;
-      } else {
-        w = __builtin_amdgcn_exp2f(x[i] - rf);
-      }
-      sum += w;
-      // weights rounded to bf16 for the product (the sum keeps fp32)
-      p[(i >> 2) & 1][4 * (i >> 3) + (i & 3)] = (__bf16)w;
-    }
-    l += sum;
-  }
-
-  __device__ __forceinline__ void product(const uint4* v, const bf16x8 (&p)[2]) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-        o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8, v[128 * ct + 32 * e]), p[e], o[ct], 0, 0, 0);
-  }
-
-  // What the infinities and NaN among a step's values add to the queries that see them
-  // (see odd_marks), ahead of the product with the values without them.
-  __device__ __forceinline__ void odd_values(const uint4* v, int t0, int h) {
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      floatx16 n = floatx16{};
-#pragma unroll 1
-      for (int e = 0; e < 2; ++e) {
-        const uint4 y = v[128 * ct + 32 * e];
-        uint32_t w[4] = {y.x, y.y, y.z, y.w}, u[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = odd_marks(w[i]);
-        bf16x8 seen;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int t = t0 + 16 * e + 8 * h + k;
-          seen[k] = (__bf16)(t >= lo && t < hi ? 1.f : 0.f);
-        }
-        n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), seen, n, 0, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[ct][i] += odd_sum(n[i]);
-      asm volatile("" : "+v"(o[ct]));  // done here, before the next coordinates' counts
-    }
-  }
-
-  // Scores of the step at t0 made ready: bias and cap (general), - infinity for keys that
-  // a query does not see, and the reference moved where a score passes it by 2^8 (each
-  // query's by its own scores). The scores of a bounded cap need none of it.
-  __device__ __forceinline__ void ready(int t0, bool inner, int h) {
-    if constexpr (KIND == kCapped) return;
-    if constexpr (KIND == kGeneral) {
-      const float base = (float)(pos - t0);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float y = x[i] * mul;
-        if (cap2 > 0.f)
-          y = cap2 * (1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.f));
-        x[i] = fmaf(-slope2, fabsf(base - (float)token(i, h)), y);
-      }
-    }
-    if (!inner) {
-      const uint32_t a = (uint32_t)(t0 + 8 * h - lo), n = (uint32_t)(hi - lo);
-#pragma unroll
-      for (int i = 0; i < 16; ++i)  // lo <= token < hi
-        x[i] = a + (uint32_t)token(i, 0) < n ? x[i] : -INFINITY;
-    }
-    float nm = x[0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) nm = fmaxf(nm, x[i]);
-    nm = fmaxf(nm, xor32(nm));
-    if constexpr (KIND == kPlain) nm *= mul;
-    const bool move = nm > ref + 8.f;
-    if (__any(move)) {
-      // (never zero: an infinity that odd_values left would become NaN)
-      const float alpha = move ? __builtin_amdgcn_exp2f(fmaxf(ref - nm, -126.f)) : 1.f;
-      ref = move ? nm : ref;
-      l *= alpha;
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[ct][i] *= alpha;
-    }
-  }
-};
-
-template <int D, int KIND>
-__global__ __launch_bounds__(512, 2) void attend_wide_kernel(AttendArgs a) {
-  __shared__ WideTile<D> tile0, tile1, tile2;
-  __shared__ int4 s_range[8];
-  __shared__ __align__(16) int s_odd[3][8];
-  const Dims& m = a.m;
-  const int bh = (int)(blockIdx.x % (unsigned)m.bh);
-  // tiles of late queries, which see the most keys, first
-  const int tile = a.n_tiles - 1 - (a.tile0 + (int)(blockIdx.x / (unsigned)m.bh));
-  const int split = (int)blockIdx.y;
-  const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, h = lane >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int L = attend_length(a, bh);
-  const AttendRow row = attend_row(a, (int64_t)tile * kWideRows + w * 32 + r, bh, L);
-  const bool any = row.hi > row.lo;
-  WidePass<D, KIND> ps;
-  {
-    const int64_t at = row.valid ? ((int64_t)row.t * m.batch + bh / m.hkv) * m.hq + row.head : 0;
-    const bf16_t* qp = static_cast<const bf16_t*>(a.q) + at * D + 8 * h;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s)
-      ps.q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + 16 * s));
-#pragma unroll
-    for (int ct = 0; ct < D / 32; ++ct) ps.o[ct] = floatx16{};
-    const ScoreMap map(a, row.valid ? row.head : 0);
-    ps.mul = map.mul;
-    ps.cap2 = map.cap2;
-    ps.slope2 = map.slope2;
-    ps.ref = KIND == kCapped ? 0.f : -INFINITY;
-    ps.l = 0.f;
-    ps.pos = row.pos;
-    ps.lo = row.lo;
-    ps.hi = row.hi;
-  }
-  // keys of this wavefront's queries, and those that all of its (non-empty) ones see
-  int lo_min = -cols32_max(any ? -row.lo : -INT32_MAX), hi_max = cols32_max(row.hi);
-  int lo_max = cols32_max(any ? row.lo : 0), hi_min = -cols32_max(any ? -row.hi : -INT32_MAX);
-  if (lane == 0) s_range[w] = make_int4(lo_min, hi_max, lo_max, hi_min);
-  __syncthreads();
-  int4 g = s_range[0];  // of the workgroup's
-#pragma unroll
-  for (int i = 1; i < 8; ++i) {
-    const int4 x = s_range[i];
-    g = make_int4(min(g.x, x.x), max(g.y, x.y), max(g.z, x.z), min(g.w, x.w));
-  }
-  const int g_lo = __builtin_amdgcn_readfirstlane(g.x), g_hi = __builtin_amdgcn_readfirstlane(g.y);
-  const int g_lo_max = __builtin_amdgcn_readfirstlane(g.z);
-  const int g_hi_min = __builtin_amdgcn_readfirstlane(g.w);
-  lo_min = __builtin_amdgcn_readfirstlane(lo_min);
-  hi_max = __builtin_amdgcn_readfirstlane(hi_max);
-  lo_max = __builtin_amdgcn_readfirstlane(lo_max);
-  hi_min = __builtin_amdgcn_readfirstlane(hi_min);
-  const int step0 = g_hi > 0 ? g_lo / 32 : 0, step_end = g_hi > 0 ? (g_hi + 31) / 32 : 0;
-  const int n_kt = (step_end - step0 + 1) / 2;  // tiles of keys
-  const int per = max((n_kt + a.n_split - 1) / a.n_split, kTileMinSplit);
-  const int n_eff = (n_kt + per - 1) / per;
-  if (split > 0 && split >= n_eff) return;
-  const int first = split * per, last = min(first + per, n_kt);
-
-  // wavefront w copies pieces w, w + 8, ... (1 KiB each) of a tile's two steps; a step
-  // past the last is the last again (masked)
-  const int sh = m.B == 32 ? 0 : m.B == 64 ? 1 : 2;  // log2 of the steps per block
-  constexpr int PPS = D / 16;  // pieces per step
-  auto load = [&](const void* src, uint4 (&dst)[2][D * 4], int kt) {
-#pragma unroll
-    for (int i = 0; i < 2 * PPS; i += 8) {
-      const int s2 = (i + w) / PPS, pc = (i + w) % PPS;
-      const int st = min(step0 + 2 * kt + s2, step_end - 1);
-      const int64_t at = (attend_slot(a, bh, st >> sh) * m.B + (st & ((1 << sh) - 1)) * 32) * D;
-      copy_to_lds(reinterpret_cast<const char*>(static_cast<const bf16_t*>(src) + at) + pc * 1024 +
-                      lane * 16,
-                  &dst[s2][pc * 64]);
-    }
-  };
-  const int at_k = (r >> 4) * (D * 2) + 16 * h + (r & 15), at_v = (r >> 4) * 64 + 16 * h + (r & 15);
-  auto none = [&](int t0) { return t0 >= hi_max || t0 + 32 <= lo_min; };  // of this wavefront
-  // tile kt in `cur`: the keys of kt + 1 are in `nxt`, whose values are on their way
-  auto use = [&](WideTile<D>& cur, WideTile<D>& nxt, WideTile<D>& far, int kt, int* odd) {
-    wait_copies();  // this wavefront's copies: values of tile kt, keys of kt + 1
-    const int tile_t0 = (step0 + 2 * kt) * 32;
-    const bool g_inner = tile_t0 >= g_lo_max && tile_t0 + kTileTokens <= g_hi_min;
-    if (!g_inner) {  // every wavefront looks through the values it copied
-      uint32_t bad = 0u;
-#pragma unroll
-      for (int i = 0; i < 2 * PPS; i += 8) {
-        const uint4 v = cur.v[(i + w) / PPS][(i + w) % PPS * 64 + lane];
-        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          bad |= ((x[k] & 0x7F80u) == 0x7F80u || (x[k] & 0x7F800000u) == 0x7F800000u) ? 1u : 0u;
-      }
-      const bool one = __any(bad != 0u);
-      if (lane == 0) odd[w] = one;
-    }
-    __syncthreads();
-    if (kt + 2 < last) load(a.k, far.k, kt + 2);
-    if (kt + 1 < last) load(a.v, nxt.v, kt + 1);
-    const int4* of = reinterpret_cast<const int4*>(odd);
-    if (__builtin_expect(!g_inner && (of[0].x | of[0].y | of[0].z | of[0].w | of[1].x | of[1].y |
-                                      of[1].z | of[1].w), 0)) {
-#pragma unroll 1
-      for (int s2 = 0; s2 < 2; ++s2) ps.odd_values(&cur.v[s2][at_v], tile_t0 + 32 * s2, h);
-      __syncthreads();  // (the same for all wavefronts) then they leave the values
-#pragma unroll
-      for (int i = 0; i < 2 * PPS; i += 8) {
-        uint4& v = cur.v[(i + w) / PPS][(i + w) % PPS * 64 + lane];
-        uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) odd_marks(x[k]);
-        v = make_uint4(x[0], x[1], x[2], x[3]);
-      }
-      __syncthreads();
-    }
-#pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2) {
-      const int t0 = tile_t0 + 32 * s2;
-      const uint4* kp = s2 == 0 ? &cur.k[1][at_k] : &nxt.k[0][at_k];  // of the next step
-      const bool now = !none(t0), next = (s2 == 0 || kt + 1 < last) && !none(t0 + 32);
-      if (!now && !next) continue;
-      // one path for every step, so that the outputs keep their registers: a step of which
-      // this wavefront sees nothing has weights of zero, scores past the last are not used
-      const bool inner = t0 >= lo_max && t0 + 32 <= hi_min;
-      ps.ready(t0, inner, h);
-      bf16x8 p[2];
-      floatx16 y;
-      if constexpr (KIND == kCapped) {
-        if (inner) {
-          __builtin_amdgcn_sched_barrier(0);
-          y = ps.scores(kp);
-          ps.template weights<false>(p);
-          wide_order<D / 16, 6>();
-        } else {
-          ps.template weights<true>(p, t0, h);
-          y = ps.scores(kp);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        ps.product(&cur.v[s2][at_v], p);
-      } else {
-        __builtin_amdgcn_sched_barrier(0);
-        y = ps.scores(kp);
-        ps.template weights<false>(p);
-        ps.product(&cur.v[s2][at_v], p);
-        wide_order<D / 16 + 2 * (D / 32), 5>();
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      ps.x = y;
-    }
-  };
-  if (first < last) {
-    load(a.k, tile0.k, first);
-    load(a.v, tile0.v, first);
-    if (first + 1 < last) load(a.k, tile1.k, first + 1);
-    wait_copies();
-    __syncthreads();
-    if (!none((step0 + 2 * first) * 32)) ps.x = ps.scores(&tile0.k[0][at_k]);
-  }
-#pragma unroll 1
-  for (int kt = first; kt < last; kt += 3) {
-    use(tile0, tile1, tile2, kt, s_odd[0]);
-    if (kt + 1 < last) use(tile1, tile2, tile0, kt + 1, s_odd[1]);
-    if (kt + 2 < last) use(tile2, tile0, tile1, kt + 2, s_odd[2]);
-  }
-
-  const int64_t u = (int64_t)bh * a.n_tiles + tile;
-  if (a.n_split > 1 && split == 0 && tid == 0) a.n_eff[u] = n_eff;
-  tile_write<D>(a, row, bh, h, ps.o, ps.ref, ps.l, n_eff,
-                (u * a.n_split + split) * kWideRows + w * 32 + r);
-}
-
 static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
   using Kernel = void (*)(AttendArgs);
   const auto go = [&](Kernel kern, Kernel join = nullptr) {
@@ -1234,34 +928,22 @@ static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
     for (a.tile0 = 0; a.tile0 < a.n_tiles; a.tile0 += most) {
       const int n = a.n_tiles - a.tile0 < most ? a.n_tiles - a.tile0 : most;
       const unsigned wgs = (unsigned)a.m.bh * (unsigned)n;
-      hipLaunchKernelGGL(kern, dim3(wgs, (unsigned)a.n_split), dim3(a.rows == kWideRows ? 512 : 256), 0,
-                         st, a);
+      hipLaunchKernelGGL(kern, dim3(wgs, (unsigned)a.n_split), dim3(256), 0, st, a);
       if (a.n_split > 1 && join)
         hipLaunchKernelGGL(join, dim3(wgs * (unsigned)(a.rows / 16)), dim3(256), 0, st, a);
     }
   };
+  // a cap this small bounds every score: weights against a reference of 0 stay in range
   const bool cap = a.o.softcap > 0.f, bias = a.o.slopes != nullptr;
+  const bool bounded = cap && !bias && a.o.softcap * kLog2e <= 60.f;
   const auto tile = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    const auto join = attend_join_kernel<D>;
-    if (cap && bias) go(attend_tile_kernel<D, true, true>, join);
-    else if (cap) go(attend_tile_kernel<D, true, false>, join);
-    else if (bias) go(attend_tile_kernel<D, false, true>, join);
-    else go(attend_tile_kernel<D, false, false>, join);
+    if (bounded) go(attend_tile_kernel<D, kCapped>, attend_join_kernel<D>);
+    else if (cap) go(attend_tile_kernel<D, kGeneral>, attend_join_kernel<D>);
+    else if (bias) go(attend_tile_kernel<D, kBiased>, attend_join_kernel<D>);
+    else go(attend_tile_kernel<D, kPlain>, attend_join_kernel<D>);
   };
-  // a cap this small bounds every score: weights against a reference of 0 stay in range
-  const bool bounded = cap && !bias && a.o.softcap * kLog2e <= 60.f;
-  const auto wide = [&](auto d) {
-    constexpr int D = decltype(d)::value;
-    const auto join = attend_join_kernel<D>;
-    if (bounded) go(attend_wide_kernel<D, kCapped>, join);
-    else if (cap || bias) go(attend_wide_kernel<D, kGeneral>, join);
-    else go(attend_wide_kernel<D, kPlain>, join);
-  };
-  if (a.rows == kWideRows) {
-    if (a.m.d == 64) wide(std::integral_constant<int, 64>{});
-    else wide(std::integral_constant<int, 128>{});
-  } else if (a.rows == kTileRows) {
+  if (a.rows == kTileRows) {
     if (a.m.d == 64) tile(std::integral_constant<int, 64>{});
     else tile(std::integral_constant<int, 128>{});
   } else if (a.m.elem == 4) {

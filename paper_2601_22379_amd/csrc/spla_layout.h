@@ -434,7 +434,6 @@ SPLA_HD AppendRopeWs append_rope_ws_layout(const Dims& m, int max_new) {
 // workgroup per tile and split of the keys.
 constexpr int kAttendRows = 16;
 constexpr int kTileRows = 128;
-constexpr int kWideRows = 256;
 constexpr int kAttendFill = 768;      // workgroups to aim for (three per compute unit)
 constexpr int kTileFill = 512;        // ... of tiles of 128 rows (two)
 constexpr int kAttendMaxSplit = 128;  // workgroups that share one tile's keys at most
@@ -461,10 +460,10 @@ struct AttendWs {
 SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
   AttendWs w;
   const bool wide = attend_wide(m, n_tokens);
-  w.rows = wide ? ((int64_t)n_tokens * m.group > 256 ? kWideRows : kTileRows) : kAttendRows;
+  w.rows = wide ? kTileRows : kAttendRows;
   w.n_tiles = (int)ceil_div((int64_t)n_tokens * m.group, w.rows);
   const int64_t wgs = (int64_t)m.bh * w.n_tiles;
-  int64_t n = wgs > 0 ? (wide ? kTileFill * kTileRows / w.rows / wgs : ceil_div(kAttendFill, wgs)) : 1;
+  int64_t n = wgs > 0 ? (wide ? kTileFill / wgs : ceil_div(kAttendFill, wgs)) : 1;
   const int64_t most = ceil_div(m.cap, wide ? kTileMinSplit * 64 : kAttendMinSteps * kSubTokens);
   n = n < most ? n : most;
   n = n < kAttendMaxSplit ? n : kAttendMaxSplit;
