@@ -586,8 +586,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 // ---------------------------------------------------------------- many rows
 // bf16 calls of many query rows are bound by the matrix cores: a workgroup takes
 // 128 rows, 32 per wavefront, and its keys and values pass through LDS once for
-// all four wavefronts, 64 tokens (two steps) at a time in two buffers, copied
-// there by the loads themselves (no registers) while the tile before is used.
+// all four wavefronts, a step of 32 tokens at a time in two buffers, copied there
+// by the loads themselves (no registers) while the step before is used. Three
+// workgroups share a compute unit (164 registers, 33 KB of LDS), so that the
+// exponentials of some run beside the products of others: two, with 64 tokens at a
+// time, took 3 to 6 % longer.
 //
 // v_mfma_f32_32x32x16_bf16, scores transposed (rows = tokens, columns = queries).
 // The cache's step is an operand image for this shape too: row r = 16 mt + i of
@@ -599,12 +602,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 // cache's bytes as they are, every operand read is runs of 512 bytes, and the
 // weights never leave their lane.
 typedef float floatx16 __attribute__((ext_vector_type(16)));
-constexpr int kTileTokens = 64;
 
 template <int D>
 struct alignas(16) TileBuf {
-  uint4 k[2][D * 4];  // two steps of 32 D elements
-  uint4 v[2][D * 4];
+  uint4 k[D * 4];  // a step: 32 D elements
+  uint4 v[D * 4];
 };
 
 // 16 bytes per lane from src (per lane) to dst (uniform) + 16 lane, without a
@@ -638,9 +640,9 @@ struct TilePass {
     return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z) + 1.f), cap2);
   }
 
-  // x[16 s2 + 4 (2 mt + e) + b]: score of token 32 s2 + 16 e + 8 h + 4 mt + b
-  static __device__ __forceinline__ int token(int i, int h) {
-    return 32 * (i >> 4) + 16 * ((i >> 2) & 1) + 8 * h + 4 * ((i >> 3) & 1) + (i & 3);
+  // x[4 (2 mt + e) + b]: score of token 16 e + 8 h + 4 mt + b; here for h = 0
+  static __device__ __forceinline__ int token(int i) {
+    return 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3);
   }
 
   __device__ __forceinline__ void step(const TileBuf<D>& buf, int t0, bool inner, int lane) {
@@ -648,41 +650,35 @@ struct TilePass {
     // pieces of this lane's score row and of its value coordinate: coordinates 16 s
     // + 8 h .. + 7 at + 32 s, coordinate 32 c + r, tokens 16 e + 8 h .. at + 128 c + 32 e
     const int at_k = (r >> 4) * (D * 2) + 16 * h + (r & 15), at_v = (r >> 4) * 64 + 16 * h + (r & 15);
-    floatx16 x[2];
+    floatx16 x = floatx16{};
 #pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2) {
-      x[s2] = floatx16{};
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const uint4 a = buf.k[s2][at_k + 32 * s];
-        x[s2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), q[s], x[s2],
-                                                        0, 0, 0);
-      }
-    }
+    for (int s = 0; s < KS; ++s)
+      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, buf.k[at_k + 32 * s]),
+                                                  q[s], x, 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (KIND == kBiased || KIND == kGeneral) {
       const float base = (float)(pos - t0 - 8 * h);
 #pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        float y = x[i >> 4][i & 15] * mul;
+      for (int i = 0; i < 16; ++i) {
+        float y = x[i] * mul;
         if constexpr (KIND == kGeneral) y = capped(y);
-        x[i >> 4][i & 15] = fmaf(-slope2, fabsf(base - (float)token(i, 0)), y);
+        x[i] = fmaf(-slope2, fabsf(base - (float)token(i)), y);
       }
     }
     if constexpr (KIND == kCapped) {
 #pragma unroll
-      for (int i = 0; i < 32; ++i) x[i >> 4][i & 15] = capped(x[i >> 4][i & 15] * mul);
+      for (int i = 0; i < 16; ++i) x[i] = capped(x[i] * mul);
     }
     if (!inner) {
       const uint32_t a = (uint32_t)(t0 + 8 * h - lo), n = (uint32_t)(hi - lo);
 #pragma unroll
-      for (int i = 0; i < 32; ++i)  // lo <= token < hi
-        x[i >> 4][i & 15] = a + (uint32_t)token(i, 0) < n ? x[i >> 4][i & 15] : -INFINITY;
+      for (int i = 0; i < 16; ++i)  // lo <= token < hi
+        x[i] = a + (uint32_t)token(i) < n ? x[i] : -INFINITY;
     }
     if constexpr (KIND != kCapped) {
-      float nm = x[0][0];
+      float nm = x[0];
 #pragma unroll
-      for (int i = 1; i < 32; ++i) nm = fmaxf(nm, x[i >> 4][i & 15]);
+      for (int i = 1; i < 16; ++i) nm = fmaxf(nm, x[i]);
       nm = fmaxf(nm, xor32(nm));
       if constexpr (KIND == kPlain) nm *= mul;
       // the reference moves only when a score passes it by 2^8: weights up to there are as
@@ -701,24 +697,24 @@ struct TilePass {
       }
     }
     const float rf = ref == -INFINITY ? 0.f : ref;
-    bf16x8 p[4];
+    bf16x8 p[2];
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float y = x[i >> 4][i & 15];
+    for (int i = 0; i < 16; ++i) {
+      const float y = x[i];
       const float w = __builtin_amdgcn_exp2f(KIND == kPlain ? fmaf(y, mul, -rf)
                                              : KIND == kCapped ? y : y - rf);
       sum += w;
       // weights rounded to bf16 for the product (the sum keeps fp32)
-      p[2 * (i >> 4) + ((i >> 2) & 1)][4 * ((i >> 3) & 1) + (i & 3)] = (__bf16)w;
+      p[(i >> 2) & 1][4 * (i >> 3) + (i & 3)] = (__bf16)w;
     }
     l += sum;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)  // tokens 16 e .. + 15 of the tile
+    for (int e = 0; e < 2; ++e)  // tokens 16 e .. + 15 of the step
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
-        const uint4 a = buf.v[e >> 1][at_v + 128 * c + 32 * (e & 1)];
+        const uint4 a = buf.v[at_v + 128 * c + 32 * e];
         o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), p[e], o[c], 0,
                                                        0, 0);
       }
@@ -733,8 +729,8 @@ struct TilePass {
     for (int c = 0; c < CT; ++c) {
       floatx16 n = floatx16{};
 #pragma unroll 1
-      for (int e = 0; e < 4; ++e) {
-        const uint4 v = buf.v[e >> 1][at_v + 128 * c + 32 * (e & 1)];
+      for (int e = 0; e < 2; ++e) {
+        const uint4 v = buf.v[at_v + 128 * c + 32 * e];
         uint32_t w[4] = {v.x, v.y, v.z, v.w}, u[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = odd_marks(w[i]);
@@ -788,7 +784,7 @@ __device__ __forceinline__ void tile_write(const AttendArgs& a, const AttendRow&
 }
 
 template <int D, int KIND>
-__global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, 3) void attend_tile_kernel(AttendArgs a) {
   __shared__ TileBuf<D> buf0, buf1;
   __shared__ int4 s_range[4];
   __shared__ int s_odd[2][4];
@@ -820,11 +816,11 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
   const int g_hi_min = __builtin_amdgcn_readfirstlane(g.w);
   const int step0 = g_hi > 0 ? g_lo / 32 : 0;
   const int step_end = g_hi > 0 ? (g_hi + 31) / 32 : 0;
-  const int n_kt = (step_end - step0 + 1) / 2;  // tiles of keys
-  const int per = max((n_kt + a.n_split - 1) / a.n_split, kTileMinSplit);
-  const int n_eff = (n_kt + per - 1) / per;
+  const int n_steps = step_end - step0;
+  const int per = max((n_steps + a.n_split - 1) / a.n_split, kTileMinSplit);
+  const int n_eff = (n_steps + per - 1) / per;
   if (split > 0 && split >= n_eff) return;
-  const int first = split * per, last = min(first + per, n_kt);
+  const int first = step0 + split * per, last = min(first + per, step_end);
 
   TilePass<D, KIND> ps;
   const int64_t qrow = row.valid ? ((int64_t)row.t * m.batch + bh / m.hkv) * m.hq + row.head : 0;
@@ -847,71 +843,61 @@ __global__ __launch_bounds__(256, 2) void attend_tile_kernel(AttendArgs a) {
   ps.lo = row.lo;
   ps.hi = row.hi;
 
-  // wavefront w copies pieces w, w + 4, ... (1 KiB each) of the tile's two key
-  // steps and two value steps; a step past the last is the last again (masked)
+  // wavefront w copies pieces w, w + 4, ... (1 KiB each) of a step's keys and values
   const int sh = m.B == 32 ? 0 : m.B == 64 ? 1 : 2;  // log2 of the steps per block
-  auto load = [&](TileBuf<D>& buf, int kt) {
+  auto load = [&](TileBuf<D>& buf, int st) {
+    const int64_t o = (attend_slot(a, bh, st >> sh) * m.B + (st & ((1 << sh) - 1)) * 32) * D;
+    const char* kp = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.k) + o) + lane * 16;
+    const char* vp = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.v) + o) + lane * 16;
 #pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2) {
-      const int st = min(step0 + 2 * kt + s2, step_end - 1);
-      const int64_t o = (attend_slot(a, bh, st >> sh) * m.B + (st & ((1 << sh) - 1)) * 32) * D;
-      const char* kp = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.k) + o) + lane * 16;
-      const char* vp = reinterpret_cast<const char*>(static_cast<const bf16_t*>(a.v) + o) + lane * 16;
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) {
-        const int pc = w + 4 * i;
-        copy_to_lds(kp + pc * 1024, &buf.k[s2][pc * 64]);
-        copy_to_lds(vp + pc * 1024, &buf.v[s2][pc * 64]);
-      }
+    for (int i = 0; i < D / 64; ++i) {
+      const int pc = w + 4 * i;
+      copy_to_lds(kp + pc * 1024, &buf.k[pc * 64]);
+      copy_to_lds(vp + pc * 1024, &buf.v[pc * 64]);
     }
   };
-  auto use = [&](TileBuf<D>& buf, TileBuf<D>& other, int kt, int par) {
-    const int t0 = (step0 + 2 * kt) * 32;
-    wait_copies();  // this wavefront's copies of tile kt are in LDS
+  auto use = [&](TileBuf<D>& buf, TileBuf<D>& other, int st, int* s_odd) {
+    const int t0 = st * 32;
+    wait_copies();  // this wavefront's copies of the step are in LDS
     // values that some query may not see (the same for all wavefronts): every
     // wavefront looks through the pieces it copied
-    const bool g_inner = t0 >= g_lo_max && t0 + kTileTokens <= g_hi_min;
+    const bool g_inner = t0 >= g_lo_max && t0 + 32 <= g_hi_min;
     if (!g_inner) {
       uint32_t bad = 0u;
 #pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2)
+      for (int i = 0; i < D / 64; ++i) {
+        const uint4 v = buf.v[(w + 4 * i) * 64 + lane];
+        const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-          const uint4 v = buf.v[s2][(w + 4 * i) * 64 + lane];
-          const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            bad |= ((x[k] & 0x7F80u) == 0x7F80u || (x[k] & 0x7F800000u) == 0x7F800000u) ? 1u : 0u;
-        }
+        for (int k = 0; k < 4; ++k)
+          bad |= ((x[k] & 0x7F80u) == 0x7F80u || (x[k] & 0x7F800000u) == 0x7F800000u) ? 1u : 0u;
+      }
       const bool one = __any(bad != 0u);
-      if (lane == 0) s_odd[par][w] = one;
+      if (lane == 0) s_odd[w] = one;
     }
     __syncthreads();
-    if (kt + 1 < last) load(other, kt + 1);
-    if (__builtin_expect(!g_inner && (s_odd[par][0] | s_odd[par][1] | s_odd[par][2] | s_odd[par][3]),
-                         0)) {  // the same for all wavefronts
-      ps.odd_values(buf, t0, lane);
-      __syncthreads();  // then they leave the values
+    if (st + 1 < last) load(other, st + 1);
+    if (__builtin_expect(!g_inner && (s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3]), 0)) {
+      ps.odd_values(buf, t0, lane);  // (the same for all wavefronts)
+      __syncthreads();               // then the values lose them
 #pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2)
+      for (int i = 0; i < D / 64; ++i) {
+        uint4& v = buf.v[(w + 4 * i) * 64 + lane];
+        uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-          uint4& v = buf.v[s2][(w + 4 * i) * 64 + lane];
-          uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) odd_marks(x[k]);
-          v = make_uint4(x[0], x[1], x[2], x[3]);
-        }
+        for (int k = 0; k < 4; ++k) odd_marks(x[k]);
+        v = make_uint4(x[0], x[1], x[2], x[3]);
+      }
       __syncthreads();
     }
-    if (t0 >= hi_max || t0 + kTileTokens <= lo_min) return;  // nothing here for this wavefront
-    ps.step(buf, t0, t0 >= lo_max && t0 + kTileTokens <= hi_min, lane);
+    if (t0 >= hi_max || t0 + 32 <= lo_min) return;  // nothing here for this wavefront
+    ps.step(buf, t0, t0 >= lo_max && t0 + 32 <= hi_min, lane);
   };
   if (first < last) load(buf0, first);
 #pragma unroll 1
-  for (int kt = first; kt < last; kt += 2) {
-    use(buf0, buf1, kt, 0);
-    if (kt + 1 < last) use(buf1, buf0, kt + 1, 1);
+  for (int st = first; st < last; st += 2) {
+    use(buf0, buf1, st, s_odd[0]);
+    if (st + 1 < last) use(buf1, buf0, st + 1, s_odd[1]);
   }
 
   const int64_t u = (int64_t)bh * a.n_tiles + tile;

@@ -435,10 +435,10 @@ SPLA_HD AppendRopeWs append_rope_ws_layout(const Dims& m, int max_new) {
 constexpr int kAttendRows = 16;
 constexpr int kTileRows = 128;
 constexpr int kAttendFill = 768;      // workgroups to aim for (three per compute unit)
-constexpr int kTileFill = 512;        // ... of tiles of 128 rows (two)
+constexpr int kTileFill = 768;        // ... of tiles of 128 rows (three)
 constexpr int kAttendMaxSplit = 128;  // workgroups that share one tile's keys at most
 constexpr int kAttendMinSteps = 4;    // 32-token steps per workgroup at least: one per wavefront
-constexpr int kTileMinSplit = 4;      // 64-token key tiles per workgroup at least
+constexpr int kTileMinSplit = 8;      // ... and of a tile of 128 rows
 
 SPLA_HD bool attend_wide(const Dims& m, int n_tokens) {
   return m.elem == 2 && (int64_t)n_tokens * m.group > 64;
@@ -464,7 +464,7 @@ SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
   w.n_tiles = (int)ceil_div((int64_t)n_tokens * m.group, w.rows);
   const int64_t wgs = (int64_t)m.bh * w.n_tiles;
   int64_t n = wgs > 0 ? (wide ? kTileFill / wgs : ceil_div(kAttendFill, wgs)) : 1;
-  const int64_t most = ceil_div(m.cap, wide ? kTileMinSplit * 64 : kAttendMinSteps * kSubTokens);
+  const int64_t most = ceil_div(m.cap, (wide ? kTileMinSplit : kAttendMinSteps) * kSubTokens);
   n = n < most ? n : most;
   n = n < kAttendMaxSplit ? n : kAttendMaxSplit;
   w.n_split = (int)(n > 1 ? n : 1);
