@@ -37,37 +37,58 @@ __device__ __forceinline__ uint64_t pack_f32x2(float a, float b) {
 
 constexpr float kLn2 = 0.6931471805599453f;
 
-// One query row: row r = t G + g of (sequence, KV head) bh.
-__device__ __forceinline__ int attend_length(const AttendArgs& a, int bh) {
-  return min(max(a.seq_lens[bh / a.m.hkv], 0), a.m.cap);
+// A wave-uniform word through the scalar cache. Nothing in these kernels writes the
+// arrays read so (lengths, counts, the block table).
+__device__ __forceinline__ int uniform_word(const int32_t* p, int64_t i) {
+  return reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
+      reinterpret_cast<uintptr_t>(p))[i];
 }
+
+// What the rows of a sequence have in common: all its words are asked for at once.
+struct AttendSeq {
+  int len, n, prefix;  // tokens held, queries, tokens that every query sees
+};
+__device__ __forceinline__ AttendSeq attend_seq(const AttendArgs& a, int bh) {
+  const int b = bh / a.m.hkv;
+  const int len = uniform_word(a.seq_lens, b);
+  // (no array: any word that is there, not used)
+  const int n = uniform_word(a.o.n_new ? a.o.n_new : a.seq_lens, b);
+  const int pre = uniform_word(a.o.prefix_len ? a.o.prefix_len : a.seq_lens, b);
+  AttendSeq s;
+  s.len = min(max(len, 0), a.m.cap);
+  s.n = a.o.n_new ? min(max(n, 0), a.n_tokens) : a.n_tokens;
+  s.prefix = a.o.prefix_len ? pre : 0;
+  return s;
+}
+
+// One query row: row r = t G + g of (sequence, KV head) bh.
 struct AttendRow {
   int t, head, pos, lo, hi;  // visible keys lo .. hi - 1 (none: lo = hi = 0)
   bool valid;                // a query of the call
 };
-__device__ __forceinline__ AttendRow attend_row(const AttendArgs& a, int64_t r, int bh, int L) {
-  const int b = bh / a.m.hkv, G = a.m.group;
+__device__ __forceinline__ AttendRow attend_row(const AttendArgs& a, const AttendSeq& s, int r,
+                                                int bh) {
+  const int G = a.m.group;
   AttendRow w;
-  const int t = (int)r / G;  // (tokens of a call times group: below 2^27)
-  w.t = t;
-  w.head = (bh % a.m.hkv) * G + (int)r - t * G;
-  int n = a.o.n_new ? a.o.n_new[b] : a.n_tokens;
-  n = n < 0 ? 0 : n > a.n_tokens ? a.n_tokens : n;
-  w.valid = t < n;
-  w.pos = L - n + w.t;
-  w.lo = w.hi = 0;
-  if (w.valid) {
-    int hi = w.pos + 1;
-    if (a.o.prefix_len) hi = max(hi, a.o.prefix_len[b]);
-    hi = min(hi, L);
-    int lo = 0;
-    if (a.o.first_key) lo = max(0, a.o.first_key[(int64_t)t * a.m.batch + b]);
-    if (lo < hi) {
-      w.lo = lo;
-      w.hi = hi;
-    }
-  }
+  w.t = r / G;
+  w.head = (bh % a.m.hkv) * G + r - w.t * G;
+  w.valid = w.t < s.n;
+  w.pos = s.len - s.n + w.t;
+  int lo = 0;
+  if (a.o.first_key)  // (asked for before the lengths are known: any row of the call's)
+    lo = max(0, a.o.first_key[(int64_t)min(w.t, a.n_tokens - 1) * a.m.batch + bh / a.m.hkv]);
+  const int hi = min(max(w.pos + 1, s.prefix), s.len);
+  const bool any = w.valid && lo < hi;
+  w.lo = any ? lo : 0;
+  w.hi = any ? hi : 0;
   return w;
+}
+// Where row r's query starts in q (a row past the call's: its last one; the columns of a
+// product are independent of each other).
+__device__ __forceinline__ int64_t attend_q_at(const AttendArgs& a, int64_t r, int bh) {
+  const int G = a.m.group, rc = (int)min(r, (int64_t)a.n_tokens * G - 1), t = rc / G;
+  return (((int64_t)t * a.m.batch + bh / a.m.hkv) * a.m.hq + (bh % a.m.hkv) * G + rc - t * G) *
+         a.m.d;
 }
 
 // Score of a raw product, in base 2: x log2 e with x = cap(s dot) - slope |p - j|.
@@ -91,8 +112,8 @@ struct ScoreMap {
 // Slot of the block of token t0: its place in the cache buffers.
 __device__ __forceinline__ int64_t attend_slot(const AttendArgs& a, int bh, int blk) {
   if (!a.table) return (int64_t)bh * a.m.nb_cap + blk;
-  const int p = block_page(a.m, a.table, bh, blk);
-  return (int64_t)(p < 0 ? 0 : p) * a.m.hkv + bh % a.m.hkv;
+  const int p = uniform_word(a.table, (int64_t)(bh / a.m.hkv) * a.m.nb_cap + blk);
+  return (int64_t)(p < 0 || p >= a.m.pages ? 0 : p) * a.m.hkv + bh % a.m.hkv;
 }
 
 // Infinities and NaN among values that some query does not see: a zero weight
@@ -328,17 +349,10 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
   const int bh = (int)(blockIdx.x % (unsigned)m.bh);
   const int tile = a.tile0 + (int)(blockIdx.x / (unsigned)m.bh), split = (int)blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, j = lane & 15, g = lane >> 4;
-  // the queries first: their loads wait for nothing. A column past the call's rows
-  // reads its last one: the columns of a product are independent of each other
-  StepOps<T, D> ops;
-  {
-    const int64_t r = min((int64_t)tile * kAttendRows + j, (int64_t)a.n_tokens * m.group - 1);
-    const int64_t t = r / m.group;
-    ops.load_q(static_cast<const T*>(a.q) + ((t * m.batch + bh / m.hkv) * m.hq +
-               (bh % m.hkv) * m.group + (r - t * m.group)) * D, g);
-  }
-  const int L = attend_length(a, bh);
-  const AttendRow row = attend_row(a, (int64_t)tile * kAttendRows + j, bh, L);
+  StepOps<T, D> ops;  // the queries first: their loads wait for nothing
+  ops.load_q(static_cast<const T*>(a.q) + attend_q_at(a, (int64_t)tile * kAttendRows + j, bh), g);
+  const AttendSeq seq = attend_seq(a, bh);
+  const AttendRow row = attend_row(a, seq, tile * kAttendRows + j, bh);
   const bool any = row.hi > row.lo;
   // the tile's keys, and those that all of its (non-empty) queries see
   const int lo_min = -cols_max<16>(any ? -row.lo : -INT32_MAX), hi_max = cols_max<16>(row.hi);
@@ -358,6 +372,7 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
   const int sh = m.B == 32 ? 0 : m.B == 64 ? 1 : 2;  // log2 of the steps per block
   // the next step's page is looked up while this one's rows are used
   int64_t slot = first + w < last ? attend_slot(a, bh, (first + w) >> sh) : 0;
+#pragma unroll 1
   for (int st = first + w; st < last; st += 4) {
     const int t0 = st * 32;
     ops.load_kv(m, a.k, a.v, slot, (st & ((1 << sh) - 1)) * 32, lane);
@@ -446,7 +461,7 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
 #pragma unroll
     for (int e = 0; e < E; ++e) y[e] = fmaf(s_o[x][r][c0 + e], f, y[e]);
   }
-  const AttendRow out_row = attend_row(a, (int64_t)tile * kAttendRows + r, bh, L);
+  const AttendRow out_row = attend_row(a, seq, tile * kAttendRows + r, bh);
   if (n_eff <= 1) {
     attend_write<T, D>(a, out_row, bh, c0, y, mt, lt);
     return;
@@ -526,7 +541,7 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
       for (int e = 0; e < E; ++e) y[e] = fmaf(s_o[0][x * R + jr][c0 + e], f, y[e]);
     }
   }
-  attend_write<T, D>(a, attend_row(a, (int64_t)tile * kAttendRows + jr, bh, L), bh, c0, y, jm, jl);
+  attend_write<T, D>(a, attend_row(a, seq, tile * kAttendRows + jr, bh), bh, c0, y, jm, jl);
 }
 
 // Joins the records of 16 rows of a tile's splits (tiles of 128 rows); thread (row,
@@ -541,7 +556,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   const int64_t u = (int64_t)bh * a.n_tiles + tile;
   const int n = a.n_eff[u];
   if (n <= 1) return;  // written by the pass
-  const AttendRow row = attend_row(a, (int64_t)tile * a.rows + r, bh, attend_length(a, bh));
+  const AttendRow row = attend_row(a, attend_seq(a, bh), tile * a.rows + r, bh);
   const int64_t rec0 = u * a.n_split * a.rows + r;
   float mt = -INFINITY, lt = 0.f, y[E];
 #pragma unroll
@@ -795,9 +810,17 @@ __global__ __launch_bounds__(256, 3) void attend_tile_kernel(AttendArgs a) {
   const int split = (int)blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int L = attend_length(a, bh);
   const int rr = w * 32 + (lane & 31), h = lane >> 5;  // this lane's row of the tile
-  const AttendRow row = attend_row(a, (int64_t)tile * kTileRows + rr, bh, L);
+  TilePass<D, KIND> ps;
+  {  // the queries first: their loads wait for nothing
+    const bf16_t* qp = static_cast<const bf16_t*>(a.q) +
+                       attend_q_at(a, (int64_t)tile * kTileRows + rr, bh) + 8 * h;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      ps.q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + 16 * s));
+  }
+  const AttendSeq seq = attend_seq(a, bh);
+  const AttendRow row = attend_row(a, seq, tile * kTileRows + rr, bh);
   const bool any = row.hi > row.lo;
   // keys of this wavefront's queries, and those that all of its (non-empty) ones see
   const int lo_min = -cols_max<32>(any ? -row.lo : -INT32_MAX), hi_max = cols_max<32>(row.hi);
@@ -822,15 +845,6 @@ __global__ __launch_bounds__(256, 3) void attend_tile_kernel(AttendArgs a) {
   if (split > 0 && split >= n_eff) return;
   const int first = step0 + split * per, last = min(first + per, step_end);
 
-  TilePass<D, KIND> ps;
-  const int64_t qrow = row.valid ? ((int64_t)row.t * m.batch + bh / m.hkv) * m.hq + row.head : 0;
-  const bf16_t* qp = static_cast<const bf16_t*>(a.q) + qrow * D + 8 * h;
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    uint4 x = *reinterpret_cast<const uint4*>(qp + 16 * s);
-    if (!row.valid) x = make_uint4(0u, 0u, 0u, 0u);
-    ps.q[s] = __builtin_bit_cast(bf16x8, x);
-  }
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) ps.o[c] = floatx16{};
   const ScoreMap map(a, row.valid ? row.head : 0);
