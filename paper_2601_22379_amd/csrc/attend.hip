@@ -37,6 +37,12 @@ __device__ __forceinline__ uint64_t pack_f32x2(float a, float b) {
 
 constexpr float kLn2 = 0.6931471805599453f;
 
+// What a sum against reference from is multiplied by against reference to (base 2,
+// from <= to): never zero, so that an infinity a query has taken in stays one.
+__device__ __forceinline__ float rescale(float from, float to) {
+  return __builtin_amdgcn_exp2f(fmaxf(from - to, -126.f));
+}
+
 // A wave-uniform word through the scalar cache. Nothing in these kernels writes the
 // arrays read so (lengths, counts, the block table).
 __device__ __forceinline__ int uniform_word(const int32_t* p, int64_t i) {
@@ -395,7 +401,7 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
     nm = fmaxf(nm, xor16(nm));
     nm = fmaxf(fmaxf(nm, xor32(nm)), mx);
     const float ref = nm == -INFINITY ? 0.f : nm;  // nothing seen yet: no weight
-    const float alpha = __builtin_amdgcn_exp2f(mx - ref);
+    const float alpha = rescale(mx, ref);
     mx = nm;
     float p[8], sum = 0.f;
 #pragma unroll
@@ -456,7 +462,7 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
   for (int e = 0; e < E; ++e) y[e] = 0.f;
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
-    const float f = __builtin_amdgcn_exp2f(s_m[x][r] - ref);
+    const float f = rescale(s_m[x][r], ref);
     lt = fmaf(s_l[x][r], f, lt);
 #pragma unroll
     for (int e = 0; e < E; ++e) y[e] = fmaf(s_o[x][r][c0 + e], f, y[e]);
@@ -501,7 +507,7 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
     float nm = jm;
 #pragma unroll
     for (int x = 0; x < 8; ++x) nm = fmaxf(nm, hd[x].x);
-    const float rf = nm == -INFINITY ? 0.f : nm, alpha = __builtin_amdgcn_exp2f(jm - rf);
+    const float rf = nm == -INFINITY ? 0.f : nm, alpha = rescale(jm, rf);
     jm = nm;
     jl *= alpha;
 #pragma unroll
@@ -509,7 +515,7 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
       if (x0 + x * P >= n_eff) break;
-      const float f = __builtin_amdgcn_exp2f(hd[x].x - rf);
+      const float f = rescale(hd[x].x, rf);
       jl = fmaf(hd[x].y, f, jl);
 #pragma unroll
       for (int e = 0; e < E / 4; ++e) {
@@ -535,7 +541,7 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
 #pragma unroll
     for (int e = 0; e < E; ++e) y[e] = 0.f;
     for (int x = 0; x < P; ++x) {
-      const float f = __builtin_amdgcn_exp2f(s_m[0][x * R + jr] - rf);
+      const float f = rescale(s_m[0][x * R + jr], rf);
       jl = fmaf(s_l[0][x * R + jr], f, jl);
 #pragma unroll
       for (int e = 0; e < E; ++e) y[e] = fmaf(s_o[0][x * R + jr][c0 + e], f, y[e]);
@@ -576,7 +582,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
     float nm = mt;
 #pragma unroll
     for (int x = 0; x < 8; ++x) nm = fmaxf(nm, h[x].x);
-    const float ref = nm == -INFINITY ? 0.f : nm, alpha = __builtin_amdgcn_exp2f(mt - ref);
+    const float ref = nm == -INFINITY ? 0.f : nm, alpha = rescale(mt, ref);
     mt = nm;
     lt *= alpha;
 #pragma unroll
@@ -584,7 +590,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
       if (x0 + x >= n) break;
-      const float f = __builtin_amdgcn_exp2f(h[x].x - ref);
+      const float f = rescale(h[x].x, ref);
       lt = fmaf(h[x].y, f, lt);
 #pragma unroll
       for (int e = 0; e < E / 4; ++e) {
@@ -701,8 +707,7 @@ struct TilePass {
       // by its own scores, so that no query's rounding hangs on another's)
       const bool move = nm > ref + 8.f;
       if (__any(move)) {
-        // (never zero: an infinity that odd_values left would become NaN)
-        const float alpha = move ? __builtin_amdgcn_exp2f(fmaxf(ref - nm, -126.f)) : 1.f;
+        const float alpha = move ? rescale(ref, nm) : 1.f;
         ref = move ? nm : ref;
         l *= alpha;
 #pragma unroll
