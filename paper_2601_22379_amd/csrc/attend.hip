@@ -27,6 +27,7 @@ struct AttendArgs {
   float scale;  // softmax scale
   int n_tokens, n_tiles, n_split, rows;  // rows per tile
   int tile0;  // first row tile of this launch
+  int join;   // parts of attend_join_kernel (0: no such launch)
   float *part, *ml;
   int32_t *n_eff, *count;
 };
@@ -343,6 +344,79 @@ __device__ __forceinline__ void attend_write(const AttendArgs& a, const AttendRo
   if (a.lse && c0 == 0) a.lse[row] = any ? (mx + log2f(l)) * kLn2 : -INFINITY;
 }
 
+// Joins records p, p + P, ... of n (of row r of a tile: rec0 + x step, coordinates c0 ..) into
+// y against reference mx with sum l; eight records are in flight at a time.
+template <int D, bool COHERENT>
+__device__ __forceinline__ void join_records(const AttendArgs& a, int64_t rec0, int64_t step, int n,
+                                             int p, int P, int c0, float (&y)[D / 16], float& mx,
+                                             float& l) {
+  constexpr int E = D / 16;
+  mx = -INFINITY;
+  l = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] = 0.f;
+  for (int x0 = p; x0 < n; x0 += 8 * P) {
+    float2 hd[8];
+    float4 v[8][E / 4];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const int64_t rec = rec0 + (int64_t)min(x0 + x * P, n - 1) * step;
+      hd[x] = Mem<COHERENT>::ld2(a.ml + rec * 2);
+#pragma unroll
+      for (int e = 0; e < E / 4; ++e) v[x][e] = Mem<COHERENT>::ld4(a.part + rec * D + c0 + 4 * e);
+    }
+    float nm = mx;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) nm = fmaxf(nm, hd[x].x);
+    const float ref = nm == -INFINITY ? 0.f : nm, alpha = rescale(mx, ref);
+    mx = nm;
+    l *= alpha;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] *= alpha;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      if (x0 + x * P >= n) break;
+      const float f = rescale(hd[x].x, ref);
+      l = fmaf(hd[x].y, f, l);
+#pragma unroll
+      for (int e = 0; e < E / 4; ++e) {
+        y[4 * e] = fmaf(v[x][e].x, f, y[4 * e]);
+        y[4 * e + 1] = fmaf(v[x][e].y, f, y[4 * e + 1]);
+        y[4 * e + 2] = fmaf(v[x][e].z, f, y[4 * e + 2]);
+        y[4 * e + 3] = fmaf(v[x][e].w, f, y[4 * e + 3]);
+      }
+    }
+  }
+}
+
+// Joins the P parts of R rows each (P R = 16; thread: part p, row r, coordinates c0 ..)
+// into those of part 0.
+template <int D>
+__device__ __forceinline__ void join_parts(float (&s_m)[16], float (&s_l)[16],
+                                           float (&s_o)[16][D + 4], int p, int P, int r, int R,
+                                           int c0, float (&y)[D / 16], float& mx, float& l) {
+  constexpr int E = D / 16;
+  if (c0 == 0) {
+    s_m[p * R + r] = mx;
+    s_l[p * R + r] = l;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) s_o[p * R + r][c0 + e] = y[e];
+  __syncthreads();
+  if (p > 0) return;
+  for (int x = 1; x < P; ++x) mx = fmaxf(mx, s_m[x * R + r]);
+  const float ref = mx == -INFINITY ? 0.f : mx;
+  l = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) y[e] = 0.f;
+  for (int x = 0; x < P; ++x) {
+    const float f = rescale(s_m[x * R + r], ref);
+    l = fmaf(s_l[x * R + r], f, l);
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = fmaf(s_o[x * R + r][c0 + e], f, y[e]);
+  }
+}
+
 // A tile of 16 query rows; the four wavefronts take every fourth 32-token step of
 // this split's keys and are joined at the end.
 template <typename T, int D>
@@ -468,15 +542,25 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
     for (int e = 0; e < E; ++e) y[e] = fmaf(s_o[x][r][c0 + e], f, y[e]);
   }
   const AttendRow out_row = attend_row(a, seq, tile * kAttendRows + r, bh);
+  if (a.join && split == 0 && tid == 0) a.n_eff[(int64_t)bh * a.n_tiles + tile] = n_eff;
   if (n_eff <= 1) {
     attend_write<T, D>(a, out_row, bh, c0, y, mt, lt);
     return;
   }
+  const int64_t u = (int64_t)bh * a.n_tiles + tile, rec0 = u * a.n_split * kAttendRows;
+  const int64_t rec = rec0 + (int64_t)split * kAttendRows + r;
+  if (a.join) {  // attend_join_kernel joins the records
+    if (!out_row.valid) return;
+#pragma unroll
+    for (int e = 0; e < E; e += 4)
+      *reinterpret_cast<float4*>(a.part + rec * D + c0 + e) =
+          make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+    if (c0 == 0) *reinterpret_cast<float2*>(a.ml + rec * 2) = make_float2(mt, lt);
+    return;
+  }
   // the tile's last workgroup to arrive joins the records of all (device-coherent:
   // other workgroups of this launch wrote them), in the order of the splits
-  const int64_t u = (int64_t)bh * a.n_tiles + tile, rec0 = u * a.n_split * kAttendRows;
   if (out_row.valid) {
-    const int64_t rec = rec0 + (int64_t)split * kAttendRows + r;
 #pragma unroll
     for (int e = 0; e < E; e += 2)
       Mem<true>::st(reinterpret_cast<uint64_t*>(a.part + rec * D + c0 + e), pack_f32x2(y[e], y[e + 1]));
@@ -491,117 +575,40 @@ __global__ __launch_bounds__(256) void attend_stream_kernel(AttendArgs a) {
   int R = 1;
   while (R < nv) R *= 2;
   const int P = 16 / R, p = tid / (16 * R), jr = (tid >> 4) % R;
-  float jm = -INFINITY, jl = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) y[e] = 0.f;
-  for (int x0 = p; x0 < n_eff; x0 += 8 * P) {  // eight records in flight
-    float2 hd[8];
-    float4 v[8][E / 4];
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      const int64_t rec = rec0 + (int64_t)min(x0 + x * P, n_eff - 1) * kAttendRows + jr;
-      hd[x] = Mem<true>::ld2(a.ml + rec * 2);
-#pragma unroll
-      for (int e = 0; e < E / 4; ++e) v[x][e] = Mem<true>::ld4(a.part + rec * D + c0 + 4 * e);
-    }
-    float nm = jm;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) nm = fmaxf(nm, hd[x].x);
-    const float rf = nm == -INFINITY ? 0.f : nm, alpha = rescale(jm, rf);
-    jm = nm;
-    jl *= alpha;
-#pragma unroll
-    for (int e = 0; e < E; ++e) y[e] *= alpha;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      if (x0 + x * P >= n_eff) break;
-      const float f = rescale(hd[x].x, rf);
-      jl = fmaf(hd[x].y, f, jl);
-#pragma unroll
-      for (int e = 0; e < E / 4; ++e) {
-        y[4 * e] = fmaf(v[x][e].x, f, y[4 * e]);
-        y[4 * e + 1] = fmaf(v[x][e].y, f, y[4 * e + 1]);
-        y[4 * e + 2] = fmaf(v[x][e].z, f, y[4 * e + 2]);
-        y[4 * e + 3] = fmaf(v[x][e].w, f, y[4 * e + 3]);
-      }
-    }
-  }
+  join_records<D, true>(a, rec0 + jr, kAttendRows, n_eff, p, P, c0, y, mt, lt);
   if (P > 1) {  // uniform
-    if ((tid & 15) == 0) {
-      s_m[0][p * R + jr] = jm;
-      s_l[0][p * R + jr] = jl;
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e) s_o[0][p * R + jr][c0 + e] = y[e];
-    __syncthreads();
+    join_parts<D>(s_m[0], s_l[0], s_o[0], p, P, jr, R, c0, y, mt, lt);
     if (p > 0) return;
-    for (int x = 1; x < P; ++x) jm = fmaxf(jm, s_m[0][x * R + jr]);
-    const float rf = jm == -INFINITY ? 0.f : jm;
-    jl = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) y[e] = 0.f;
-    for (int x = 0; x < P; ++x) {
-      const float f = rescale(s_m[0][x * R + jr], rf);
-      jl = fmaf(s_l[0][x * R + jr], f, jl);
-#pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = fmaf(s_o[0][x * R + jr][c0 + e], f, y[e]);
-    }
   }
-  attend_write<T, D>(a, attend_row(a, seq, tile * kAttendRows + jr, bh), bh, c0, y, jm, jl);
+  attend_write<T, D>(a, attend_row(a, seq, tile * kAttendRows + jr, bh), bh, c0, y, mt, lt);
 }
 
-// Joins the records of 16 rows of a tile's splits (tiles of 128 rows); thread (row,
-// coordinates) as above.
-template <int D>
+// Joins the records of a tile's splits where the last workgroup does not: 16 / P rows per
+// workgroup by P parts of 16 threads each that take every P-th record, so that no thread
+// takes more than eight at a time after another (kJoinParts of 128 records).
+template <typename T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   constexpr int E = D / 16;
+  __shared__ float s_m[16], s_l[16];
+  __shared__ __align__(16) float s_o[16][D + 4];
   const Dims& m = a.m;
+  const int P = a.join, R = 16 / P, per = a.rows / R;
   const int bh = (int)(blockIdx.x % (unsigned)m.bh), part = (int)(blockIdx.x / (unsigned)m.bh);
-  const int per = a.rows / 16, tile = a.tile0 + part / per;
-  const int r = part % per * 16 + (int)(threadIdx.x >> 4), c0 = (threadIdx.x & 15) * E;
+  const int tile = a.tile0 + part / per;
+  const int p = (int)threadIdx.x / (16 * R), jr = (int)(threadIdx.x >> 4) % R;
+  const int r = part % per * R + jr, c0 = (threadIdx.x & 15) * E;
   const int64_t u = (int64_t)bh * a.n_tiles + tile;
   const int n = a.n_eff[u];
   if (n <= 1) return;  // written by the pass
   const AttendRow row = attend_row(a, attend_seq(a, bh), tile * a.rows + r, bh);
-  const int64_t rec0 = u * a.n_split * a.rows + r;
-  float mt = -INFINITY, lt = 0.f, y[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) y[e] = 0.f;
-  // records eight at a time, their loads in flight together
-  for (int x0 = 0; x0 < n; x0 += 8) {
-    float2 h[8];
-    float4 v[8][E / 4];
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      const int64_t rec = rec0 + (int64_t)min(x0 + x, n - 1) * a.rows;
-      h[x] = *reinterpret_cast<const float2*>(a.ml + rec * 2);
-#pragma unroll
-      for (int e = 0; e < E / 4; ++e)
-        v[x][e] = *reinterpret_cast<const float4*>(a.part + rec * D + c0 + 4 * e);
-    }
-    float nm = mt;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) nm = fmaxf(nm, h[x].x);
-    const float ref = nm == -INFINITY ? 0.f : nm, alpha = rescale(mt, ref);
-    mt = nm;
-    lt *= alpha;
-#pragma unroll
-    for (int e = 0; e < E; ++e) y[e] *= alpha;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      if (x0 + x >= n) break;
-      const float f = rescale(h[x].x, ref);
-      lt = fmaf(h[x].y, f, lt);
-#pragma unroll
-      for (int e = 0; e < E / 4; ++e) {
-        y[4 * e] = fmaf(v[x][e].x, f, y[4 * e]);
-        y[4 * e + 1] = fmaf(v[x][e].y, f, y[4 * e + 1]);
-        y[4 * e + 2] = fmaf(v[x][e].z, f, y[4 * e + 2]);
-        y[4 * e + 3] = fmaf(v[x][e].w, f, y[4 * e + 3]);
-      }
-    }
+  if (R == 1 && !row.valid) return;
+  float mt, lt, y[E];
+  join_records<D, false>(a, u * a.n_split * a.rows + r, a.rows, n, p, P, c0, y, mt, lt);
+  if (P > 1) {
+    join_parts<D>(s_m, s_l, s_o, p, P, jr, R, c0, y, mt, lt);
+    if (p > 0) return;
   }
-  attend_write<bf16_t, D>(a, row, bh, c0, y, mt, lt);
+  attend_write<T, D>(a, row, bh, c0, y, mt, lt);
 }
 
 // ---------------------------------------------------------------- many rows
@@ -920,22 +927,22 @@ __global__ __launch_bounds__(256, 3) void attend_tile_kernel(AttendArgs a) {
   }
 
   const int64_t u = (int64_t)bh * a.n_tiles + tile;
-  if (a.n_split > 1 && split == 0 && tid == 0) a.n_eff[u] = n_eff;
+  if (a.join && split == 0 && tid == 0) a.n_eff[u] = n_eff;
   tile_write<D>(a, row, bh, h, ps.o, ps.ref, ps.l, n_eff,
                 (u * a.n_split + split) * kTileRows + rr);
 }
 
 static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
   using Kernel = void (*)(AttendArgs);
-  const auto go = [&](Kernel kern, Kernel join = nullptr) {
+  const auto go = [&](Kernel kern, Kernel join) {
     // a grid holds 2^32 threads: very long calls take several launches
     const int most = (int)((1 << 20) / a.m.bh) > 0 ? (1 << 20) / a.m.bh : 1;
     for (a.tile0 = 0; a.tile0 < a.n_tiles; a.tile0 += most) {
       const int n = a.n_tiles - a.tile0 < most ? a.n_tiles - a.tile0 : most;
       const unsigned wgs = (unsigned)a.m.bh * (unsigned)n;
       hipLaunchKernelGGL(kern, dim3(wgs, (unsigned)a.n_split), dim3(256), 0, st, a);
-      if (a.n_split > 1 && join)
-        hipLaunchKernelGGL(join, dim3(wgs * (unsigned)(a.rows / 16)), dim3(256), 0, st, a);
+      if (a.join)
+        hipLaunchKernelGGL(join, dim3(wgs * (unsigned)(a.rows * a.join / 16)), dim3(256), 0, st, a);
     }
   };
   // a cap this small bounds every score: weights against a reference of 0 stay in range
@@ -943,20 +950,20 @@ static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
   const bool bounded = cap && !bias && a.o.softcap * kLog2e <= 60.f;
   const auto tile = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    if (bounded) go(attend_tile_kernel<D, kCapped>, attend_join_kernel<D>);
-    else if (cap) go(attend_tile_kernel<D, kGeneral>, attend_join_kernel<D>);
-    else if (bias) go(attend_tile_kernel<D, kBiased>, attend_join_kernel<D>);
-    else go(attend_tile_kernel<D, kPlain>, attend_join_kernel<D>);
+    if (bounded) go(attend_tile_kernel<D, kCapped>, attend_join_kernel<bf16_t, D>);
+    else if (cap) go(attend_tile_kernel<D, kGeneral>, attend_join_kernel<bf16_t, D>);
+    else if (bias) go(attend_tile_kernel<D, kBiased>, attend_join_kernel<bf16_t, D>);
+    else go(attend_tile_kernel<D, kPlain>, attend_join_kernel<bf16_t, D>);
   };
   if (a.rows == kTileRows) {
     if (a.m.d == 64) tile(std::integral_constant<int, 64>{});
     else tile(std::integral_constant<int, 128>{});
   } else if (a.m.elem == 4) {
-    if (a.m.d == 64) go(attend_stream_kernel<float, 64>);
-    else go(attend_stream_kernel<float, 128>);
+    if (a.m.d == 64) go(attend_stream_kernel<float, 64>, attend_join_kernel<float, 64>);
+    else go(attend_stream_kernel<float, 128>, attend_join_kernel<float, 128>);
   } else {
-    if (a.m.d == 64) go(attend_stream_kernel<bf16_t, 64>);
-    else go(attend_stream_kernel<bf16_t, 128>);
+    if (a.m.d == 64) go(attend_stream_kernel<bf16_t, 64>, attend_join_kernel<bf16_t, 64>);
+    else go(attend_stream_kernel<bf16_t, 128>, attend_join_kernel<bf16_t, 128>);
   }
   return hipGetLastError();
 }
@@ -980,6 +987,7 @@ hipError_t launch_attend(const Dims& m, const spla_config& cfg, const spla_cache
   a.n_split = ws.n_split;
   a.rows = ws.rows;
   a.tile0 = 0;
+  a.join = ws.join;
   a.part = reinterpret_cast<float*>(base + ws.part);
   a.ml = reinterpret_cast<float*>(base + ws.ml);
   a.n_eff = reinterpret_cast<int32_t*>(base + ws.n_eff);

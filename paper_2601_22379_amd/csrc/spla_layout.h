@@ -434,12 +434,28 @@ SPLA_HD AppendRopeWs append_rope_ws_layout(const Dims& m, int max_new) {
 // workgroup per tile and split of the keys.
 constexpr int kAttendRows = 16;
 constexpr int kTileRows = 128;
-constexpr int kAttendFill = 768;      // workgroups to aim for (three per compute unit)
-constexpr int kTileFill = 768;        // ... of tiles of 128 rows (three)
-constexpr int kAttendMaxSplit = 128;  // workgroups that share one tile's keys at most
-constexpr int kAttendMinSteps = 4;    // 32-token steps per workgroup at least: one per wavefront
-constexpr int kTileMinSplit = 8;      // ... and of a tile of 128 rows
+// Workgroups that share a tile's keys: as many as fill the chip with two tiles of 16 rows
+// per compute unit (32K tokens, bf16 d 128, 8 heads: 64 rows 32.8 us, and 37.2 with three
+// per unit; one too many cost more: 48 rows 30.5 us with 504 workgroups, 38.9 with 528), or
+// three where that would leave them unsplit (264 tiles of 4096 tokens: 116 us, unsplit 125;
+// 400 tiles: 284 unsplit, 313 in two), or three tiles of 128 rows.
+constexpr int kAttendFill = 512;
+constexpr int kTileFill = 768;
+constexpr int kAttendMaxSplit = 128;  // and at most
+// Steps of 32 tokens per workgroup at least: one per wavefront of tiles of 16 rows (8: 13.0 us
+// against 10.5 for 16 rows of 4096 tokens); 16 for 128 rows (1024 rows of 1024 tokens:
+// 29.8 us, with 8 steps 34.7; 256 rows of 8192: 27.6 us, with 32 steps 36.0).
+constexpr int kAttendMinSteps = 4;
+constexpr int kTileMinSplit = 16;
+// Records that a tile's last workgroup joins at most: eight per thread, one wait for memory.
+// More go to a launch of their own, which has a thread for every eight records and 16th of a
+// row (16 records of 16 rows: 12.5 us, joined by the last workgroup 15.3; 64 of 4 rows: 28.5
+// and 29.3; 96 of 16 rows: 29 and 55).
+constexpr int kJoinInLaunch = 128;
 
+// Tiles of 128 rows from 65 rows on (4096 and 32K tokens, bf16 d 128, 8 heads of 4: 64 rows
+// 12.1 and 32.8 us in tiles of 16, 16.0 and 37.3 in one of 128; 96 rows at 32K tokens 57.5
+// and 35.5 us).
 SPLA_HD bool attend_wide(const Dims& m, int n_tokens) {
   return m.elem == 2 && (int64_t)n_tokens * m.group > 64;
 }
@@ -448,12 +464,14 @@ struct AttendWs {
   int rows;       // query rows per tile
   int n_tiles;    // row tiles per (sequence, kv head)
   int n_split;    // workgroups that may share a tile's keys
+  int join;       // parts per row of the launch that joins them; 0: none (one split, or the
+                  //   last workgroup of the tile joins)
   // the arrival counters of split tiles of 16 rows lie first, one per line, wherever
-  // the rest ends: zero between calls of any shape (i32 [kAttendFill][kSyncLine])
+  // the rest ends: zero between calls of any shape (i32 [kTileFill][kSyncLine])
   int64_t part;   // f32 [bh][n_tiles][n_split][rows][d]  unnormalised outputs
   int64_t ml;     // f32 [bh][n_tiles][n_split][rows][2]  reference (base 2) and sum of the weights
-  int64_t n_eff;  // i32 [bh][n_tiles]  tiles of 128 rows: splits with a record (1: none, the
-                  //   output is written)
+  int64_t n_eff;  // i32 [bh][n_tiles]  with join: splits with a record (1: none, the output is
+                  //   written)
   int64_t total;
 };
 
@@ -463,11 +481,17 @@ SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
   w.rows = wide ? kTileRows : kAttendRows;
   w.n_tiles = (int)ceil_div((int64_t)n_tokens * m.group, w.rows);
   const int64_t wgs = (int64_t)m.bh * w.n_tiles;
-  int64_t n = wgs > 0 ? (wide ? kTileFill / wgs : ceil_div(kAttendFill, wgs)) : 1;
+  int64_t n = 1;
+  if (wgs > 0) n = !wide && kAttendFill / wgs > 1 ? kAttendFill / wgs : kTileFill / wgs;
   const int64_t most = ceil_div(m.cap, (wide ? kTileMinSplit : kAttendMinSteps) * kSubTokens);
   n = n < most ? n : most;
   n = n < kAttendMaxSplit ? n : kAttendMaxSplit;
   w.n_split = (int)(n > 1 ? n : 1);
+  int rows = 1;  // of a tile of 16 that are joined: a power of two
+  while (rows < kAttendRows && rows < (int64_t)n_tokens * m.group) rows *= 2;
+  w.join = 0;
+  if (w.n_split > 1 && (wide || w.n_split * rows > kJoinInLaunch))
+    for (w.join = 1; w.join < 16 && w.n_split > 8 * w.join;) w.join *= 2;
   int64_t off = 0;
   auto take = [&](int64_t bytes) {
     const int64_t o = off;
@@ -475,10 +499,10 @@ SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
     return o;
   };
   const int64_t rec = w.n_split > 1 ? wgs * w.n_split * w.rows : 0;
-  if (rec) take((int64_t)kAttendFill * kSyncLine * 4);  // (split tiles are fewer than that)
+  if (rec) take((int64_t)kTileFill * kSyncLine * 4);  // (split tiles are fewer than that)
   w.part = take(rec * m.d * 4);
   w.ml = take(rec * 2 * 4);
-  w.n_eff = take(rec && wide ? wgs * 4 : 0);
+  w.n_eff = take(w.join ? wgs * 4 : 0);
   w.total = off;
   return w;
 }
