@@ -118,9 +118,11 @@ hipError_t launch_rotate(const Dims& m, const spla_rope& rope, const RotateRows&
   if (n == 0) return hipSuccess;
   const int vec = 16 / m.elem;
   const bool pieces = rope.rot_dim % (2 * vec) == 0;
-  // four rows per workgroup share the fp64 sine over all its threads; with fewer
-  // than 1024 rows a row each, which fills more of the chip
-  const bool many = n >= 1024;
+  // rows whose heads do not keep 256 threads busy go four to a workgroup, once that
+  // leaves one for every compute unit (16384 rows of 40 heads, bf16: d 64, 160 units,
+  // 31.5 us against 39.7 with a row each; d 128, 320 units, 55.8 against 57.9, fp32 d 128
+  // 120 against 113)
+  const bool many = n >= 1024 && (a.heads + b.heads) * (m.d / (2 * vec)) < 256;
   auto go = [&](auto one, auto four, auto any) {
     const int per = pieces && many ? 4 : 1;
     auto kern = !pieces ? any : many ? four : one;
