@@ -260,8 +260,12 @@ typedef struct spla_rope {
 
 /* ---------------------------------------------------- options of spla_attend
  * Zero-filled (or a NULL pointer): every query sees the tokens up to its own. */
+#define SPLA_SOFTCAP_MIN 0.0009765625f
+#define SPLA_SOFTCAP_MAX 1024.0f
+
 typedef struct spla_attend_opts {
-  float softcap;             /* c > 0: scores x become c tanh(x / c); 0: none */
+  float softcap;             /* c, SPLA_SOFTCAP_MIN .. SPLA_SOFTCAP_MAX: scores x become
+                                c tanh(x / c); 0: none */
   float reserved;
   const float* slopes;       /* device fp32 [Hq] or NULL: slopes[m] |p - j| is
                                 subtracted from the (capped) score of the query
@@ -491,7 +495,8 @@ int32_t spla_rotate(const spla_config* cfg, const spla_rope* rope, int32_t n_tok
  *              give the rotary position (a sequence whose oldest tokens were
  *              dropped, or that begins in the middle of a text).
  * The other arguments as spla_append; the workspace from
- * spla_append_rope_workspace_bytes, zero-filled before its first use. Queries of the same tokens: spla_rotate. */
+ * spla_append_rope_workspace_bytes, zero-filled before its first use. Queries of
+ * the same tokens: spla_rotate. */
 int32_t spla_append_rope(const spla_config* cfg, const spla_cache* cache, const spla_rope* rope,
                          const void* k_new, const void* v_new, int32_t max_new,
                          const int32_t* n_new, const int32_t* pos_shift, void* workspace,

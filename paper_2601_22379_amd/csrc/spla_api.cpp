@@ -398,7 +398,8 @@ extern "C" int32_t spla_attend(const spla_config* cfg, const spla_cache* cache, 
   if (n_tokens < 0) return SPLA_ERR_INVALID_ARG;
   if (n_tokens > cfg->max_seq_len) return SPLA_ERR_CAPACITY;
   const spla_attend_opts o = opts ? *opts : spla_attend_opts{};
-  if (!(o.softcap >= 0.f) || o.softcap > 3.4e38f) return SPLA_ERR_INVALID_ARG;  // NaN, infinite
+  if (o.softcap != 0.f && !(o.softcap >= SPLA_SOFTCAP_MIN && o.softcap <= SPLA_SOFTCAP_MAX))
+    return SPLA_ERR_INVALID_ARG;  // (NaN too)
   if (n_tokens == 0) return SPLA_OK;
   if (!q || !out || out == q || !aligned16(q) || !aligned16(out)) return SPLA_ERR_INVALID_ARG;
   const Dims m = spla::make_dims(*cfg);

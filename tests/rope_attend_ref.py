@@ -58,7 +58,8 @@ def check_turned(got, x, pos, w, **kw):
     assert torch.equal(got[..., r:], x[..., r:])
 
 
-def attention(q, k, v, pos, scale=None, softcap=0.0, slope=0.0, lo=None, hi=None):
+def attention(q, k, v, pos, scale=None, softcap=0.0, slope=0.0, lo=None, hi=None,
+              cap_series=False):
     """One head in fp64: q [T, d], k, v [L, d], visible keys lo[t] .. hi[t] - 1.
     Returns out, lse and bounds on the error of each (see bounds in the body)."""
     dt = q.dtype
@@ -69,22 +70,25 @@ def attention(q, k, v, pos, scale=None, softcap=0.0, slope=0.0, lo=None, hi=None
     j = torch.arange(L, device=q.device)
     see = (j >= lo[:, None]) & (j < hi[:, None])
     dot = q @ k.t() * scale
-    x = softcap * torch.tanh(dot / softcap) if softcap else dot
-    x = x - slope * (pos[:, None] - j).abs()
+    capped = softcap * torch.tanh(dot / softcap) if softcap else dot
+    x = capped - slope * (pos[:, None] - j).abs()
     x = x.masked_fill(~see, -math.inf)
     lse = torch.logsumexp(x, -1) if L else torch.full((T,), -math.inf, device=q.device).double()
     p = torch.exp(x - torch.where(lse == -math.inf, torch.zeros_like(lse), lse)[:, None])
     p = p.masked_fill(~see, 0.0)
     out = p @ torch.where(torch.isfinite(v), v, torch.zeros_like(v))
     # error of a score: d + 4 fp32 roundings of the sum's terms, 4 of the score's own size and of
-    # the running maximum's (scaling, bias, difference to it), tanh within 2^-21, exp2 within 2
-    # steps. A weight is off by that share of itself; bf16 weights are rounded once more; the
+    # the running maximum's (scaling, bias, difference to it), tanh within 2^-21, with
+    # cap_series (fp32, and few rows) also within 2^-18 of itself (below 1/4 six roundings, above
+    # that 2^-21 of four times itself), exp2 within 2 steps. A weight is off by that share of itself; bf16 weights are rounded once more; the
     # sums of L weights take fp32 roundings; the output is rounded once.
     top = x.amax(-1, keepdim=True) if L else torch.zeros((T, 1), device=q.device)
     top = torch.where(top == -math.inf, torch.zeros_like(top), top)
     xa = torch.where(see, x, torch.zeros_like(x)).abs()
     eps = (2.0 ** -24 * (d + 4) * scale * (q.abs() @ k.abs().t()) + 2.0 ** -22 * (xa + top.abs())
-           + softcap * 2.0 ** -21 + 2.0 ** -21)
+           + 2.0 ** -21)
+    cap = torch.full_like(x, softcap * 2.0 ** -21)
+    eps = eps + (torch.minimum(cap, 2.0 ** -18 * capped.abs()) if cap_series else cap)
     eps = torch.where(see, eps, torch.zeros_like(eps))
     steps = min(L, 4096) * 2.0 ** -24
     pe = p * (eps + steps)
@@ -107,7 +111,7 @@ def visible(L, n, T, first=None, prefix=0):
 
 
 def check_attend(out, lse, q, K, V, lens, news=None, scale=None, softcap=0.0, slopes=None,
-                 first=None, prefix=None, before=None):
+                 first=None, prefix=None, before=None, cap_series=False):
     """out, lse of a call against the 64-bit form. K, V [b, h, max, d]; q [T, b, hq, d];
     before: (out, lse) ahead of the call, which rows without a query keep."""
     T, b, hq, d = q.shape
@@ -122,7 +126,7 @@ def check_attend(out, lse, q, K, V, lens, news=None, scale=None, softcap=0.0, sl
         for m in range(hq):
             ref, rl, tol, lt = attention(q[:n, i, m], K[i, m // G, :L], V[i, m // G, :L], pos,
                                          scale, softcap, 0.0 if slopes is None else
-                                         float(slopes[m]), lo, hi)
+                                         float(slopes[m]), lo, hi, cap_series)
             err = (out[:n, i, m].double() - ref).abs()
             assert bool((err <= tol).all()), (i, m, float((err / tol).max()), float(err.max()))
             gone = rl == -math.inf

@@ -64,6 +64,11 @@ CASES = {
     "f32_chunk": ("f32", 128, 6, 2, 64, [300, 90], 77, True),
     "f32_g16": ("f32", 64, 16, 1, 128, [640], 9, False),
     "f32_long": ("f32", 128, 1, 1, 64, [5000], 2, False),
+    # keys in many splits, joined by a launch of their own; short sequences beside a long one
+    "splits": ("bf16", 128, 8, 2, 64, [3001, 0, 5, 129], 4, True),
+    "splits_rows_48": ("bf16", 64, 8, 2, 32, [2500, 40], 12, False),
+    "splits_rows_96": ("bf16", 128, 8, 2, 64, [6100, 300], 24, False),
+    "f32_splits": ("f32", 128, 4, 2, 64, [2800, 1, 70], 8, True),
 }
 KINDS = ["causal", "softcap", "bias", "docs", "prefix", "ragged", "all"]
 
@@ -117,6 +122,62 @@ def test_scale_and_three_dimensions(dev):
     out, lse = cache.attend(q)
     assert out.shape == (2, 8, 128) and lse.shape == (2, 8)
     R.check_attend(out[None], lse[None], q[None], K, V, [200, 90], scale=0.3)
+
+
+@pytest.mark.parametrize("softcap", [2.0 ** -10, 41.0, 42.0, 1024.0])
+@pytest.mark.parametrize("dtype,T", [("bf16", 9), ("bf16", 100), ("f32", 9)])
+def test_caps(dev, dtype, T, softcap):
+    """The smallest and the largest cap, and those on the two sides of the one up to which
+    weights need no maximum; scores up to a few hundred."""
+    cache, K, V = filled(dev, dtype, [400, 333], 8, 2, 128, 64)
+    q = randn(dev, dtype, T, 2, 8, 128, seed=3, scale=30.0)
+    for slopes in (None, torch.linspace(0.0, 1.0, 8, device=dev)):
+        out, lse = cache.attend(q, softcap=softcap, slopes=slopes)
+        R.check_attend(out, lse, q, K, V, [400, 333], softcap=softcap, slopes=slopes,
+                       cap_series=dtype == "f32" or T * 4 <= 64)
+
+
+@pytest.mark.parametrize("size", [2.0 ** 70, 2.0 ** -30])
+@pytest.mark.parametrize("softcap", [0.0, 41.0, 42.0])
+@pytest.mark.parametrize("dtype,T", [("bf16", 9), ("bf16", 100), ("f32", 9)])
+def test_large_and_small_values(dev, dtype, T, softcap, size):
+    """Queries against the keys' mean direction: scores at both ends of the cap."""
+    cache, K, V = filled(dev, dtype, [400, 333], 8, 2, 128, 64)
+    cache.reset()
+    K, V = K + 2.0, V * size
+    cache.append(K, V, torch.tensor([400, 333], dtype=torch.int32, device=dev))
+    q = randn(dev, dtype, T, 2, 8, 128, seed=3)
+    q[:, :, ::2] = 1.0
+    q[:, :, 1::2] = -1.0
+    out, lse = cache.attend(q, softcap=softcap)
+    R.check_attend(out, lse, q, K, V, [400, 333], softcap=softcap,
+                   cap_series=dtype == "f32" or T * 4 <= 64)
+
+
+@pytest.mark.parametrize("dtype,T", [("bf16", 12), ("bf16", 70), ("f32", 30)])
+def test_more_queries_than_tokens_and_first_keys_outside(dev, dtype, T):
+    lens = [5, 40, 0, 700]
+    cache, K, V = filled(dev, dtype, lens, 4, 1, 64, 32)
+    q = randn(dev, dtype, T, 4, 4, 64, seed=5)
+    for pre in (None, [4, 0, 3, 900]):
+        dev_pre = None if pre is None else torch.tensor(pre, dtype=torch.int32, device=dev)
+        out, lse = cache.attend(q, prefix_len=dev_pre)
+        R.check_attend(out, lse, q, K, V, lens, prefix=pre)
+    g = torch.Generator().manual_seed(T)
+    first = torch.randint(-50, 750, (T, 4), generator=g).int().to(dev)
+    first[0, 0], first[1, 0] = -(1 << 31), (1 << 31) - 1
+    out, lse = cache.attend(q, first_key=first)
+    R.check_attend(out, lse, q, K, V, lens, first=first)
+
+
+@pytest.mark.parametrize("T", [1, 30])
+def test_sequences_that_share_pages(dev, T):
+    cache, K, V = filled(dev, "bf16", [300, 192], 4, 1, 128, 64, paged=True)
+    cache.block_table[1, :3] = cache.block_table[0, :3]
+    K[1, :, :192], V[1, :, :192] = K[0, :, :192], V[0, :, :192]
+    q = randn(dev, "bf16", T, 2, 4, 128, seed=6)
+    out, lse = cache.attend(q)
+    R.check_attend(out, lse, q, K, V, [300, 192])
 
 
 @pytest.mark.parametrize("dtype,T", [("bf16", 40), ("bf16", 2), ("bf16", 300), ("f32", 40)])

@@ -36,6 +36,7 @@ SHAPES = [  # dtype, d, rot, layout, T, batch, hq, hkv
     ("bf16", 128, 128, "interleaved", 7, 3, 5, 1),
     ("bf16", 128, 64, "half", 300, 4, 8, 2),          # four rows per workgroup, part rotated
     ("bf16", 128, 96, "interleaved", 1031, 1, 4, 4),
+    ("bf16", 128, 128, "half", 1100, 1, 32, 8),       # one row per workgroup, many rows
     ("bf16", 64, 64, "half", 33, 2, 16, 1),
     ("bf16", 64, 30, "half", 5, 2, 4, 2),             # pair by pair
     ("bf16", 64, 2, "interleaved", 9, 1, 3, 3),
@@ -67,6 +68,17 @@ def test_rotate(dev, case, transpose):
     none, got = spla.rotate(cfg, rope, k=k2, k_out=k2, positions=pos, transpose=transpose)
     assert none is None and got is k2
     R.check_turned(k2, k, pos[..., None], w, layout=layout, gain=1.25, transpose=transpose)
+
+
+def test_more_rows_than_a_launch_holds(dev):
+    """Over 2^22 workgroups and 2^31 elements, in place."""
+    cfg, rope, w = config(1, 8, 8, 64), spla.make_rope(64, 22), R.frequencies(22)
+    T = (1 << 22) + 5
+    base = randn(dev, "bf16", 1009, 1, 8, 64, seed=4)
+    x = base.repeat(-(-T // 1009), 1, 1, 1)[:T]
+    spla.rotate(cfg, rope, q=x, q_out=x)
+    t = torch.cat([torch.arange(0, 40), torch.arange((1 << 22) - 40, T)]).to(dev)
+    R.check_turned(x[t], base[t % 1009], t[:, None, None], w)
 
 
 def test_rotate_strided_rows(dev):

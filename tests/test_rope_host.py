@@ -132,7 +132,7 @@ def test_attend_refuses():
     assert call(q=None) == -1 and call(out=None) == -1 and call(out=256) == -1
     assert call(q=264) == -1 and call(out=520) == -1
     assert call(cache=None) == -1 and call(cache=spla.SplaCacheStruct()) == -1
-    for bad in (-1.0, float("nan"), float("inf")):
+    for bad in (-1.0, float("nan"), float("inf"), 2.0 ** -11, 1025.0, 1e-40):
         assert call(cap=bad) == -1
     need = spla.attend_workspace_bytes(c, 4)
     assert need > 0
