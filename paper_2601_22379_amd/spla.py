@@ -363,6 +363,8 @@ def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_
                 or t.device != device):
             raise ValueError(f"{name}: {n} contiguous int32 values on the rows' device")
         at.append(t.data_ptr())
+    if device.type != "cuda":
+        raise ValueError("tensors on a GPU are needed")
     _launch(lib().spla_rotate, "spla_rotate", device,
             (ctypes.byref(cfg), ctypes.byref(rope), T, at[0], at[1], qp, qs, op, os_, kp, ks, tp,
              ts, 1 if transpose else 0))
@@ -543,6 +545,9 @@ class SplaCache:
         if need is None:
             need = self._ws_sizes[kind, n] = sizes(self.cfg, n)
         if ws is None or ws.numel() < need:
+            if torch.cuda.is_current_stream_capturing():  # its zeros would come with a replay only
+                raise RuntimeError("a capture needs a call of its sizes ahead of it, which makes "
+                                   "the workspace")
             if ws is not None:
                 self._outgrown.append(ws)
             ws = _aligned_workspace(need, self.device).zero_()
@@ -567,7 +572,8 @@ class SplaCache:
                     n_new: Optional[torch.Tensor] = None,
                     pos_shift: Optional[torch.Tensor] = None):
         """append() with the keys rotated on the way, the token that lands at position p of the
-        cache by the angles of p (+ pos_shift[b], int32 [batch])."""
+        cache by the angles of p (+ pos_shift[b], int32 [batch]). Ahead of a graph capture a
+        call of the same max_new makes the workspace."""
         c = self.cfg
         if k_new.dim() != 4:
             raise ValueError("k_new: [batch, Hkv, max_new, d] is needed")
@@ -592,7 +598,8 @@ class SplaCache:
         tanh(x / softcap). slopes fp32 [Hq]: slopes[m] |p - j| is subtracted. first_key int32
         [T, batch]: the first position each query sees. prefix_len int32 [batch]: positions
         every query sees. n_new int32 [batch]: the queries each sequence really has; the
-        rows of out and lse past them are left as they are (zeros in tensors made here)."""
+        rows of out and lse past them are left as they are (zeros in tensors made here). Ahead
+        of a graph capture a call of the same T makes the workspace."""
         c, shape, dtype = self.cfg, q.shape, torch_dtype(self.cfg)
         if len(shape) not in (3, 4):
             raise ValueError("q: [T, batch, Hq, d] is needed")

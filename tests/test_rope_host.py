@@ -150,3 +150,33 @@ def test_binding_checks_rows():
                 dict(q=q[..., ::2])):
         with pytest.raises(ValueError):
             spla.rotate(c, r, **bad)
+
+
+def test_rows_on_the_host_are_refused():
+    q = torch.zeros(3, 2, 8, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        spla.rotate(_cfg(), spla.make_rope(128), q=q)
+
+
+def test_a_workspace_does_not_grow_in_a_capture(monkeypatch):
+    """A fill recorded by the capture would leave the counters of other calls undefined until
+    the first replay."""
+    cache = object.__new__(spla.SplaCache)
+    cache.cfg, cache.device = _cfg(), torch.device("cpu")
+    cache._ws_sizes, cache._outgrown = {}, []
+
+    def sizes(cfg, n):
+        return 256 * n
+    monkeypatch.setattr(spla, "_aligned_workspace",
+                        lambda n, device: torch.empty(n, dtype=torch.uint8))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    ws = cache._workspace("attend", 4, sizes, None)
+    assert ws.numel() >= 1024 and not ws.any()
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    assert cache._workspace("attend", 3, sizes, ws) is ws
+    with pytest.raises(RuntimeError):
+        cache._workspace("attend", 5, sizes, ws)
+    with pytest.raises(RuntimeError):
+        cache._workspace("rope", 1, sizes, None)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    assert cache._workspace("attend", 5, sizes, ws).numel() >= 1280 and cache._outgrown[0] is ws
