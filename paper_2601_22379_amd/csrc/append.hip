@@ -651,7 +651,7 @@ __device__ __forceinline__ double2 turn_on(double2 a, double2 b) {
 }
 
 template <int D, bool ROPE>
-__global__ __launch_bounds__(256) void append_fused_kernel(
+__global__ __launch_bounds__(256, 2) void append_fused_kernel(
     Dims m, bf16_t* __restrict__ kcache, bf16_t* __restrict__ vcache, float* __restrict__ stats,
     const int32_t* __restrict__ seq_lens, int32_t* __restrict__ err,
     const bf16_t* __restrict__ k_new, const bf16_t* __restrict__ v_new, int max_new,
