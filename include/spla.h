@@ -489,8 +489,10 @@ int32_t spla_rotate(const spla_config* cfg, const spla_rope* rope, int32_t n_tok
 /* spla_append with the rotation applied to the keys on the way: the row at
  * position p = L_b + t (plus pos_shift[b]) is rotated, rounded to the cache
  * dtype and appended; values are appended as they are. Rows, statistics and
- * lengths become those of spla_append of the rotated rows, S_bar and z_bar too up
- * to the rounding of their fp32 sums.
+ * lengths become those of spla_append of the rows that spla_rotate gives (angles of
+ * long chunks are turned on in fp64 step by step, within 1e-12 of a turn: an element
+ * next to a rounding border may come out as the neighbouring value), S_bar and z_bar
+ * too up to the rounding of their fp32 sums.
  *  pos_shift:  device int32 [batch] or NULL (0): added to the cache position to
  *              give the rotary position (a sequence whose oldest tokens were
  *              dropped, or that begins in the middle of a text).

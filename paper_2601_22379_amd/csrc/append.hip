@@ -838,7 +838,7 @@ __global__ __launch_bounds__(256, 2) void append_fused_kernel(
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         ph[s][i] = kf[i] * inv;
-        zacc[i] += ph[s][i];
+        zacc[i] = fmaf(kf[i], inv, zacc[i]);  // (written out: the compiler fuses it or not)
       }
     }
     {
