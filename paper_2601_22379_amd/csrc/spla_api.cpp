@@ -367,6 +367,8 @@ extern "C" int32_t spla_append_rope(const spla_config* cfg, const spla_cache* ca
   hipStream_t st = static_cast<hipStream_t>(stream);
   const spla::AppendWs A = spla::append_ws_layout(m, max_new);
   const bool one_pass = spla::append_fusable(m);
+  // in the registers of the one pass where pieces of 8 coordinates hold whole pairs (16384
+  // tokens of 4 x 8 units: 169 us, plain append 143), else into the workspace first (330)
   if (one_pass && rope->rot_dim % 16 == 0) {
     SPLA_TRY(spla::launch_append_fused(m, *cache, k_new, v_new, max_new, n_new, A, ws + L.append,
                                        st, rope, pos_shift));
