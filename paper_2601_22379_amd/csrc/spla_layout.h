@@ -283,7 +283,7 @@ SPLA_HD int prefill_most_splits(const Dims& m) {
 // its places make of kPrefillFill, up to two. A wavefront alone on its SIMD runs
 // little faster than two (half a round 0.8), and the ends of a first round fill with
 // a second (half a round 0.7, three quarters 0.85). 4 x 8 units at 128K, 8 positions:
-// 16 splits (1024 places) 127 us, 32 (2048) 97; 96 positions: 3 (2304) 768, 4 (3072)
+// 16 splits (1024 places) 127 us, 32 (2048) 97; 96 positions: 3 (2304) 768, 4 (a third more)
 // 621; 8 units of 5 heads, 48 positions: 12 (2304) 82, 10 (1920) 69. Of equals the
 // largest even one (lists longer than k: there 8 took 80).
 SPLA_HD int prefill_splits(const Dims& m, int T) {
