@@ -1,5 +1,7 @@
 """Exact attention over the cache on the GPU against the 64-bit form."""
 
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -292,6 +294,53 @@ def test_streams_and_graphs(dev, T):
         for got, lg, kw in ((out, lse, {}), (out2, lse2, dict(softcap=7.0))):
             want, want_lse = cache.attend(q, **kw)
             assert torch.equal(got, want) and torch.equal(lg, want_lse), i
+
+
+def test_without_options_and_lse(dev):
+    """The C call with NULL options and no log-sum-exp."""
+    cache, K, V = filled(dev, "bf16", [500, 70], 8, 2, 128, 64)
+    for T in (1, 20, 100):
+        q = randn(dev, "bf16", T, 2, 8, 128, seed=T)
+        want, _ = cache.attend(q)
+        out = torch.empty_like(q)
+        ws = torch.zeros(spla.attend_workspace_bytes(cache.cfg, T), dtype=torch.uint8, device=dev)
+        assert spla.lib().spla_attend(
+            ctypes.byref(cache.cfg), ctypes.byref(cache._struct), T, q.data_ptr(), None,
+            out.data_ptr(), None, ws.data_ptr(), ws.numel(),
+            torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("T", [1, 4, 100])
+def test_two_caches_on_two_streams(dev, T):
+    """Calls in flight at once, each on its own cache and workspace."""
+    caches = [filled(dev, "bf16", [3000, 900 + 64 * i], 8, 2, 128, 64, cap=4096, seed=i + 1)[0]
+              for i in range(2)]
+    qs = [randn(dev, "bf16", T, 2, 8, 128, seed=9 + i) for i in range(2)]
+    want = [c.attend(q) for c, q in zip(caches, qs)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [(torch.empty_like(w[0]), torch.empty_like(w[1])) for w in want]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                caches[i].attend(qs[i], *got[i])
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_sliding_window_on_a_cache_with_selection_windows(dev, T):
+    """Negative slopes too: scores that grow with the distance."""
+    lens = [1500, 64]
+    cache, K, V = filled(dev, "bf16", lens, 8, 2, 128, 64, sel_window=32, sel_stride=16)
+    q = randn(dev, "bf16", T, 2, 8, 128, seed=2)
+    pos = torch.tensor(lens) - T + torch.arange(T)[:, None]
+    first = (pos - 127).int().to(dev)
+    slopes = torch.linspace(-0.05, 0.05, 8, device=dev)
+    out, lse = cache.attend(q, first_key=first, slopes=slopes)
+    R.check_attend(out, lse, q, K, V, lens, first=first, slopes=slopes)
 
 
 def test_served_sequence(dev):
