@@ -304,33 +304,43 @@ def _launch(fn, where, device, args):
         raise SplaError(status, where)
 
 
-def _row_stride(x: torch.Tensor) -> int:
+def _row_stride(x: torch.Tensor, row: int) -> int:
     """Elements between the rows (t, b), (t, b + 1) of x [T, batch, heads, d] or [batch, heads,
-    d], whose heads and coordinates lie one after the other and whose rows are evenly spaced."""
-    b, h, d = x.shape[-3:]
+    d], whose heads and coordinates lie one after the other (row of them) and whose rows are
+    evenly spaced."""
     if x.is_contiguous():
-        return h * d
+        return row
+    b, h, d = x.shape[-3:]
     T = x.shape[0] if x.dim() == 4 else 1
-    row = x.stride(-3) if b > 1 else x.stride(0) if T > 1 else h * d
+    row = x.stride(-3) if b > 1 else x.stride(0) if T > 1 else row
     ok = x.stride(-1) == 1 and (h == 1 or x.stride(-2) == d)
     if not ok or (b > 1 and T > 1 and x.stride(0) != b * row):
         raise ValueError("rows of heads one after the other, evenly spaced, are needed")
     return row
 
 
-def _rows(name, x, y, lead, heads, cfg, dtype, device):
-    """y, or a new output of the rows x [*lead, heads, d]; both checked."""
-    shape = x.shape
-    if shape[:-2] != lead or shape[-2:] != (heads, cfg.head_dim) or x.dtype is not dtype:
-        raise ValueError(f"{name}: a {dtype} tensor [T, {cfg.batch}, {heads}, {cfg.head_dim}] is "
-                         "needed, T the same for q and k")
+def _rows(name, x, y, shape, dtype, device):
+    """y, or a new output of the rows x, with the addresses and row strides of both: (y, x's
+    address, x's stride, y's address, y's stride)."""
+    if x.shape != shape or x.dtype is not dtype or x.device != device:
+        raise ValueError(f"{name}: a {dtype} tensor {list(shape)} is needed, T and the device the "
+                         "same for q and k")
+    row = shape[-2] * shape[-1]
+    at, stride = x.data_ptr(), _row_stride(x, row)
+    if y is x:
+        return y, at, stride, at, stride
     if y is None:
         y = torch.empty(shape, dtype=dtype, device=device)
-    elif y.shape != shape or y.dtype is not dtype:
-        raise ValueError(f"{name}_out: a {dtype} tensor of {name}'s shape is needed")
-    if x.device != device or y.device != device:
-        raise ValueError("tensors on different devices")
-    return y
+    elif y.shape != shape or y.dtype is not dtype or y.device != device:
+        raise ValueError(f"{name}_out: a {dtype} tensor like {name} is needed")
+    return y, at, stride, y.data_ptr(), _row_stride(y, row)
+
+
+def _row_words(name, t, n, device):
+    """The address of the int32 values t, one of n per row or sequence."""
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name}: {n} contiguous int32 values on the rows' device")
+    return t.data_ptr()
 
 
 def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_lens=None,
@@ -343,31 +353,23 @@ def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_
     x = k if q is None else q
     if x is None or (q is None and q_out is not None) or (k is None and k_out is not None):
         raise ValueError("q or k is needed, and no output without its input")
-    lead, device, dtype = x.shape[:-2], x.device, torch_dtype(cfg)
-    if len(lead) not in (1, 2) or lead[-1] != cfg.batch:
-        raise ValueError(f"rows of [T, {cfg.batch}] or [{cfg.batch}] positions are needed")
-    T = lead[0] if len(lead) == 2 else 1
+    n, batch, d, device, dtype = x.dim(), cfg.batch, cfg.head_dim, x.device, torch_dtype(cfg)
+    if n not in (3, 4):
+        raise ValueError(f"rows of [T, {batch}] or [{batch}] positions are needed")
+    T = x.shape[0] if n == 4 else 1
+    lead = (T, batch) if n == 4 else (batch,)
     qp = qs = op = os_ = kp = ks = tp = ts = 0
     if q is not None:
-        q_out = _rows("q", q, q_out, lead, cfg.n_q_heads, cfg, dtype, device)
-        qp, qs, op, os_ = q.data_ptr(), _row_stride(q), q_out.data_ptr(), _row_stride(q_out)
+        q_out, qp, qs, op, os_ = _rows("q", q, q_out, lead + (cfg.n_q_heads, d), dtype, device)
     if k is not None:
-        k_out = _rows("k", k, k_out, lead, cfg.n_kv_heads, cfg, dtype, device)
-        kp, ks, tp, ts = k.data_ptr(), _row_stride(k), k_out.data_ptr(), _row_stride(k_out)
-    at = []
-    for name, t, n in (("positions", positions, T * cfg.batch), ("seq_lens", seq_lens, cfg.batch)):
-        if t is None:
-            at.append(None)
-            continue
-        if (t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous()
-                or t.device != device):
-            raise ValueError(f"{name}: {n} contiguous int32 values on the rows' device")
-        at.append(t.data_ptr())
+        k_out, kp, ks, tp, ts = _rows("k", k, k_out, lead + (cfg.n_kv_heads, d), dtype, device)
+    at = None if positions is None else _row_words("positions", positions, T * batch, device)
+    lens = None if seq_lens is None else _row_words("seq_lens", seq_lens, batch, device)
     if device.type != "cuda":
         raise ValueError("tensors on a GPU are needed")
     _launch(lib().spla_rotate, "spla_rotate", device,
-            (ctypes.byref(cfg), ctypes.byref(rope), T, at[0], at[1], qp, qs, op, os_, kp, ks, tp,
-             ts, 1 if transpose else 0))
+            (ctypes.byref(cfg), ctypes.byref(rope), T, at, lens, qp, qs, op, os_, kp, ks, tp, ts,
+             1 if transpose else 0))
     return q_out, k_out
 
 
