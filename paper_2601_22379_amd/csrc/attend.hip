@@ -665,7 +665,8 @@ __device__ __forceinline__ void wait_copies() {
   asm volatile("" ::: "memory");
 }
 
-// kCapped: a cap that bounds all scores, no bias; kGeneral: any cap, and a bias
+// kCapped: a cap that bounds all scores, no bias; kBiased: no cap, and no prefix; kGeneral:
+// any. (Packed documents, 2 x 4096 tokens of 32 heads: kBiased 148 us, kGeneral 187.)
 enum { kPlain = 0, kCapped = 1, kBiased = 2, kGeneral = 3 };
 
 template <int D, int KIND>
@@ -701,12 +702,17 @@ struct TilePass {
       x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, buf.k[at_k + 32 * s]),
                                                   q[s], x, 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (KIND == kBiased || KIND == kGeneral) {
-      const float base = (float)(pos - t0 - 8 * h);
+    const float base = (float)(pos - t0 - 8 * h);
+    if constexpr (KIND == kBiased) {  // no token after the query's is seen: |p - j| = p - j
+      const float c = -slope2 * base;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = fmaf(x[i], mul, fmaf(slope2, (float)token(i), c));
+    }
+    if constexpr (KIND == kGeneral) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         float y = x[i] * mul;
-        if constexpr (KIND == kGeneral) y = capped(y);
+        if (cap2 > 0.f) y = capped(y);
         x[i] = fmaf(-slope2, fabsf(base - (float)token(i)), y);
       }
     }
@@ -970,7 +976,8 @@ static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
   const auto tile = [&](auto d) {
     constexpr int D = decltype(d)::value;
     if (bounded) go(attend_tile_kernel<D, kCapped>, attend_join_kernel<bf16_t, D>);
-    else if (cap) go(attend_tile_kernel<D, kGeneral>, attend_join_kernel<bf16_t, D>);
+    else if (cap || (bias && a.o.prefix_len))
+      go(attend_tile_kernel<D, kGeneral>, attend_join_kernel<bf16_t, D>);
     else if (bias) go(attend_tile_kernel<D, kBiased>, attend_join_kernel<bf16_t, D>);
     else go(attend_tile_kernel<D, kPlain>, attend_join_kernel<bf16_t, D>);
   };

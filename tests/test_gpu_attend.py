@@ -330,6 +330,19 @@ def test_two_caches_on_two_streams(dev, T):
         assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
 
 
+@pytest.mark.parametrize("T", [12, 90])
+def test_bias_with_a_prefix(dev, T):
+    """Keys on both sides of the query, with steep slopes."""
+    lens = [700, 130]
+    cache, K, V = filled(dev, "bf16", lens, 8, 2, 128, 64)
+    q = randn(dev, "bf16", T, 2, 8, 128, seed=2)
+    slopes = torch.linspace(0.0, 2.0, 8, device=dev)
+    for prefix in (None, [700, 100]):
+        pre = None if prefix is None else torch.tensor(prefix, dtype=torch.int32, device=dev)
+        out, lse = cache.attend(q, slopes=slopes, prefix_len=pre)
+        R.check_attend(out, lse, q, K, V, lens, slopes=slopes, prefix=prefix)
+
+
 @pytest.mark.parametrize("T", [1, 40])
 def test_sliding_window_on_a_cache_with_selection_windows(dev, T):
     """Negative slopes too: scores that grow with the distance."""
