@@ -265,6 +265,26 @@ struct StepOps<float, D> {
         v[t][s] = *reinterpret_cast<const float4*>(vp + (int64_t)16 * s * m.B + 16 * t);
       }
   }
+  // The same pieces by way of LDS, each 1 KiB in lane order: 2 D / 16 of keys, then as
+  // many of values. src_piece: where lane l of piece p finds its 16 bytes.
+  static constexpr int kPieces = D / 4;
+  static __device__ __forceinline__ const float* src_piece(const Dims& m, const void* kc,
+                                                           const void* vc, int64_t slot, int tb,
+                                                           int p, int lane) {
+    const int j = lane & 15, g = lane >> 4, t = p / (D / 16) & 1, s = p % (D / 16);
+    return p < kPieces / 2
+               ? static_cast<const float*>(kc) + (slot * m.B + tb + 16 * t + j) * D + 16 * s + 4 * g
+               : static_cast<const float*>(vc) + (slot * D + 16 * s + j) * m.B + tb + 16 * t + 4 * g;
+  }
+  __device__ __forceinline__ void load_lds(const float4* buf, int lane) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) {
+        k[t][s] = buf[(t * (D / 16) + s) * 64 + lane];
+        v[t][s] = buf[(kPieces / 2 + t * (D / 16) + s) * 64 + lane];
+      }
+  }
   static __device__ __forceinline__ floatx4 dot4(float4 a, float4 b, floatx4 c) {
     c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x, b.x, c, 0, 0, 0);
     c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.y, b.y, c, 0, 0, 0);
@@ -424,51 +444,37 @@ __device__ __forceinline__ void join_parts(float (&s_m)[16], float (&s_l)[16],
   }
 }
 
-// A tile of 16 query rows; the four wavefronts take every fourth 32-token step of
-// this split's keys and are joined at the end. Few rows are bound by the keys' and
-// values' bytes: one token of 4 heads on each of 8 KV heads (bf16, d 128) reads 16 x 64K
-// tokens at 6.0 TB/s, 16 x 16K to 64K at 5.2, and 32K tokens in 28 us; 4096 tokens take
-// 9.6 us, of which loads and join are a few round trips to memory. Two workgroups per compute
-// unit: left to itself the compiler takes 292 registers for fp32 rows of 128 coordinates,
-// which leaves one (1024 rows over 1312 tokens 132 us against 115).
+// One wavefront's tile of 16 query rows (columns) over steps of 32 tokens.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void attend_stream_kernel(AttendArgs a) {
-  constexpr int OT = D / 16;
-  __shared__ float s_m[4][16], s_l[4][16];
-  __shared__ __align__(16) float s_o[4][16][D + 4];
-  __shared__ int s_last;
-  const Dims& m = a.m;
-  const int bh = (int)(blockIdx.x % (unsigned)m.bh);
-  const int tile = a.tile0 + (int)(blockIdx.x / (unsigned)m.bh), split = (int)blockIdx.y;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, j = lane & 15, g = lane >> 4;
-  StepOps<T, D> ops;  // the queries first: their loads wait for nothing
-  ops.load_q(static_cast<const T*>(a.q) + attend_q_at(a, (int64_t)tile * kAttendRows + j, bh), g);
-  const AttendSeq seq = attend_seq(a, bh);
-  const AttendRow row = attend_row(a, seq, tile * kAttendRows + j, bh);
-  const bool any = row.hi > row.lo;
-  // the tile's keys, and those that all of its (non-empty) queries see
-  const int lo_min = -cols_max<16>(any ? -row.lo : -INT32_MAX), hi_max = cols_max<16>(row.hi);
-  const int lo_max = cols_max<16>(any ? row.lo : 0), hi_min = -cols_max<16>(any ? -row.hi : -INT32_MAX);
-  const int step0 = hi_max > 0 ? lo_min / 32 : 0;
-  const int n_steps = hi_max > 0 ? (hi_max + 31) / 32 - step0 : 0;
-  const int per = max((n_steps + a.n_split - 1) / a.n_split, kAttendMinSteps);
-  const int n_eff = (n_steps + per - 1) / per;
-  if (split > 0 && split >= n_eff) return;
-  const int first = step0 + split * per, last = min(first + per, step0 + n_steps);
-
-  const ScoreMap map(a, row.valid ? row.head : 0);
-  float mx = -INFINITY, l = 0.f;
+struct StreamPass {
+  static constexpr int OT = D / 16;
+  StepOps<T, D> ops;
+  AttendRow row;
+  ScoreMap map;
+  int lo_min, hi_max, lo_max, hi_min;  // keys of the tile, and those all its (non-empty) rows see
+  float mx, l;                         // running maximum (base 2), sum of this lane's weights
   floatx4 o[OT];
+
+  __device__ __forceinline__ StreamPass(const AttendArgs& a, int bh, int64_t row0, int lane)
+      : map(a, 0) {
+    const int j = lane & 15, g = lane >> 4;
+    // the queries first: their loads wait for nothing
+    ops.load_q(static_cast<const T*>(a.q) + attend_q_at(a, row0 + j, bh), g);
+    row = attend_row(a, attend_seq(a, bh), (int)row0 + j, bh);
+    map = ScoreMap(a, row.valid ? row.head : 0);
+    const bool any = row.hi > row.lo;
+    lo_min = -cols_max<16>(any ? -row.lo : -INT32_MAX);
+    hi_max = cols_max<16>(row.hi);
+    lo_max = cols_max<16>(any ? row.lo : 0);
+    hi_min = -cols_max<16>(any ? -row.hi : -INT32_MAX);
+    mx = -INFINITY;
+    l = 0.f;
 #pragma unroll
-  for (int t = 0; t < OT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const int sh = m.B == 32 ? 0 : m.B == 64 ? 1 : 2;  // log2 of the steps per block
-  // the next step's page is looked up while this one's rows are used
-  int64_t slot = first + w < last ? attend_slot(a, bh, (first + w) >> sh) : 0;
-#pragma unroll 1
-  for (int st = first + w; st < last; st += 4) {
-    const int t0 = st * 32;
-    ops.load_kv(m, a.k, a.v, slot, (st & ((1 << sh) - 1)) * 32, lane);
-    if (st + 4 < last) slot = attend_slot(a, bh, (st + 4) >> sh);
+    for (int t = 0; t < OT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // The step at t0, whose rows are in ops.
+  __device__ __forceinline__ void step(int t0, int g) {
     float x[8];
     ops.scores(x);
 #pragma unroll
@@ -502,9 +508,7 @@ __global__ __launch_bounds__(256, 2) void attend_stream_kernel(AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[t][i] *= alpha;
     }
-    // values that some query of the tile does not see are multiplied by a zero
-    // weight: harmless only if they are finite. Infinities and NaN are taken out
-    // of the product and given to the queries that see them.
+    // values that some query of the tile does not see (see odd_marks)
     const bool odd = !inner && __any(ops.odd());
     if (odd) {
       float see[8];
@@ -525,8 +529,50 @@ __global__ __launch_bounds__(256, 2) void attend_stream_kernel(AttendArgs a) {
 #pragma unroll
     for (int t = 0; t < OT; ++t) o[t] = ops.product(t, pk, o[t]);
   }
-  l += xor16(l);
-  l += xor32(l);
+
+  // The sum over the tokens of all lanes of this lane's column.
+  __device__ __forceinline__ float sum() const {
+    const float s = l + xor16(l);
+    return s + xor32(s);
+  }
+};
+
+// A tile of 16 query rows; the four wavefronts take every fourth 32-token step of
+// this split's keys and are joined at the end. Few rows are bound by the keys' and
+// values' bytes: one token of 4 heads on each of 8 KV heads (bf16, d 128) reads 16 x 64K
+// tokens at 6.0 TB/s, 16 x 16K to 64K at 5.2, and 32K tokens in 28 us; 4096 tokens take
+// 9.6 us, of which loads and join are a few round trips to memory. Two workgroups per compute
+// unit: left to itself the compiler takes 292 registers for fp32 rows of 128 coordinates,
+// which leaves one (1024 rows over 1312 tokens 132 us against 115).
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void attend_stream_kernel(AttendArgs a) {
+  constexpr int OT = D / 16;
+  __shared__ float s_m[4][16], s_l[4][16];
+  __shared__ __align__(16) float s_o[4][16][D + 4];
+  __shared__ int s_last;
+  const Dims& m = a.m;
+  const int bh = (int)(blockIdx.x % (unsigned)m.bh);
+  const int tile = a.tile0 + (int)(blockIdx.x / (unsigned)m.bh), split = (int)blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, j = lane & 15, g = lane >> 4;
+  StreamPass<T, D> ps(a, bh, (int64_t)tile * kAttendRows, lane);
+  const AttendSeq seq = attend_seq(a, bh);
+  const int step0 = ps.hi_max > 0 ? ps.lo_min / 32 : 0;
+  const int n_steps = ps.hi_max > 0 ? (ps.hi_max + 31) / 32 - step0 : 0;
+  const int per = max((n_steps + a.n_split - 1) / a.n_split, kAttendMinSteps);
+  const int n_eff = (n_steps + per - 1) / per;
+  if (split > 0 && split >= n_eff) return;
+  const int first = step0 + split * per, last = min(first + per, step0 + n_steps);
+  const int sh = m.B == 32 ? 0 : m.B == 64 ? 1 : 2;  // log2 of the steps per block
+  // the next step's page is looked up while this one's rows are used
+  int64_t slot = first + w < last ? attend_slot(a, bh, (first + w) >> sh) : 0;
+#pragma unroll 1
+  for (int st = first + w; st < last; st += 4) {
+    ps.ops.load_kv(m, a.k, a.v, slot, (st & ((1 << sh) - 1)) * 32, lane);
+    if (st + 4 < last) slot = attend_slot(a, bh, (st + 4) >> sh);
+    ps.step(st * 32, g);
+  }
+  const float l = ps.sum(), mx = ps.mx;
+  const auto& o = ps.o;
   if (g == 0) {
     s_m[w][j] = mx;
     s_l[w][j] = l;
@@ -583,7 +629,7 @@ __global__ __launch_bounds__(256, 2) void attend_stream_kernel(AttendArgs a) {
   if (tid == 0) store_agent(ctr, 0);  // zero again for the next call
   // the valid rows are the first ones: R of them (a power of two) by 16 threads
   // each, in P = 16 / R parts that take every P-th record
-  const int nv = __popcll(__ballot(row.valid && lane < 16));
+  const int nv = __popcll(__ballot(ps.row.valid && lane < 16));
   int R = 1;
   while (R < nv) R *= 2;
   const int P = 16 / R, p = tid / (16 * R), jr = (tid >> 4) % R;
@@ -593,6 +639,91 @@ __global__ __launch_bounds__(256, 2) void attend_stream_kernel(AttendArgs a) {
     if (p > 0) return;
   }
   attend_write<T, D>(a, attend_row(a, seq, tile * kAttendRows + jr, bh), bh, c0, y, mt, lt);
+}
+
+// 16 bytes per lane from src (per lane) to dst (uniform) + 16 lane, without a
+// register in between; complete when vmcnt has counted it down.
+__device__ __forceinline__ void copy_to_lds(const void* src, void* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src,
+                                   (__attribute__((address_space(3))) uint32_t*)dst, 16, 0, 0);
+}
+
+// Waits for this wavefront's copies to LDS: the builtin, which the compiler counts (it
+// would otherwise wait for them, and for those issued since, at the reads).
+__device__ __forceinline__ void wait_copies() {
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt 0, the other counts open
+  asm volatile("" ::: "memory");
+}
+
+// Many fp32 rows: 64 per workgroup, 16 per wavefront, and the keys and values by way of
+// LDS (copied there in operand order a step ahead, as in the tiles of 128 rows): a load of
+// fp32 operands touches 16 rows of 64 bytes each, and four wavefronts that read them for
+// themselves wait on the first-level cache. 2048 tokens of 32 heads on 8 over 4096 (d 128) 980 us,
+// 105 of the 154 TFLOP/s of a large fp32 product, against 1435 in tiles of 16.
+template <int D>
+__global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a) {
+  using Ops = StepOps<float, D>;
+  __shared__ float4 buf0[Ops::kPieces * 64], buf1[Ops::kPieces * 64];
+  __shared__ int2 s_range[4];
+  const Dims& m = a.m;
+  const int bh = (int)(blockIdx.x % (unsigned)m.bh);
+  const int tile = a.n_tiles - 1 - (a.tile0 + (int)(blockIdx.x / (unsigned)m.bh));
+  const int split = (int)blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, j = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  StreamPass<float, D> ps(a, bh, (int64_t)tile * kRowsRows + w * 16, lane);
+  if (lane == 0) s_range[w] = make_int2(ps.lo_min, ps.hi_max);
+  __syncthreads();
+  int lo = s_range[0].x, hi = s_range[0].y;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) {
+    lo = min(lo, s_range[i].x);
+    hi = max(hi, s_range[i].y);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  const int step0 = hi > 0 ? lo / 32 : 0, n_steps = hi > 0 ? (hi + 31) / 32 - step0 : 0;
+  const int per = max((n_steps + a.n_split - 1) / a.n_split, kRowsMinSplit);
+  const int n_eff = (n_steps + per - 1) / per;
+  if (split > 0 && split >= n_eff) return;
+  const int first = step0 + split * per, last = min(first + per, step0 + n_steps);
+  const int sh = m.B == 32 ? 0 : m.B == 64 ? 1 : 2;  // log2 of the steps per block
+  auto load = [&](float4* buf, int st) {
+    const int64_t slot = attend_slot(a, bh, st >> sh);
+    const int tb = (st & ((1 << sh) - 1)) * 32;
+#pragma unroll
+    for (int i = 0; i < Ops::kPieces; i += 4)
+      copy_to_lds(Ops::src_piece(m, a.k, a.v, slot, tb, i + w, lane), buf + (i + w) * 64);
+  };
+  auto use = [&](float4* buf, float4* other, int st) {
+    wait_copies();  // this wavefront's copies of the step are in LDS
+    __syncthreads();
+    if (st + 1 < last) load(other, st + 1);
+    const int t0 = st * 32;
+    if (t0 >= ps.hi_max || t0 + 32 <= ps.lo_min) return;  // nothing here for this wavefront
+    ps.ops.load_lds(buf, lane);
+    ps.step(t0, g);
+  };
+  if (first < last) load(buf0, first);
+#pragma unroll 1
+  for (int st = first; st < last; st += 2) {
+    use(buf0, buf1, st);
+    if (st + 1 < last) use(buf1, buf0, st + 1);
+  }
+  const float l = ps.sum();
+  const int64_t u = (int64_t)bh * a.n_tiles + tile;
+  if (a.join && split == 0 && tid == 0) a.n_eff[u] = n_eff;
+  const int64_t rec = (u * a.n_split + split) * kRowsRows + w * 16 + j;
+  if (n_eff > 1 && g == 0) *reinterpret_cast<float2*>(a.ml + rec * 2) = make_float2(ps.mx, l);
+#pragma unroll
+  for (int t = 0; t < D / 16; ++t) {  // coordinates 16 t + 4 g ..
+    const float y[4] = {ps.o[t][0], ps.o[t][1], ps.o[t][2], ps.o[t][3]};
+    if (n_eff > 1)
+      *reinterpret_cast<float4*>(a.part + rec * D + 16 * t + 4 * g) =
+          make_float4(y[0], y[1], y[2], y[3]);
+    else
+      attend_write<float, D>(a, ps.row, bh, 16 * t + 4 * g, y, ps.mx, l);
+  }
 }
 
 // Joins the records of a tile's splits where the last workgroup does not: 16 / P rows per
@@ -650,20 +781,6 @@ struct alignas(16) TileBuf {
   uint4 k[D * 4];  // a step: 32 D elements
   uint4 v[D * 4];
 };
-
-// 16 bytes per lane from src (per lane) to dst (uniform) + 16 lane, without a
-// register in between; complete when vmcnt has counted it down.
-__device__ __forceinline__ void copy_to_lds(const void* src, void* dst) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src,
-                                   (__attribute__((address_space(3))) uint32_t*)dst, 16, 0, 0);
-}
-
-// Waits for this wavefront's copies to LDS: the builtin, which the compiler counts (it
-// would otherwise wait for them, and for those issued since, at the reads).
-__device__ __forceinline__ void wait_copies() {
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt 0, the other counts open
-  asm volatile("" ::: "memory");
-}
 
 // kCapped: a cap that bounds all scores, no bias; kBiased: no cap, and no prefix; kGeneral:
 // any. (Packed documents, 2 x 4096 tokens of 32 heads: kBiased 148 us, kGeneral 187.)
@@ -984,6 +1101,9 @@ static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
   if (a.rows == kTileRows) {
     if (a.m.d == 64) tile(std::integral_constant<int, 64>{});
     else tile(std::integral_constant<int, 128>{});
+  } else if (a.rows == kRowsRows) {
+    if (a.m.d == 64) go(attend_rows_kernel<64>, attend_join_kernel<float, 64>);
+    else go(attend_rows_kernel<128>, attend_join_kernel<float, 128>);
   } else if (a.m.elem == 4) {
     if (a.m.d == 64) go(attend_stream_kernel<float, 64>, attend_join_kernel<float, 64>);
     else go(attend_stream_kernel<float, 128>, attend_join_kernel<float, 128>);

@@ -430,12 +430,11 @@ SPLA_HD AppendRopeWs append_rope_ws_layout(const Dims& m, int max_new) {
 // ---- exact attention -------------------------------------------------------
 // The query rows of a (sequence, KV head), (position t, head g of the group) =
 // t G + g, in tiles: of 16 rows (the columns of one matrix-core tile; keys and
-// values straight from the cache), or of 128 (through LDS, bf16 only). One
+// values straight from the cache), or by way of LDS of 128 (bf16) or 64 (fp32). One
 // workgroup per tile and split of the keys.
-constexpr int kAttendRows = 16;
-constexpr int kTileRows = 128;
-// Workgroups that share a tile's keys: as many as fill the chip with two tiles of 16 rows
-// per compute unit (32K tokens, bf16 d 128, 8 heads: 64 rows 32.8 us, and 37.2 with three
+constexpr int kAttendRows = 16, kRowsRows = 64, kTileRows = 128;
+// Workgroups that share a tile's keys: as many as fill the chip with two tiles of 16 (or 64)
+// rows per compute unit (32K tokens, bf16 d 128, 8 heads: 64 rows 32.8 us, and 37.2 with three
 // per unit; one too many cost more: 48 rows 30.5 us with 504 workgroups, 38.9 with 528), or
 // three where that would leave them unsplit (264 tiles of 4096 tokens: 116 us, unsplit 125;
 // 400 tiles: 284 unsplit, 313 in two), or three tiles of 128 rows.
@@ -443,9 +442,11 @@ constexpr int kAttendFill = 512;
 constexpr int kTileFill = 768;
 constexpr int kAttendMaxSplit = 128;  // and at most
 // Steps of 32 tokens per workgroup at least: one per wavefront of tiles of 16 rows (8: 13.0 us
-// against 10.5 for 16 rows of 4096 tokens); 16 for 128 rows (1024 rows of 1024 tokens:
-// 29.8 us, with 8 steps 34.7; 256 rows of 8192: 27.6 us, with 32 steps 36.0).
+// against 10.5 for 16 rows of 4096 tokens); 2 for 64 rows of fp32 (256 rows over 1312 tokens,
+// d 128: 28.5 us, with 4 steps 33.2); 16 for 128 rows (1024 rows of 1024 tokens: 29.8 us, with
+// 8 steps 34.7; 256 rows of 8192: 27.6 us, with 32 steps 36.0).
 constexpr int kAttendMinSteps = 4;
+constexpr int kRowsMinSplit = 2;
 constexpr int kTileMinSplit = 16;
 // Records that a tile's last workgroup joins at most: eight per thread, one wait for memory.
 // More go to a launch of their own, which has a thread for every eight records and 16th of a
@@ -453,11 +454,19 @@ constexpr int kTileMinSplit = 16;
 // and 29.3; 96 of 16 rows: 29 and 55).
 constexpr int kJoinInLaunch = 128;
 
-// Tiles of 128 rows from 65 rows on (4096 and 32K tokens, bf16 d 128, 8 heads of 4: 64 rows
-// 12.1 and 32.8 us in tiles of 16, 16.0 and 37.3 in one of 128; 96 rows at 32K tokens 57.5
-// and 35.5 us).
-SPLA_HD bool attend_wide(const Dims& m, int n_tokens) {
-  return m.elem == 2 && (int64_t)n_tokens * m.group > 64;
+// Few rows are bound by the keys' bytes from memory (tiles of 16), many by the products
+// (128), or in fp32 by the operand reads (64). bf16, d 128, 8 heads of 4, 4096 and 32K tokens:
+// 64 rows 12.1 and 32.8 us in tiles of 16, 16.0 and 37.3 in one of 128; 96 rows at 32K tokens
+// 57.5 and 35.5 us. fp32, d 64 and 128, 4 heads of 2, 1312 tokens: 66 rows 12.8 and 17.9 us in
+// tiles of 16, 14.7 and 21.9 in tiles of 64; 128 rows 14.5 and 24.9, 15.0 and 22.8.
+SPLA_HD int attend_min_steps(int rows) {
+  return rows == kAttendRows ? kAttendMinSteps : rows == kTileRows ? kTileMinSplit : kRowsMinSplit;
+}
+
+SPLA_HD int attend_rows(const Dims& m, int n_tokens) {
+  const int64_t rows = (int64_t)n_tokens * m.group;
+  if (m.elem == 2) return rows <= 64 ? kAttendRows : kTileRows;
+  return rows <= 96 ? kAttendRows : kRowsRows;
 }
 
 struct AttendWs {
@@ -477,13 +486,13 @@ struct AttendWs {
 
 SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
   AttendWs w;
-  const bool wide = attend_wide(m, n_tokens);
-  w.rows = wide ? kTileRows : kAttendRows;
+  w.rows = attend_rows(m, n_tokens);
+  const bool wide = w.rows != kAttendRows;
   w.n_tiles = (int)ceil_div((int64_t)n_tokens * m.group, w.rows);
   const int64_t wgs = (int64_t)m.bh * w.n_tiles;
   int64_t n = 1;
-  if (wgs > 0) n = !wide && kAttendFill / wgs > 1 ? kAttendFill / wgs : kTileFill / wgs;
-  const int64_t most = ceil_div(m.cap, (wide ? kTileMinSplit : kAttendMinSteps) * kSubTokens);
+  if (wgs > 0) n = w.rows != kTileRows && kAttendFill / wgs > 1 ? kAttendFill / wgs : kTileFill / wgs;
+  const int64_t most = ceil_div(m.cap, attend_min_steps(w.rows) * kSubTokens);
   n = n < most ? n : most;
   n = n < kAttendMaxSplit ? n : kAttendMaxSplit;
   w.n_split = (int)(n > 1 ? n : 1);

@@ -70,6 +70,8 @@ CASES = {
     "splits": ("bf16", 128, 8, 2, 64, [3001, 0, 5, 129], 4, True),
     "splits_rows_48": ("bf16", 64, 8, 2, 32, [2500, 40], 12, False),
     "splits_rows_96": ("bf16", 128, 8, 2, 64, [6100, 300], 24, False),
+    "f32_rows": ("f32", 64, 8, 2, 32, [1000, 333, 40], 50, True),
+    "f32_rows_splits": ("f32", 128, 8, 2, 64, [2501, 0, 90], 25, False),
     "f32_splits": ("f32", 128, 4, 2, 64, [2800, 1, 70], 8, True),
 }
 KINDS = ["causal", "softcap", "bias", "docs", "prefix", "ragged", "all"]
@@ -127,7 +129,7 @@ def test_scale_and_three_dimensions(dev):
 
 
 @pytest.mark.parametrize("softcap", [2.0 ** -10, 41.0, 42.0, 1024.0])
-@pytest.mark.parametrize("dtype,T", [("bf16", 9), ("bf16", 100), ("f32", 9)])
+@pytest.mark.parametrize("dtype,T", [("bf16", 9), ("bf16", 100), ("f32", 9), ("f32", 40)])
 def test_caps(dev, dtype, T, softcap):
     """The smallest and the largest cap, and those on the two sides of the one up to which
     weights need no maximum; scores up to a few hundred."""
@@ -141,7 +143,7 @@ def test_caps(dev, dtype, T, softcap):
 
 @pytest.mark.parametrize("size", [2.0 ** 70, 2.0 ** -30])
 @pytest.mark.parametrize("softcap", [0.0, 41.0, 42.0])
-@pytest.mark.parametrize("dtype,T", [("bf16", 9), ("bf16", 100), ("f32", 9)])
+@pytest.mark.parametrize("dtype,T", [("bf16", 9), ("bf16", 100), ("f32", 9), ("f32", 40)])
 def test_large_and_small_values(dev, dtype, T, softcap, size):
     """Queries against the keys' mean direction: scores at both ends of the cap."""
     cache, K, V = filled(dev, dtype, [400, 333], 8, 2, 128, 64)

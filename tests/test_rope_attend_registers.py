@@ -13,6 +13,7 @@ from test_kernel_registers import kernels  # noqa: F401  (the fixture)
     (r"append_rope_one_kernel<", 4, 64),
     (r"append_fused_kernel<128, (true|false)>", 2, 256),
     (r"attend_stream_kernel<", 4, 256),
+    (r"attend_rows_kernel<", 2, 256),
     (r"attend_tile_kernel<\d+, \d>", 8, 168),
     (r"attend_join_kernel<", 4, 128),
 ])
