@@ -521,7 +521,11 @@ int32_t spla_append_rope(const spla_config* cfg, const spla_cache* cache, const 
  *  workspace: device, at least spla_attend_workspace_bytes(cfg, n_tokens),
  *        256-byte aligned, zero-filled before its first use.
  * Keys and values that a query does not see do not change its result, whatever
- * they hold (infinities and NaN included). Sums and softmax statistics are fp32;
+ * they hold (infinities and NaN included). Finite values of magnitudes up to 2^97
+ * (2^75 with a softcap below 42) keep every sum finite: weights times values are
+ * summed before they are divided by the weights' sum. A weight below 2^-126 of its
+ * query's largest counts as zero (zero times an infinity, too: NaN or that infinity).
+ * Sums and softmax statistics are fp32;
  * for bf16 caches the weights e^(x_j - m) are rounded to bf16 before the product
  * with the values. Reads the K/V rows, seq_lens and the block table of the cache;
  * top_k, the statistics and the linear state play no part. The cache is only

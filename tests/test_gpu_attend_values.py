@@ -1,0 +1,91 @@
+"""Exact attention at the ends of the value range, and the precision of capped scores, on the
+GPU against the 64-bit form."""
+
+import math
+
+import pytest
+import torch
+
+import rope_attend_ref as R
+from paper_2601_22379_amd import spla
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    spla.lib()
+    return torch.device("cuda:0")
+
+
+def randn(dev, dtype, *shape, seed=0, scale=1.0):
+    g = torch.Generator(device=dev)
+    g.manual_seed(seed)
+    return (torch.randn(shape, generator=g, device=dev) * scale).to(DT[dtype])
+
+
+def held(dev, dtype, K, V, cap, hq):
+    """A cache with softmax_scale 1 that holds K, V [b, hkv, L, d]."""
+    b, hkv, L, d = K.shape
+    cfg = spla.make_config(b, hq, hkv, d, 32, 2, cap, dtype, n_sink=0, n_local=0,
+                           softmax_scale=1.0)
+    cache = spla.SplaCache(cfg, dev)
+    cache.append(K, V)
+    return cache
+
+
+# 16 heads on one KV head. Tiles of 16 rows: the four wavefronts' joint, the last workgroup's
+# join of 8 splits, the join in a launch of its own (32 splits); many rows: unsplit and split.
+FORMS = [("bf16", 1, 100, 128), ("bf16", 1, 1000, 1024), ("bf16", 1, 4000, 4096),
+         ("bf16", 7, 500, 512), ("bf16", 7, 4000, 4096),
+         ("f32", 1, 100, 128), ("f32", 1, 1000, 1024), ("f32", 1, 4000, 4096),
+         ("f32", 7, 50, 64), ("f32", 7, 1000, 1024)]
+
+
+@pytest.mark.parametrize("last", [True, False])
+@pytest.mark.parametrize("kind", ["plain", "bias", "cap"])
+@pytest.mark.parametrize("form", FORMS, ids=lambda f: "-".join(map(str, f)))
+def test_large_values_of_vanishing_weight(dev, form, kind, last):
+    """Keys whose scores lie more than 126 bits under the highest, with values of 2^97, beside
+    values of 2^-30 at the highest scores (seen last, or first): what the former add is below
+    2^97 e^-120 = 2^-76, and the outputs are the mean of the latter."""
+    dtype, T, L, cap = form
+    K = torch.zeros(1, 1, L, 128, dtype=DT[dtype], device=dev)
+    V = randn(dev, dtype, 1, 1, L, 128, seed=1)
+    top = torch.zeros(L, dtype=torch.bool, device=dev)
+    top[L - T - 3 if last else 0:L if last else 5] = True
+    K[0, 0, top, 0] = 140.0
+    V *= torch.where(top, 2.0 ** -30, 2.0 ** 95)[:, None].to(DT[dtype])
+    cache = held(dev, dtype, K, V, cap, 16)
+    q = torch.zeros(T, 1, 16, 128, dtype=DT[dtype], device=dev)
+    q[..., 0] = 1.0
+    kw = {}
+    if kind == "bias":
+        kw["slopes"] = torch.linspace(0.0, 2.0 ** -10, 16, device=dev)
+    if kind == "cap":
+        kw["softcap"] = 200.0
+    out, lse = cache.attend(q, **kw)
+    R.check_attend(out, lse, q, K, V, [L], scale=1.0, cap_series=True, **kw)
+    assert float(out.abs().max()) < 2.0 ** -26
+
+
+@pytest.mark.parametrize("softcap,size", [(0.0, 2.0 ** 95), (42.0, 2.0 ** 95), (41.0, 2.0 ** 73),
+                                          (5.0, 2.0 ** 73)])
+@pytest.mark.parametrize("form", FORMS, ids=lambda f: "-".join(map(str, f)))
+def test_largest_values(dev, form, softcap, size):
+    """Values up to the documented 2^97 (2^75 with a small cap) leave every sum finite."""
+    dtype, T, L, cap = form
+    K, V = randn(dev, dtype, 1, 1, L, 128, seed=2), randn(dev, dtype, 1, 1, L, 128, seed=3)
+    K[..., 0] = 8.0
+    V = V.abs() * size
+    cache = held(dev, dtype, K, V, cap, 16)
+    q = randn(dev, dtype, T, 1, 16, 128, seed=4)
+    q[..., 0] = 40.0  # scores at the upper end of the cap
+    out, lse = cache.attend(q, softcap=softcap)
+    assert bool(torch.isfinite(out).all())
+    R.check_attend(out, lse, q, K, V, [L], scale=1.0, softcap=softcap,
+                   cap_series=dtype == "f32" or T == 1)
