@@ -525,6 +525,7 @@ int32_t spla_append_rope(const spla_config* cfg, const spla_cache* cache, const 
  * (2^75 with a softcap below 42) keep every sum finite: weights times values are
  * summed before they are divided by the weights' sum. A weight below 2^-126 of its
  * query's largest counts as zero (zero times an infinity, too: NaN or that infinity).
+ * A capped score is off by c 2^-21 at most, for c above 64 also by 2^-18 of itself.
  * Sums and softmax statistics are fp32;
  * for bf16 caches the weights e^(x_j - m) are rounded to bf16 before the product
  * with the values. Reads the K/V rows, seq_lens and the block table of the cache;

@@ -119,10 +119,18 @@ __device__ __forceinline__ int64_t attend_q_at(const AttendArgs& a, int64_t r, i
          a.m.d;
 }
 
+// c log2 e tanh(x ln 2 / 2), cap2 = c log2 e. tanh y = 1 - 2 / (e^2y + 1): off by 2^-21 at most,
+// and 1 (-1) where e^2y overflows (vanishes); below 1/4, where that would cost the score's own
+// bits under a large cap, by its series (the first term left out is below 2^-24 of the sum).
+__device__ __forceinline__ float cap_score(float x, float cap2) {
+  const float y = x * (0.5f * kLn2), u = y * y;
+  const float low = y * fmaf(u, fmaf(u, fmaf(u, fmaf(u, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f),
+                                     -1.f / 3.f), 1.f);
+  const float high = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x) + 1.f), 1.f);
+  return cap2 * (fabsf(y) < 0.25f ? low : high);
+}
+
 // Score of a raw product, in base 2: x log2 e with x = cap(s dot) - slope |p - j|.
-// tanh y = 1 - 2 / (e^2y + 1): off by 2^-21 at most, and 1 (-1) where e^2y overflows
-// (vanishes); below 1/4, where that would cost the score's own bits under a large cap, by its
-// series (the first term left out is below 2^-24 of the sum).
 struct ScoreMap {
   float mul, cap2, slope2;  // cap: dot -> 2 log2 e s / c dot; cap2 = c log2 e (0: none)
   __device__ __forceinline__ ScoreMap(const AttendArgs& a, int head) {
@@ -133,13 +141,7 @@ struct ScoreMap {
   }
   __device__ __forceinline__ float operator()(float dot, int dist) const {
     float x = dot * mul;
-    if (cap2 > 0.f) {
-      const float y = x * (0.5f * kLn2), u = y * y;
-      const float low = y * fmaf(u, fmaf(u, fmaf(u, fmaf(u, 62.f / 2835.f, -17.f / 315.f),
-                                                2.f / 15.f), -1.f / 3.f), 1.f);
-      const float high = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x) + 1.f), 1.f);
-      x = cap2 * (fabsf(y) < 0.25f ? low : high);
-    }
+    if (cap2 > 0.f) x = cap_score(x, cap2);
     return fmaf(-slope2, (float)dist, x);
   }
 };
@@ -812,6 +814,10 @@ struct alignas(16) TileBuf {
 // any. (Packed documents, 2 x 4096 tokens of 32 heads: kBiased 148 us, kGeneral 187.)
 enum { kPlain = 0, kCapped = 1, kBiased = 2, kGeneral = 3 };
 
+// Up to this cap, scores of many rows do without the series of cap_score (1024 queries of 4
+// heads on each of 8 KV heads, 8000 tokens: 202 us without, 249 with it).
+constexpr float kSeriesCap = 64.f;
+
 template <int D, int KIND>
 struct TilePass {
   static constexpr int KS = D / 16, CT = D / 32;
@@ -821,9 +827,8 @@ struct TilePass {
   int pos, lo, hi;    // this column's query
   float mul, cap2, slope2;
 
-  // c log2 e tanh(z / 2) of a product z scaled to 2 log2 e / c (see ScoreMap; kCapped: less
-  // the reference): within c 2^-21 without the series, 2^-11 for the largest cap, against
-  // weights rounded to 2^-9
+  // cap_score without its series (kCapped: less the reference), for caps up to kSeriesCap: off
+  // by c 2^-21, 2^-15 at most
   __device__ __forceinline__ float capped(float z) const {
     return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z) + 1.f),
                 KIND == kCapped ? 0.5f * cap2 : cap2);
@@ -855,7 +860,8 @@ struct TilePass {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         float y = x[i] * mul;
-        if (cap2 > 0.f) y = capped(y);
+        if (cap2 > kSeriesCap * kLog2e) y = cap_score(y, cap2);
+        else if (cap2 > 0.f) y = capped(y);
         x[i] = fmaf(-slope2, fabsf(base - (float)token(i)), y);
       }
     }

@@ -89,3 +89,36 @@ def test_largest_values(dev, form, softcap, size):
     assert bool(torch.isfinite(out).all())
     R.check_attend(out, lse, q, K, V, [L], scale=1.0, softcap=softcap,
                    cap_series=dtype == "f32" or T == 1)
+
+
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("softcap", [20.0, 64.0, 65.0, 200.0, 1024.0])
+@pytest.mark.parametrize("form", [("bf16", 1), ("bf16", 40), ("f32", 1), ("f32", 40)],
+                         ids=lambda f: "-".join(map(str, f)))
+def test_capped_scores(dev, form, softcap, bias):
+    """Queries that see one key each (products of one coordinate: exact): the log-sum-exp is the
+    capped score, off by c 2^-21 at most, for caps above 64 also by 2^-18 of itself, and four
+    fp32 roundings. The bias of a query's own position is none."""
+    dtype, T = form
+    L = 300
+    K = torch.zeros(1, 1, L, 128, dtype=DT[dtype], device=dev)
+    size = torch.exp2(torch.linspace(-12.0, 1.0, L, device=dev)) * softcap
+    K[0, 0, :, 0] = (size * randn(dev, "f32", L, seed=6)).to(DT[dtype])
+    K = K[:, :, torch.randperm(L, generator=torch.Generator().manual_seed(7)).to(dev)].contiguous()
+    V = randn(dev, dtype, 1, 1, L, 128, seed=8)
+    cache = held(dev, dtype, K, V, 320, 16)
+    q = torch.zeros(T, 1, 16, 128, dtype=DT[dtype], device=dev)
+    q[..., 0] = 1.0
+    pos = torch.arange(L - T, L, device=dev)
+    kw = dict(slopes=torch.linspace(0.5, 2.0, 16, device=dev)) if bias else {}
+    out, lse = cache.attend(q, softcap=softcap, first_key=pos.int()[:, None].contiguous(), **kw)
+    want = softcap * torch.tanh(K[0, 0, pos, 0].double() / softcap)[:, None, None]
+    tol = torch.full_like(want, softcap * 2.0 ** -21)
+    if softcap > 64.0:
+        tol = torch.minimum(tol, want.abs() * 2.0 ** -18)
+    tol = tol + want.abs() * 2.0 ** -22
+    assert bool(((lse.double() - want).abs() <= tol).all()), float(
+        ((lse.double() - want).abs() / tol).max())
+    # (in bf16 the weight, e to a difference of references, may be rounded beside the output)
+    v = V[0, 0, pos][:, None, None].double()
+    assert bool(((out.double() - v).abs() <= v.abs() * 2.01 * 2.0 ** -8).all())
