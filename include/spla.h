@@ -527,8 +527,9 @@ int32_t spla_append_rope(const spla_config* cfg, const spla_cache* cache, const 
  * query's largest counts as zero (zero times an infinity, too: NaN or that infinity).
  * A capped score is off by c 2^-21 at most, for c above 64 also by 2^-18 of itself.
  * Sums and softmax statistics are fp32;
- * for bf16 caches the weights e^(x_j - m) are rounded to bf16 before the product
- * with the values. Reads the K/V rows, seq_lens and the block table of the cache;
+ * for bf16 caches the weights e^(x_j - m) are rounded before the product with the
+ * values: to 16 bits where a KV head has up to 64 query rows (n_tokens Hq / Hkv), to
+ * bf16 where it has more. Reads the K/V rows, seq_lens and the block table of the cache;
  * top_k, the statistics and the linear state play no part. The cache is only
  * read. n_tokens = 0 does nothing. */
 int32_t spla_attend(const spla_config* cfg, const spla_cache* cache, int32_t n_tokens,

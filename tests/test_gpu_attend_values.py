@@ -122,3 +122,41 @@ def test_capped_scores(dev, form, softcap, bias):
     # (in bf16 the weight, e to a difference of references, may be rounded beside the output)
     v = V[0, 0, pos][:, None, None].double()
     assert bool(((out.double() - v).abs() <= v.abs() * 2.01 * 2.0 ** -8).all())
+
+
+@pytest.mark.parametrize("kind", ["plain", "bias", "cap", "prefix"])
+@pytest.mark.parametrize("T,L,cap", [(1, 100, 128), (2, 1000, 1024), (4, 4000, 4096), (4, 37, 64)])
+def test_weights_of_few_rows(dev, T, L, cap, kind):
+    """bf16 values that cancel in pairs, so that the rounding of a weight shows: weights of few
+    rows are products of two bf16 terms, off by 2^-16."""
+    K, V = randn(dev, "bf16", 1, 1, L, 128, seed=11), randn(dev, "bf16", 1, 1, L, 128, seed=12)
+    q = randn(dev, "bf16", 1, 1, 16, 128, seed=13, scale=0.1).expand(T, 1, 16, 128).contiguous()
+    kw, prefix = {}, 0
+    if kind == "bias":
+        kw["slopes"] = torch.full((16,), 2.0 ** -8, device=dev)
+    if kind == "cap":
+        kw["softcap"] = 3.0
+    if kind == "prefix":
+        prefix = L
+    dot = q[0, 0, 0].double() @ K[0, 0].double().t()
+    x = 3.0 * torch.tanh(dot / 3.0) if kind == "cap" else dot
+    if kind == "bias":  # relative to any position after both
+        x = x + torch.arange(L, device=dev) * 2.0 ** -8
+    n = L // 2 * 2
+    V[0, 0, 1:n:2] = (-V[0, 0, 0:n:2].double() * torch.exp(x[0:n:2] - x[1:n:2])[:, None]).bfloat16()
+    cache = held(dev, "bf16", K, V, cap, 16)
+    q[:, :, 1:] = q[:, :, :1]
+    pre = torch.tensor([L], dtype=torch.int32, device=dev) if prefix else None
+    out, lse = cache.attend(q, prefix_len=pre, **kw)
+    pos, lo, hi = (t.to(dev) for t in R.visible(L, T, T, None, prefix))
+    slope = float(kw["slopes"][0]) if kind == "bias" else 0.0
+    ref, rl, tol, lt = R.attention(q[:, 0, 0], K[0, 0], V[0, 0], pos, 1.0, kw.get("softcap", 0.0),
+                                   slope, lo, hi, True)
+    j = torch.arange(L, device=dev)
+    xs = x[None] - (slope * pos[:, None] if slope else 0.0)
+    p = torch.exp(xs - rl[:, None]) * ((j >= lo[:, None]) & (j < hi[:, None]))
+    pv = p @ V[0, 0].double().abs()
+    tol = tol - pv * 2.0 ** -8 + pv * 2.0 ** -16
+    for m in range(16):
+        err = (out[:, 0, m].double() - ref).abs()
+        assert bool((err <= tol).all()), (m, float((err / tol).max()))
