@@ -407,7 +407,7 @@ class SplaCache:
         self._prefill_ws = None
         self._rope_ws = None
         self._attend_ws = None
-        self._outgrown = []  # workspaces that captured graphs may still name
+        self._outgrown = []  # workspaces that captured graphs name
         self._ws_sizes = {}
         self._struct = SplaCacheStruct(self.k.data_ptr(), self.v.data_ptr(),
                                        self.stats.data_ptr(), self.state.data_ptr(),
@@ -542,17 +542,24 @@ class SplaCache:
 
     def _workspace(self, kind, n, sizes, ws):
         """The workspace ws, or a larger one in its place (zeros: its counters), for a call of
-        n tokens; the sizes of earlier calls are remembered."""
+        n tokens; the sizes of earlier calls are remembered. It grows by half at least, so that
+        calls that get longer one by one seldom make a new one, and one that a capture has used
+        is kept."""
         need = self._ws_sizes.get((kind, n))
         if need is None:
             need = self._ws_sizes[kind, n] = sizes(self.cfg, n)
+        capturing = torch.cuda.is_current_stream_capturing()
         if ws is None or ws.numel() < need:
-            if torch.cuda.is_current_stream_capturing():  # its zeros would come with a replay only
+            if capturing:  # its zeros would come with a replay only
                 raise RuntimeError("a capture needs a call of its sizes ahead of it, which makes "
                                    "the workspace")
             if ws is not None:
-                self._outgrown.append(ws)
+                need = max(need, ws.numel() * 3 // 2)
+                if ws.is_cuda:  # calls on this stream, not its own, may still use it
+                    ws.record_stream(torch.cuda.current_stream(ws.device))
             ws = _aligned_workspace(need, self.device).zero_()
+        elif capturing and not any(ws is kept for kept in self._outgrown):
+            self._outgrown.append(ws)
         return ws
 
     def _given(self, name, t, shape, dtype):

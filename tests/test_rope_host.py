@@ -180,3 +180,41 @@ def test_a_workspace_does_not_grow_in_a_capture(monkeypatch):
         cache._workspace("rope", 1, sizes, None)
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     assert cache._workspace("attend", 5, sizes, ws).numel() >= 1280 and cache._outgrown[0] is ws
+
+
+def _growing(monkeypatch, capturing):
+    """A cache's workspaces on the CPU: (cache, sizes) with 256 bytes per token."""
+    cache = object.__new__(spla.SplaCache)
+    cache.cfg, cache.device = _cfg(), torch.device("cpu")
+    cache._ws_sizes, cache._outgrown = {}, []
+    monkeypatch.setattr(spla, "_aligned_workspace",
+                        lambda n, device: torch.empty(n, dtype=torch.uint8))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    return cache, lambda cfg, n: 256 * n
+
+
+def test_outgrown_workspaces_are_let_go(monkeypatch):
+    """Prompts that get longer one by one: one workspace is kept, of at most half as much again
+    as the largest call needs, made anew a few times only."""
+    cache, sizes = _growing(monkeypatch, [False])
+    ws, made = None, 0
+    for n in range(1, 400):
+        new = cache._workspace("rope", n, sizes, ws)
+        made, ws = made + (new is not ws), new
+        assert 256 * n <= ws.numel() <= 256 * n * 3 // 2
+    assert cache._outgrown == [] and made <= 18  # log(400) / log(1.5), and the first small ones
+
+
+def test_captured_workspaces_are_kept(monkeypatch):
+    """A graph names the workspace of its capture: that one stays, the others do not."""
+    on = [False]
+    cache, sizes = _growing(monkeypatch, on)
+    ws = cache._workspace("rope", 4, sizes, None)
+    on[0] = True
+    assert cache._workspace("rope", 4, sizes, ws) is ws
+    assert cache._workspace("rope", 3, sizes, ws) is ws
+    on[0] = False
+    big = cache._workspace("rope", 100, sizes, ws)
+    bigger = cache._workspace("rope", 1000, sizes, big)
+    assert bigger is not big is not ws
+    assert len(cache._outgrown) == 1 and cache._outgrown[0] is ws
