@@ -328,11 +328,17 @@ int32_t spla_prefill_workspace_bytes(const spla_config* cfg, int32_t n_tokens,
 int32_t spla_rope_init(const spla_rope_config* cfg, spla_rope* out);
 
 /* Device workspace that spla_append_rope needs for up to max_new tokens per
- * sequence (host-only query). Zero-fill it once before its first use, or after
- * other data was in it: its first bytes are counters, which must be zero when a
- * call starts and which every call leaves zero. */
+ * sequence, whatever the rotation (host-only query). Zero-fill it once before its
+ * first use, or after other data was in it: its first bytes are counters, which must
+ * be zero when a call starts and which every call leaves zero. */
 int32_t spla_append_rope_workspace_bytes(const spla_config* cfg, int32_t max_new,
                                          size_t* out_bytes);
+
+/* The same for one rotation (NULL: any): less by the rotated keys, max_new rows per
+ * (sequence, KV head), where they need not pass through memory (bf16, head_dim 128, no
+ * selection windows, a rot_dim that is a multiple of 16). */
+int32_t spla_append_rope_workspace_bytes_ex(const spla_config* cfg, const spla_rope* rope,
+                                            int32_t max_new, size_t* out_bytes);
 
 /* Device workspace that spla_attend needs for n_tokens queries per sequence
  * (host-only query): arrival counters and the partial results of sequences whose
@@ -497,8 +503,8 @@ int32_t spla_rotate(const spla_config* cfg, const spla_rope* rope, int32_t n_tok
  *              give the rotary position (a sequence whose oldest tokens were
  *              dropped, or that begins in the middle of a text).
  * The other arguments as spla_append; the workspace from
- * spla_append_rope_workspace_bytes, zero-filled before its first use. Queries of
- * the same tokens: spla_rotate. */
+ * spla_append_rope_workspace_bytes (or _ex with this rotation), zero-filled before its
+ * first use. Queries of the same tokens: spla_rotate. */
 int32_t spla_append_rope(const spla_config* cfg, const spla_cache* cache, const spla_rope* rope,
                          const void* k_new, const void* v_new, int32_t max_new,
                          const int32_t* n_new, const int32_t* pos_shift, void* workspace,

@@ -1306,8 +1306,6 @@ hipError_t launch_block_states(const Dims& m, const spla_cache& c, const void* k
   return hipGetLastError();
 }
 
-bool append_fusable(const Dims& m) { return m.elem == 2 && m.d == 128 && !windowed(m); }
-
 hipError_t launch_append_fused(const Dims& m, const spla_cache& c, const void* k_new,
                                const void* v_new, int max_new, const int32_t* n_new,
                                const AppendWs& ws, char* base, hipStream_t st,

@@ -292,15 +292,6 @@ extern "C" int32_t spla_prefill(const spla_config* cfg, const spla_cache* cache,
 // ---- rotary positions and exact attention ------------------------------------
 namespace {
 
-int32_t check_rope(const spla_config* cfg, const spla_rope* r) {
-  if (!r || r->head_dim != cfg->head_dim) return SPLA_ERR_INVALID_ARG;
-  if (r->rot_dim < 2 || r->rot_dim > r->head_dim || r->rot_dim % 2 != 0)
-    return SPLA_ERR_INVALID_ARG;
-  if (r->layout != SPLA_ROPE_HALF && r->layout != SPLA_ROPE_INTERLEAVED)
-    return SPLA_ERR_INVALID_ARG;
-  return SPLA_OK;
-}
-
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 // rows of `heads` heads at a stride of `stride` elements
@@ -317,7 +308,7 @@ extern "C" int32_t spla_rotate(const spla_config* cfg, const spla_rope* rope, in
                                int32_t transpose, void* stream) {
   int32_t s = spla_validate(cfg);
   if (s != SPLA_OK) return s;
-  if ((s = check_rope(cfg, rope)) != SPLA_OK) return s;
+  if ((s = spla::check_rope(*cfg, rope)) != SPLA_OK) return s;
   if (n_tokens < 0 || (transpose != 0 && transpose != 1)) return SPLA_ERR_INVALID_ARG;
   if (n_tokens == 0) return SPLA_OK;
   if ((!q && !k) || (q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr))
@@ -349,13 +340,13 @@ extern "C" int32_t spla_append_rope(const spla_config* cfg, const spla_cache* ca
   int32_t s = spla_validate(cfg);
   if (s != SPLA_OK) return s;
   if ((s = check_cache(cfg, cache)) != SPLA_OK) return s;
-  if ((s = check_rope(cfg, rope)) != SPLA_OK) return s;
+  if ((s = spla::check_rope(*cfg, rope)) != SPLA_OK) return s;
   if (max_new < 0) return SPLA_ERR_INVALID_ARG;
   if (max_new > cfg->max_seq_len) return SPLA_ERR_CAPACITY;
   if (max_new == 0) return SPLA_OK;
   if (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new)) return SPLA_ERR_INVALID_ARG;
   const Dims m = spla::make_dims(*cfg);
-  const spla::AppendRopeWs L = spla::append_rope_ws_layout(m, max_new);
+  const spla::AppendRopeWs L = spla::append_rope_ws_layout(m, max_new, rope->rot_dim);
   if ((s = check_ws(workspace, workspace_bytes, (size_t)L.total)) != SPLA_OK) return s;
   char* ws = static_cast<char*>(workspace);
   if (max_new == 1) {
@@ -367,9 +358,7 @@ extern "C" int32_t spla_append_rope(const spla_config* cfg, const spla_cache* ca
   hipStream_t st = static_cast<hipStream_t>(stream);
   const spla::AppendWs A = spla::append_ws_layout(m, max_new);
   const bool one_pass = spla::append_fusable(m);
-  // in the registers of the one pass where pieces of 8 coordinates hold whole pairs (16384
-  // tokens of 4 x 8 units: 169 us, plain append 143), else into the workspace first (330)
-  if (one_pass && rope->rot_dim % 16 == 0) {
+  if (spla::append_rotates(m, rope->rot_dim)) {
     SPLA_TRY(spla::launch_append_fused(m, *cache, k_new, v_new, max_new, n_new, A, ws + L.append,
                                        st, rope, pos_shift));
     return SPLA_OK;

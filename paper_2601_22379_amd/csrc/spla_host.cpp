@@ -169,15 +169,22 @@ extern "C" int32_t spla_rope_init(const spla_rope_config* c, spla_rope* out) {
   return SPLA_OK;
 }
 
-extern "C" int32_t spla_append_rope_workspace_bytes(const spla_config* c, int32_t max_new,
-                                                    size_t* out) {
+extern "C" int32_t spla_append_rope_workspace_bytes_ex(const spla_config* c, const spla_rope* rope,
+                                                       int32_t max_new, size_t* out) {
   if (!out) return SPLA_ERR_INVALID_ARG;
   int32_t st = spla_validate(c);
   if (st != SPLA_OK) return st;
+  if (rope && (st = spla::check_rope(*c, rope)) != SPLA_OK) return st;
   if (max_new < 0) return SPLA_ERR_INVALID_ARG;
   if (max_new > c->max_seq_len) return SPLA_ERR_CAPACITY;
-  *out = (size_t)spla::append_rope_ws_layout(spla::make_dims(*c), max_new).total;
+  const int rot_dim = rope ? rope->rot_dim : 2;  // 2: one that needs the most
+  *out = (size_t)spla::append_rope_ws_layout(spla::make_dims(*c), max_new, rot_dim).total;
   return SPLA_OK;
+}
+
+extern "C" int32_t spla_append_rope_workspace_bytes(const spla_config* c, int32_t max_new,
+                                                    size_t* out) {
+  return spla_append_rope_workspace_bytes_ex(c, nullptr, max_new, out);
 }
 
 extern "C" int32_t spla_attend_workspace_bytes(const spla_config* c, int32_t n_tokens,

@@ -405,26 +405,44 @@ SPLA_HD AppendWs append_ws_layout(const Dims& m, int max_new) {
   return w;
 }
 
+// The bulk appends that run in one pass over the new rows.
+SPLA_HD bool append_fusable(const Dims& m) { return m.elem == 2 && m.d == 128 && !windowed(m); }
+// Those that rotate rot_dim coordinates in that pass's registers, where pieces of 8 coordinates
+// hold whole pairs (16384 tokens of 4 x 8 units: 169 us, plain append 143); others rotate into
+// the workspace first (330).
+SPLA_HD bool append_rotates(const Dims& m, int rot_dim) {
+  return append_fusable(m) && rot_dim % 16 == 0;
+}
+
 // The rotating append: the counters of its single-token form (zero between calls of
-// any length), the rotated keys, then the append's own workspace.
+// any length), the append's own workspace, then the rotated keys where they pass through it.
 struct AppendRopeWs {
   int64_t count;   // i32 [batch][kSyncLine]
-  int64_t k_rot;   // dtype [bh][max_new][d]
   int64_t append;  // AppendWs
+  int64_t k_rot;   // dtype [bh][max_new][d], or nothing (append_rotates)
   int64_t total;
 };
 
-SPLA_HD AppendRopeWs append_rope_ws_layout(const Dims& m, int max_new) {
+SPLA_HD AppendRopeWs append_rope_ws_layout(const Dims& m, int max_new, int rot_dim) {
   AppendRopeWs w;
   w.count = 0;
-  w.k_rot = align_up((int64_t)m.batch * kSyncLine * 4, SPLA_WORKSPACE_ALIGN);
-  if (max_new <= 1) {
-    w.append = w.total = w.k_rot;
-    return w;
-  }
-  w.append = w.k_rot + align_up((int64_t)m.bh * max_new * m.d * m.elem, SPLA_WORKSPACE_ALIGN);
-  w.total = w.append + append_ws_layout(m, max_new).total;
+  w.append = align_up((int64_t)m.batch * kSyncLine * 4, SPLA_WORKSPACE_ALIGN);
+  w.k_rot = w.total = w.append;
+  if (max_new <= 1) return w;
+  w.k_rot = w.total = w.append + append_ws_layout(m, max_new).total;
+  if (!append_rotates(m, rot_dim))
+    w.total += align_up((int64_t)m.bh * max_new * m.d * m.elem, SPLA_WORKSPACE_ALIGN);
   return w;
+}
+
+// Whether a rotation is one of spla_rope_init's for this head size.
+inline int32_t check_rope(const spla_config& c, const spla_rope* r) {
+  if (!r || r->head_dim != c.head_dim) return SPLA_ERR_INVALID_ARG;
+  if (r->rot_dim < 2 || r->rot_dim > r->head_dim || r->rot_dim % 2 != 0)
+    return SPLA_ERR_INVALID_ARG;
+  if (r->layout != SPLA_ROPE_HALF && r->layout != SPLA_ROPE_INTERLEAVED)
+    return SPLA_ERR_INVALID_ARG;
+  return SPLA_OK;
 }
 
 // ---- exact attention -------------------------------------------------------

@@ -39,7 +39,8 @@ STATUS = {0: "ok", -1: "invalid argument", -2: "unsupported shape",
 HOST_EXPORTS = ["spla_status_string", "spla_phase_name", "spla_validate", "spla_cache_bytes",
                 "spla_workspace_bytes", "spla_append_workspace_bytes", "spla_decode_phase_mask",
                 "spla_prefill_workspace_bytes", "spla_rope_init",
-                "spla_append_rope_workspace_bytes", "spla_attend_workspace_bytes"]
+                "spla_append_rope_workspace_bytes", "spla_append_rope_workspace_bytes_ex",
+                "spla_attend_workspace_bytes"]
 EXPORTS = HOST_EXPORTS + ["spla_workspace_init", "spla_reset", "spla_append", "spla_decode",
                           "spla_decode_ex", "spla_step", "spla_step_ex", "spla_prefill",
                           "spla_prefill_ex", "spla_decode_noalloc", "spla_rotate",
@@ -111,6 +112,9 @@ def _declare(lib, host_only=False):
     lib.spla_rope_init.argtypes = [POINTER(SplaRopeConfig), POINTER(SplaRope)]
     lib.spla_append_rope_workspace_bytes.restype = c_int32
     lib.spla_append_rope_workspace_bytes.argtypes = [cfgp, c_int32, POINTER(c_size_t)]
+    lib.spla_append_rope_workspace_bytes_ex.restype = c_int32
+    lib.spla_append_rope_workspace_bytes_ex.argtypes = [cfgp, POINTER(SplaRope), c_int32,
+                                                        POINTER(c_size_t)]
     lib.spla_attend_workspace_bytes.restype = c_int32
     lib.spla_attend_workspace_bytes.argtypes = [cfgp, c_int32, POINTER(c_size_t)]
     if host_only:
@@ -230,11 +234,12 @@ def prefill_workspace_bytes(cfg: SplaConfig, n_tokens: int, library=None) -> int
     return int(n.value)
 
 
-def append_rope_workspace_bytes(cfg: SplaConfig, max_new: int, library=None) -> int:
+def append_rope_workspace_bytes(cfg: SplaConfig, max_new: int, library=None, rope=None) -> int:
+    """For one rotation, or (None) whatever the rotation."""
     n = c_size_t(0)
-    _check((library or lib()).spla_append_rope_workspace_bytes(ctypes.byref(cfg), int(max_new),
-                                                               ctypes.byref(n)),
-           "spla_append_rope_workspace_bytes")
+    _check((library or lib()).spla_append_rope_workspace_bytes_ex(
+        ctypes.byref(cfg), None if rope is None else ctypes.byref(rope), int(max_new),
+        ctypes.byref(n)), "spla_append_rope_workspace_bytes")
     return int(n.value)
 
 
@@ -593,8 +598,9 @@ class SplaCache:
         np_ = None if n_new is None else self._given("n_new", n_new, (c.batch,), torch.int32)
         sp = (None if pos_shift is None
               else self._given("pos_shift", pos_shift, (c.batch,), torch.int32))
-        ws = self._rope_ws = self._workspace("rope", max_new, append_rope_workspace_bytes,
-                                             self._rope_ws)
+        ws = self._rope_ws = self._workspace(
+            ("rope", rope.head_dim, rope.rot_dim), max_new,
+            lambda cfg, n: append_rope_workspace_bytes(cfg, n, rope=rope), self._rope_ws)
         _launch(lib().spla_append_rope, "spla_append_rope", self.device,
                 (ctypes.byref(c), ctypes.byref(self._struct), ctypes.byref(rope), kp, vp, max_new,
                  np_, sp, ws.data_ptr(), ws.numel()))

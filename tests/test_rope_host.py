@@ -218,3 +218,23 @@ def test_captured_workspaces_are_kept(monkeypatch):
     bigger = cache._workspace("rope", 1000, sizes, big)
     assert bigger is not big is not ws
     assert len(cache._outgrown) == 1 and cache._outgrown[0] is ws
+
+
+@pytest.mark.parametrize("libname", ["hip", "host"])
+def test_workspace_of_one_rotation(libname):
+    """Keys that are rotated in registers need no room for the rotated rows; the query for any
+    rotation is the largest."""
+    lib, rows = _lib(libname), 2 * 2 * 1000 * 128 * 2
+    for kw, rot, saved in ((dict(), 128, rows), (dict(), 48, rows), (dict(), 40, 0), (dict(), 2, 0),
+                           (dict(head_dim=64), 64, 0), (dict(dtype="f32"), 128, 0),
+                           (dict(sel_window=32, sel_stride=16), 128, 0)):
+        c = _cfg(**kw)
+        rope = spla.make_rope(c.head_dim, rot, library=lib)
+        got = spla.append_rope_workspace_bytes(c, 1000, lib, rope)
+        assert got + saved == spla.append_rope_workspace_bytes(c, 1000, lib)
+        assert got % 256 == 0 and got >= spla.append_workspace_bytes(c, 1000, lib)
+    n = ctypes.c_size_t(0)
+    for bad in (spla.SplaRope(), spla.make_rope(64, library=lib)):
+        assert lib.spla_append_rope_workspace_bytes_ex(ctypes.byref(_cfg()), ctypes.byref(bad), 4,
+                                                       ctypes.byref(n)) == -1
+    assert lib.spla_append_rope_workspace_bytes_ex(ctypes.byref(_cfg()), None, 4, None) == -1
