@@ -341,10 +341,11 @@ def _rows(name, x, y, shape, dtype, device):
     return y, at, stride, y.data_ptr(), _row_stride(y, row)
 
 
-def _row_words(name, t, n, device):
-    """The address of the int32 values t, one of n per row or sequence."""
-    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{name}: {n} contiguous int32 values on the rows' device")
+def _row_words(name, t, shape, device):
+    """The address of the int32 values t, one per row or sequence."""
+    if t.shape != shape or t.dtype is not torch.int32 or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name}: a contiguous int32 tensor {list(shape)} on the rows' device is "
+                         "needed")
     return t.data_ptr()
 
 
@@ -352,9 +353,9 @@ def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_
            q_out=None, k_out=None, transpose=False):
     """Rotates q [T, batch, Hq, d] and / or k [T, batch, Hkv, d] (or without T: one position)
     into q_out, k_out (new tensors by default; q_out=q rotates in place) and returns the two.
-    Rows may be slices of wider ones (a fused projection's). positions int32 [T, batch];
-    without it row (t, b) stands at seq_lens[b] + t (seq_lens int32 [batch], or zeros).
-    transpose: the transposed map (the gradient)."""
+    Rows may be slices of wider ones (a fused projection's). positions int32 [T, batch] (rows
+    without T: [batch] too); without it row (t, b) stands at seq_lens[b] + t (seq_lens int32
+    [batch], or zeros). transpose: the transposed map (the gradient)."""
     x = k if q is None else q
     if x is None or (q is None and q_out is not None) or (k is None and k_out is not None):
         raise ValueError("q or k is needed, and no output without its input")
@@ -368,8 +369,10 @@ def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_
         q_out, qp, qs, op, os_ = _rows("q", q, q_out, lead + (cfg.n_q_heads, d), dtype, device)
     if k is not None:
         k_out, kp, ks, tp, ts = _rows("k", k, k_out, lead + (cfg.n_kv_heads, d), dtype, device)
-    at = None if positions is None else _row_words("positions", positions, T * batch, device)
-    lens = None if seq_lens is None else _row_words("seq_lens", seq_lens, batch, device)
+    at = None
+    if positions is not None:
+        at = _row_words("positions", positions, (T, batch) if positions.dim() == 2 else lead, device)
+    lens = None if seq_lens is None else _row_words("seq_lens", seq_lens, (batch,), device)
     if device.type != "cuda":
         raise ValueError("tensors on a GPU are needed")
     _launch(lib().spla_rotate, "spla_rotate", device,

@@ -238,3 +238,23 @@ def test_workspace_of_one_rotation(libname):
         assert lib.spla_append_rope_workspace_bytes_ex(ctypes.byref(_cfg()), ctypes.byref(bad), 4,
                                                        ctypes.byref(n)) == -1
     assert lib.spla_append_rope_workspace_bytes_ex(ctypes.byref(_cfg()), None, 4, None) == -1
+
+
+def test_positions_of_another_shape_are_refused():
+    """Position ids as [batch, T] have the right count, and would turn rows by others' angles."""
+    c, r = _cfg(), spla.make_rope(128)
+    q = torch.zeros(3, 2, 8, 128, dtype=torch.bfloat16)
+    ids = torch.arange(6).int()
+    for bad in (ids.view(2, 3), ids, ids.view(3, 2, 1)):
+        with pytest.raises(ValueError, match="positions"):
+            spla.rotate(c, r, q=q, positions=bad)
+    with pytest.raises(ValueError, match="positions"):
+        spla.rotate(c, r, q=q[0], positions=ids[:2].view(2, 1))
+    for bad in (ids[:2].view(2, 1), ids[:2].view(1, 2)):
+        with pytest.raises(ValueError, match="seq_lens"):
+            spla.rotate(c, r, q=q, seq_lens=bad)
+    for ok in (dict(q=q, positions=ids.view(3, 2)), dict(q=q[0], positions=ids[:2]),
+               dict(q=q[0], positions=ids[:2].view(1, 2)),
+               dict(q=q, seq_lens=ids[:2])):
+        with pytest.raises(ValueError, match="on a GPU"):  # all else is right
+            spla.rotate(c, r, **ok)
