@@ -330,6 +330,9 @@ def _rows(name, x, y, shape, dtype, device):
     if x.shape != shape or x.dtype is not dtype or x.device != device:
         raise ValueError(f"{name}: a {dtype} tensor {list(shape)} is needed, T and the device the "
                          "same for q and k")
+    if (x.requires_grad or y is not None and y.requires_grad) and torch.is_grad_enabled():
+        raise ValueError(f"{name}: no gradient is recorded here (detach it, or torch.no_grad(); "
+                         "transpose=True is the gradient's map)")
     row = shape[-2] * shape[-1]
     at, stride = x.data_ptr(), _row_stride(x, row)
     if y is x:
@@ -355,7 +358,8 @@ def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_
     into q_out, k_out (new tensors by default; q_out=q rotates in place) and returns the two.
     Rows may be slices of wider ones (a fused projection's). positions int32 [T, batch] (rows
     without T: [batch] too); without it row (t, b) stands at seq_lens[b] + t (seq_lens int32
-    [batch], or zeros). transpose: the transposed map (the gradient)."""
+    [batch], or zeros). transpose: the transposed map (the gradient); nothing is recorded for
+    autograd, and rows that it would record are refused."""
     x = k if q is None else q
     if x is None or (q is None and q_out is not None) or (k is None and k_out is not None):
         raise ValueError("q or k is needed, and no output without its input")

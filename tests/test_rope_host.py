@@ -258,3 +258,19 @@ def test_positions_of_another_shape_are_refused():
                dict(q=q, seq_lens=ids[:2])):
         with pytest.raises(ValueError, match="on a GPU"):  # all else is right
             spla.rotate(c, r, **ok)
+
+
+def test_rows_that_record_a_gradient_are_refused():
+    """The results lie outside autograd's graph, and a rotation in place would change a tensor
+    that a recorded product has kept."""
+    c, r = _cfg(), spla.make_rope(128)
+    q = torch.zeros(3, 2, 8, 128, dtype=torch.bfloat16)
+    k, leaf = q[:, :, :2].contiguous(), q.clone().requires_grad_(True)
+    for bad in (dict(q=leaf), dict(q=leaf * 2), dict(q=q, q_out=leaf), dict(q=leaf, q_out=leaf),
+                dict(q=q, k=k.clone().requires_grad_(True)), dict(k=k, k_out=leaf[:, :, :2])):
+        with pytest.raises(ValueError, match="gradient"):
+            spla.rotate(c, r, **bad)
+        with pytest.raises(ValueError, match="on a GPU"), torch.no_grad():  # all else is right
+            spla.rotate(c, r, **bad)
+    with pytest.raises(ValueError, match="on a GPU"):
+        spla.rotate(c, r, q=leaf.detach(), transpose=True)
