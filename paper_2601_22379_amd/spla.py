@@ -280,6 +280,14 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else c_void_p(t.data_ptr())
 
 
+def _indexed(device) -> torch.device:
+    """The device, by its index: "cuda" is the current one now, not whichever is later."""
+    device = torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        return torch.device("cuda", torch.cuda.current_device())
+    return device
+
+
 def _stream(device) -> c_void_p:
     return c_void_p(torch.cuda.current_stream(device).cuda_stream)
 
@@ -300,8 +308,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 def _launch(fn, where, device, args):
     """fn(*args, current stream of device), with that device the current one."""
     index = device.index
-    if index is None or index == torch.cuda.current_device():
-        status = fn(*args, _raw_stream(torch.cuda.current_device()))
+    if index == torch.cuda.current_device():
+        status = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
             status = fn(*args, _raw_stream(index))
@@ -393,7 +401,7 @@ class SplaCache:
         """block_table: int32 [batch, max_seq_len / block_size] on the device,
         page of each block, required when cfg.kv_pages > 0 (paged pool)."""
         self.cfg = cfg
-        self.device = torch.device(device)
+        self.device = _indexed(device)
         if (cfg.kv_pages > 0) != (block_table is not None):
             raise ValueError("a block table goes with kv_pages > 0, and only then")
         if block_table is not None:

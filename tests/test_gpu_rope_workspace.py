@@ -40,3 +40,18 @@ def test_exact_workspace(d, rot, dtype, T):
         T, None, None, ws.data_ptr(), need - 1, torch.cuda.current_stream().cuda_stream) == -4
     two.append_rope(rope, k[:, :, :1].contiguous(), v[:, :, :1].contiguous())
     assert two._rope_ws.numel() == spla.append_rope_workspace_bytes(cfg, 1, rope=rope)
+
+
+def test_default_device():
+    """A cache made without naming a device, from a page table on the current one."""
+    table = torch.arange(8, dtype=torch.int32, device="cuda").view(1, 8)
+    cache = spla.SplaCache(spla.make_config(1, 4, 2, 128, 64, 8, 512, "bf16", kv_pages=8),
+                           block_table=table)
+    assert cache.device == table.device == cache.seq_lens.device
+    k = torch.randn(1, 2, 70, 128, device="cuda").bfloat16()
+    cache.append_rope(spla.make_rope(128), k, k)
+    out, lse = cache.attend(torch.zeros(1, 4, 128, dtype=torch.bfloat16, device="cuda"))
+    # equal weights: fp32 sums of 70 of them, the result rounded once (2^-8 of the largest)
+    want = k.float().mean(2).repeat_interleave(2, 1)
+    assert bool(((out.float() - want).abs() <= 2.0 ** -8 * k.abs().max().float()).all())
+    assert bool((lse.cpu() - torch.log(torch.tensor(70.0))).abs().max() < 1e-5)

@@ -274,3 +274,16 @@ def test_rows_that_record_a_gradient_are_refused():
             spla.rotate(c, r, **bad)
     with pytest.raises(ValueError, match="on a GPU"):
         spla.rotate(c, r, q=leaf.detach(), transpose=True)
+
+
+def test_a_device_without_an_index_is_the_one_it_named_then(monkeypatch):
+    """A cache made on "cuda" stays on the device that was current, whichever is later: its calls
+    launch there, and its workspaces lie there."""
+    at = [3]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: at[0])
+    device = spla._indexed("cuda")
+    at[0] = 5
+    assert device == torch.device("cuda:3") and device.index == 3
+    assert spla._indexed("cuda:1") == torch.device("cuda:1")
+    assert spla._indexed(torch.device("cuda")) == torch.device("cuda:5")
+    assert spla._indexed("cpu") == torch.device("cpu")
