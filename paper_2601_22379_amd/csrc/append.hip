@@ -641,7 +641,7 @@ __global__ __launch_bounds__(256) void append_state_mfma_kernel(
 // fp32 that follows. The kernel is bound by its
 // instructions, 660 vector ones per step and wavefront at two wavefronts per SIMD (held to
 // that, so that the accumulators stay out of a register file of their own: 174 us without,
-// 170 with; 492 MB, 2.9 TB/s).
+// 170 with, each the fastest of its run; at the median 177, 492 MB, 2.8 TB/s).
 struct RopeStep {
   double2 one[SPLA_ROPE_MAX_PAIRS], step[SPLA_ROPE_MAX_PAIRS];
   double2 two[4][SPLA_ROPE_MAX_PAIRS];  // turns of 2, 4, 8 and 16 positions
@@ -1146,11 +1146,11 @@ __global__ __launch_bounds__(256) void append_one_kernel(
 
 // append_one_kernel for a token whose key is rotated on the way: every workgroup
 // rotates the key of its (sequence, KV head) into LDS first (a thread per
-// coordinate, its pair's angle in fp64: the same bits as spla_rotate gives), while
-// the first loads of its part are on their way. n_new: 0 or 1 token per sequence.
-// 7.8 us for 16 sequences of 8 KV heads (bf16, d 128; 17 MB, most of it the state read and
-// written): two dependent loads, the sine, and the arrivals that let the last workgroup
-// of a sequence advance its length.
+// coordinate, its pair's angle in fp64: the same bits as spla_rotate gives); the loads
+// of its part of the state or the statistics are issued after that. n_new: 0 or 1 token
+// per sequence. 8.0 us for 16 sequences of 8 KV heads (bf16, d 128; 17 MB, most of it the
+// state read and written): the length, the key, the sine and a barrier in turn, then the
+// state, and the arrivals that let the last workgroup of a sequence advance its length.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void append_rope_one_kernel(
     Dims m, T* __restrict__ kc, T* __restrict__ vc, float* __restrict__ stats,

@@ -575,9 +575,10 @@ struct StreamPass {
 // this split's keys and are joined at the end. Few rows are bound by the keys' and
 // values' bytes: one token of 4 heads on each of 8 KV heads (bf16, d 128) reads 16 x 64K
 // tokens at 6.0 TB/s, 16 x 16K to 64K at 5.2, and 32K tokens in 28 us; 4096 tokens take
-// 9.6 us, of which loads and join are a few round trips to memory. Two workgroups per compute
-// unit: left to itself the compiler takes 292 registers for fp32 rows of 128 coordinates,
-// which leaves one (1024 rows over 1312 tokens 132 us against 115).
+// 9.9 us, of which loads and join are a few round trips to memory. fp32, 16 x 8000 tokens: 5.5
+// TB/s (d 64: 5.3). Two workgroups per compute unit: left to itself the compiler takes registers
+// for one in fp32 of 128 coordinates (8 x 8000 tokens, 32 heads on 8: 24 tokens 394 us against
+// 385, one token 110 against 113; bf16 of 16 tokens 66 against 63).
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attend_stream_kernel(AttendArgs a) {
   constexpr int OT = D / 16;
@@ -692,8 +693,8 @@ __device__ __forceinline__ void wait_copies() {
 // Many fp32 rows: 64 per workgroup, 16 per wavefront, and the keys and values by way of
 // LDS (copied there in operand order a step ahead, as in the tiles of 128 rows): a load of
 // fp32 operands touches 16 rows of 64 bytes each, and four wavefronts that read them for
-// themselves wait on the first-level cache. 2048 tokens of 32 heads on 8 over 4096 (d 128) 980 us,
-// 105 of the 154 TFLOP/s of a large fp32 product, against 1435 in tiles of 16.
+// themselves wait on the first-level cache. 2048 tokens of 32 heads on 8 over 4096 (d 128) 985 us,
+// 105 of the 154 TFLOP/s of a large fp32 product, against 1432 in tiles of 16.
 template <int D>
 __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a) {
   using Ops = StepOps<float, D>;
@@ -762,7 +763,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a) {
 
 // Joins the records of a tile's splits where the last workgroup does not: 16 / P rows per
 // workgroup by P parts of 16 threads each that take every P-th record, so that no thread
-// takes more than eight at a time after another (kJoinParts of 128 records).
+// takes more than eight (P = 16 for the kAttendMaxSplit records there may be).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   constexpr int E = D / 16;
@@ -795,9 +796,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 // by the loads themselves (no registers) while the step before is used. Three
 // workgroups share a compute unit (164 registers, 33 KB of LDS), so that the
 // exponentials of some run beside the products of others: two, with 64 tokens at a
-// time, took 3 to 6 % longer. 8192 causal tokens of 32 heads on 8 (d 128): 544 us, 1.01
-// PFLOP/s at the 1.7 to 1.9 GHz the chip holds under this load; a chunk of 509 tokens over 66045
-// with capped scores 870 us, 0.79 PFLOP/s.
+// time, took 3 to 6 % longer. 8192 causal tokens of 32 heads on 8: 556 us, 0.99 PFLOP/s (d 64:
+// 334, 0.82, half the products for each exponential); a chunk of 509 tokens over 66045 with
+// capped scores 886 us, 0.77 PFLOP/s.
 //
 // v_mfma_f32_32x32x16_bf16, scores transposed (rows = tokens, columns = queries).
 // The cache's step is an operand image for this shape too: row r = 16 mt + i of
@@ -817,7 +818,7 @@ struct alignas(16) TileBuf {
 };
 
 // kCapped: a cap that bounds all scores, no bias; kBiased: no cap, and no prefix; kGeneral:
-// any. (Packed documents, 2 x 4096 tokens of 32 heads: kBiased 148 us, kGeneral 187.)
+// any. (Packed documents, 2 x 4096 tokens of 32 heads: kBiased 137 us, kGeneral 178.)
 enum { kPlain = 0, kCapped = 1, kBiased = 2, kGeneral = 3 };
 
 // Up to this cap, scores of many rows do without the series of cap_score (1024 queries of 4
@@ -1129,7 +1130,7 @@ static hipError_t attend_launches(AttendArgs a, hipStream_t st) {
   };
   // A cap this small bounds every score: against a reference of half of it, weights lie
   // between 2^-90 and 2^30, and no maximum is sought (512 queries of 4 heads each over 64K
-  // tokens, 8 KV heads: 646 us against 752; 2 x 2048 over 2048: 93 against 109).
+  // tokens, 8 KV heads: 640 us, kGeneral 803; 2 x 2048 over 2048: 93 and 119).
   const bool cap = a.o.softcap > 0.f, bias = a.o.slopes != nullptr;
   const bool bounded = cap && !bias && a.o.softcap * kLog2e <= 60.f;
   const auto tile = [&](auto d) {

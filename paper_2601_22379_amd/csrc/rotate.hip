@@ -7,8 +7,9 @@
 // cosines and sines once, in fp64, leaves them in LDS, and then streams the
 // heads. Positions of a long context times a frequency need fp64: at p = 2^20 an
 // fp32 product is off by up to 2^-4 turns; and with cosine, sine and product in
-// fp64 a bf16 result is the rounding of the true one (through fp32), so that
-// rows rotated here and keys rotated by an append are equal bit for bit. The
+// fp64 a bf16 result is the rounding of the true one (through fp32), which is
+// also what an append that rotates its keys gives (equal but next to a rounding
+// border in chunks, whose angles are turned on step by step). The
 // fp64 rate of the chip is that of plain fp32, and eight fp64 operations per
 // pair are far from it at the rows' bandwidth: 8192 rows of 40 heads (bf16, d 128, 168 MB)
 // take 33 us, 5.1 TB/s; one row 4.6 us.
@@ -61,7 +62,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateRows rows, RotateSet 
     }
     uint4 v0 = *reinterpret_cast<const uint4*>(x + c0), v1 = *reinterpret_cast<const uint4*>(x + c1);
     if (ui < ru) {
-      const double2* w = cs[rr] + (half ? ui * VEC : ui * VEC);
+      const double2* w = cs[rr] + ui * VEC;
       T* a = reinterpret_cast<T*>(&v0);
       T* z = reinterpret_cast<T*>(&v1);
       if (half) {
@@ -120,9 +121,11 @@ hipError_t launch_rotate(const Dims& m, const spla_rope& rope, const RotateRows&
   const int vec = 16 / m.elem;
   const bool pieces = rope.rot_dim % (2 * vec) == 0;
   // rows whose heads do not keep 256 threads busy go four to a workgroup, once that
-  // leaves one for every compute unit (16384 rows of 40 heads, bf16: d 64, 160 units,
-  // 31.5 us against 39.7 with a row each; d 128, 320 units, 55.8 against 57.9, fp32 d 128
-  // 120 against 113)
+  // leaves one for every compute unit (16384 rows of 160 units, bf16 d 64, 40 heads: 31.5 us
+  // against 39.7 with a row each). From 256 units on it depends on the rows: bf16 d 128, 256,
+  // 320 and 384 units, 16384 rows 45.0, 66.5 and 82.8 us, with a row each 49.3, 70.5 and 80.2;
+  // 2048 rows 11.3, 13.1 and 15.4, with a row each 9.6, 12.0 and 13.3; fp32 d 64, 320 units, 16384
+  // rows 64.6 and 61.9
   const bool many = n >= 1024 && (a.heads + b.heads) * (m.d / (2 * vec)) < 256;
   auto go = [&](auto one, auto four, auto any) {
     const int per = pieces && many ? 4 : 1;

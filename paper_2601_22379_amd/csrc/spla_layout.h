@@ -283,7 +283,7 @@ SPLA_HD int prefill_most_splits(const Dims& m) {
 // its places make of kPrefillFill, up to two. A wavefront alone on its SIMD runs
 // little faster than two (half a round 0.8), and the ends of a first round fill with
 // a second (half a round 0.7, three quarters 0.85). 4 x 8 units at 128K, 8 positions:
-// 16 splits (1024 places) 127 us, 32 (2048) 97; 96 positions: 3 (2304) 768, 4 (a third more)
+// 16 splits (1024 places) 127 us, 32 (2048) 97; 96 positions: 3 (2304) 768, 4 (3 x 1024)
 // 621; 8 units of 5 heads, 48 positions: 12 (2304) 82, 10 (1920) 69. Of equals the
 // largest even one (lists longer than k: there 8 took 80).
 SPLA_HD int prefill_splits(const Dims& m, int T) {
@@ -408,8 +408,8 @@ SPLA_HD AppendWs append_ws_layout(const Dims& m, int max_new) {
 // The bulk appends that run in one pass over the new rows.
 SPLA_HD bool append_fusable(const Dims& m) { return m.elem == 2 && m.d == 128 && !windowed(m); }
 // Those that rotate rot_dim coordinates in that pass's registers, where pieces of 8 coordinates
-// hold whole pairs (16384 tokens of 4 x 8 units: 169 us, plain append 143); others rotate into
-// the workspace first (330).
+// hold whole pairs (16384 tokens of 4 x 8 units: 182 us, plain append 141); others rotate into
+// the workspace first (rot_dim 120: 360).
 SPLA_HD bool append_rotates(const Dims& m, int rot_dim) {
   return append_fusable(m) && rot_dim % 16 == 0;
 }
@@ -469,18 +469,23 @@ constexpr int kTileMinSplit = 16;
 // Records that a tile's last workgroup joins at most: eight per thread, one wait for memory.
 // More go to a launch of their own, which has a thread for every eight records and 16th of a
 // row (16 records of 16 rows: 12.5 us, joined by the last workgroup 15.3; 64 of 4 rows: 28.5
-// and 29.3; 96 of 16 rows: 29 and 55).
+// and 29.3; 96 of 16 rows: 29 and 55). The lengths are on the device, so the capacity decides: a
+// short sequence in a long cache takes the launch too (4100 tokens of 32768: 6.3 + 5.3 us).
 constexpr int kJoinInLaunch = 128;
+
+SPLA_HD int attend_min_steps(int rows) {
+  return rows == kAttendRows ? kAttendMinSteps : rows == kTileRows ? kTileMinSplit : kRowsMinSplit;
+}
 
 // Few rows are bound by the keys' bytes from memory (tiles of 16), many by the products
 // (128), or in fp32 by the operand reads (64). bf16, d 128, 8 heads of 4, 4096 and 32K tokens:
 // 64 rows 12.1 and 32.8 us in tiles of 16, 16.0 and 37.3 in one of 128; 96 rows at 32K tokens
 // 57.5 and 35.5 us. fp32, d 64 and 128, 4 heads of 2, 1312 tokens: 66 rows 12.8 and 17.9 us in
-// tiles of 16, 14.7 and 21.9 in tiles of 64; 128 rows 14.5 and 24.9, 15.0 and 22.8.
-SPLA_HD int attend_min_steps(int rows) {
-  return rows == kAttendRows ? kAttendMinSteps : rows == kTileRows ? kTileMinSplit : kRowsMinSplit;
-}
-
+// tiles of 16, 14.7 and 21.9 in tiles of 64; 128 rows 14.5 and 24.9, 15.0 and 22.8. Tiles of 64
+// win where there is much to read (d 64 and 128, 2048 tokens of 32 heads on 8 over 4096: 540 and
+// 985 us against 696 and 1432; 512 over 1312: 69 and 121 against 69 and 138) and lose over few
+// keys, where a tile's steps one after the other are the whole call (2 x 1024 tokens of 8 heads
+// on 4 over 1300: 69 and 120 us against 58 and 115 in tiles of 16).
 SPLA_HD int attend_rows(const Dims& m, int n_tokens) {
   const int64_t rows = (int64_t)n_tokens * m.group;
   if (m.elem == 2) return rows <= 64 ? kAttendRows : kTileRows;
