@@ -390,6 +390,9 @@ def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_
     _launch(lib().spla_rotate, "spla_rotate", device,
             (ctypes.byref(cfg), ctypes.byref(rope), T, at, lens, qp, qs, op, os_, kp, ks, tp, ts,
              1 if transpose else 0))
+    if (q is not None and q_out is q) or (k is not None and k_out is k):  # products that kept them
+        torch.autograd.graph.increment_version([x for x, y in ((q, q_out), (k, k_out))
+                                                if x is not None and y is x])
     return q_out, k_out
 
 
