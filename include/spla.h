@@ -280,6 +280,57 @@ typedef struct spla_attend_opts {
                                 n_tokens */
 } spla_attend_opts;
 
+/* ------------------------------------------------------------ 8-bit cache
+ * Keys and values of dense layers in 8 bits: spla_append8 quantises rows as it
+ * writes them, spla_read8 gives them back, spla_attend8 attends over them.
+ * For each KV head the keys of a block of B tokens (block_size) are codes times
+ * one power of two 2^e, and its values are codes times another. Codes are e4m3
+ * (sign, 4 exponent bits of bias 7, 3 mantissa bits; largest 448, smallest 2^-9; NaN,
+ * no infinities). e is the smallest with max |x| <= 448 2^e over the finite
+ * numbers of the block's rows, -100 <= e <= 119 (smaller blocks lose their
+ * smallest numbers, and magnitudes above 1.75 2^127 become that). Each number
+ * is rounded to the nearest code (ties to even); infinities and NaN become
+ * NaN. When an append brings a larger number to a block in progress, e grows,
+ * and the codes of the block's older rows are rounded again under the new
+ * scale (only numbers below 2^-6 of it can change by that). e never shrinks while a
+ * block fills.
+ *
+ * Caller-owned device buffers, sizes in bytes from spla_cache8_bytes (index in
+ * brackets); nb_cap = max_seq_len / B, slots as in spla_cache: slot (b Hkv + h) nb_cap
+ * + i for block i, or p Hkv + h for a block on page p of a pool (kv_pages > 0, with
+ * block_table as there).
+ *  [0] k_codes  uint8 [slots][B / 32][32 d]   in 32-token steps of 16-byte chunks:
+ *               key (t, c), tt = t % 32, is byte c % 16 of chunk ((tt / 4) % 2 *
+ *               (d / 64) + c / 64) * 64 + (c / 16) % 4 * 16 + 4 * (tt / 8) + tt % 4
+ *  [1] v_codes  likewise: value (t, c) is byte 8 ((c / 16) % 2) + tt % 8 of chunk
+ *               (c / 32) * 64 + (tt / 8) * 16 + c % 16
+ *  [2] scales   fp32 [slots][2]   2^e of the slot's keys and of its values
+ *  [3] seq_lens int32 [batch]
+ *  [4] counters int32 [batch][32] zero between calls
+ * err_flags: int32 [1] or NULL, as in spla_cache. A zero-filled cache is the empty
+ * one. The cfg fields read are those of spla_attend. */
+typedef struct spla_cache8 {
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  float* scales;
+  int32_t* seq_lens;
+  int32_t* counters;
+  int32_t* err_flags;
+  const int32_t* block_table;
+} spla_cache8;
+
+enum { SPLA_CACHE8_NUM_BUFFERS = 5 };
+
+/* Options of spla_attend8: those of spla_attend, and a window. Zero-filled (or a
+ * NULL pointer): every query sees the tokens up to its own. */
+typedef struct spla_attend8_opts {
+  spla_attend_opts attend;
+  int32_t window; /* > 0: the query at position p sees no key at or before p - window, but
+                     for the sinks; 0: no window */
+  int32_t sinks;  /* >= 0: with a window, the first keys that it sees all the same: those
+                     before first_key + sinks (first_key 0 where there is none) */
+} spla_attend8_opts;
+
 /* ---------------------------------------------------------- host-only calls */
 
 /* Text of a status code (static storage). */
@@ -348,6 +399,22 @@ int32_t spla_append_rope_workspace_bytes_ex(const spla_config* cfg, const spla_r
  * shape, must be zero when a call starts, and every call leaves them so. */
 int32_t spla_attend_workspace_bytes(const spla_config* cfg, int32_t n_tokens,
                                     size_t* out_bytes);
+
+/* Bytes of each buffer of an 8-bit cache, out_bytes[SPLA_CACHE8_NUM_BUFFERS] (host
+ * array), in the order listed at spla_cache8. Host only. */
+int32_t spla_cache8_bytes(const spla_config* cfg, size_t* out_bytes);
+
+/* Device workspace that spla_attend8 needs for n_tokens queries per sequence
+ * (host-only query); otherwise as spla_attend_workspace_bytes, and one workspace may
+ * serve both calls in turn. */
+int32_t spla_attend8_workspace_bytes(const spla_config* cfg, int32_t n_tokens,
+                                     size_t* out_bytes);
+
+/* Device workspace that spla_norm_rotate_grad needs for n_tokens positions per
+ * sequence where it gives gradients of weights (host-only query). Needs no
+ * preparation. */
+int32_t spla_norm_rotate_grad_workspace_bytes(const spla_config* cfg, int32_t n_tokens,
+                                              size_t* out_bytes);
 
 /* ---------------------------------------------------------- device calls */
 
@@ -541,6 +608,85 @@ int32_t spla_append_rope(const spla_config* cfg, const spla_cache* cache, const 
 int32_t spla_attend(const spla_config* cfg, const spla_cache* cache, int32_t n_tokens,
                     const void* q, const spla_attend_opts* opts, void* out, float* lse,
                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Per-head RMS norms of the queries and / or keys of n_tokens positions per
+ * sequence, with the rotation in the same pass: a head's row x becomes
+ *   y = R_p (w x / sqrt(mean(x^2) + eps))
+ * with the mean over its d coordinates and R_p as in spla_rotate (gain included).
+ *  q_weight, k_weight: device fp32, or NULL (ones): [Hq][d] and [Hkv][d] with
+ *              weight_per_head = 1, [d] for all heads with 0. 16-byte aligned.
+ *  eps:        finite, >= 0 (a row of zeros with eps = 0 gives NaN).
+ * The other arguments as spla_rotate; in place (q_out = q) too. Sums, norms and
+ * products are fp64, each result is rounded to fp32, then to the element type. */
+int32_t spla_norm_rotate(const spla_config* cfg, const spla_rope* rope, int32_t n_tokens,
+                         const int32_t* positions, const int32_t* seq_lens,
+                         const float* q_weight, const float* k_weight, int32_t weight_per_head,
+                         double eps, const void* q, int64_t q_stride, void* q_out,
+                         int64_t q_out_stride, const void* k, int64_t k_stride, void* k_out,
+                         int64_t k_out_stride, void* stream);
+
+/* Gradients of spla_norm_rotate with respect to its rows and weights.
+ *  q, k:            the rows it was given (NULL: not given).
+ *  q_grad, k_grad:  the gradients with respect to its results, strides of their own.
+ *  q_out, k_out:    the gradients with respect to the rows; may be the rows' or the
+ *                   gradients' own memory with the same stride. Other overlaps are not
+ *                   allowed.
+ *  q_weight_grad, k_weight_grad: device fp32, shaped as the weights, or NULL (not
+ *                   needed); the sum over all rows (and, with weight_per_head = 0, heads),
+ *                   in fp64 and in a fixed order. Zeros where there are no rows.
+ *  workspace:       at least spla_norm_rotate_grad_workspace_bytes(cfg, n_tokens) bytes,
+ *                   256-byte aligned, where a weight's gradient is given; NULL otherwise.
+ * The other arguments as spla_norm_rotate. */
+int32_t spla_norm_rotate_grad(const spla_config* cfg, const spla_rope* rope, int32_t n_tokens,
+                              const int32_t* positions, const int32_t* seq_lens,
+                              const float* q_weight, const float* k_weight,
+                              int32_t weight_per_head, double eps, const void* q,
+                              int64_t q_stride, const void* q_grad, int64_t q_grad_stride,
+                              void* q_out, int64_t q_out_stride, const void* k,
+                              int64_t k_stride, const void* k_grad, int64_t k_grad_stride,
+                              void* k_out, int64_t k_out_stride, float* q_weight_grad,
+                              float* k_weight_grad, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/* Empties an 8-bit cache: zero-fills seq_lens and counters. */
+int32_t spla_reset8(const spla_config* cfg, const spla_cache8* cache, void* stream);
+
+/* Appends tokens to every (sequence, KV head) of an 8-bit cache, quantised as
+ * described at spla_cache8.
+ *  k_new, v_new: device, dtype; row (t, b) of the order [n_tokens][batch] starts
+ *                k_stride (v_stride) elements after row (t, b - 1) and holds the Hkv heads
+ *                of d elements one after the other. Rows t >= n_b of sequence b are not read.
+ *                16-byte aligned, strides multiples of 16 bytes that hold a row.
+ *  n_new:        device int32 [batch] (n_b, clamped to 0 .. n_tokens), or NULL for n_tokens.
+ * Tokens that would exceed max_seq_len are dropped (SPLA_DEVERR_CAPACITY), rows
+ * whose block_table entry is out of range are not written (SPLA_DEVERR_PAGE); lengths
+ * advance as in spla_append. No workspace. */
+int32_t spla_append8(const spla_config* cfg, const spla_cache8* cache, int32_t n_tokens,
+                     const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                     const int32_t* n_new, void* stream);
+
+/* Reads rows of an 8-bit cache back, the numbers that it holds (for a layer with a 16-bit
+ * cache, to move a prefix elsewhere).
+ *  first: device int32 [batch] or NULL (0): row (t, b) is the token at position
+ *         first[b] + t. Positions that the sequence does not hold (negative ones too) give
+ *         zeros.
+ *  k_out, v_out: device, dtype [n_tokens][batch][Hkv][d], 16-byte aligned; NULL: not
+ *         read (one of the two must be given).
+ * The cache is only read. n_tokens = 0 does nothing. */
+int32_t spla_read8(const spla_config* cfg, const spla_cache8* cache, int32_t n_tokens,
+                   const int32_t* first, void* k_out, void* v_out, void* stream);
+
+/* spla_attend over an 8-bit cache, with a sliding window and sinks: the key at j is
+ * visible to the query at position p when
+ *   first_key <= j < L_b and (j <= p or j < prefix_len) and
+ *   (window = 0 or j > p - window or j < first_key + sinks).
+ * Arguments, results and limits as spla_attend, with opts of its own kind and the
+ * workspace of spla_attend8_workspace_bytes. The products are those of the numbers the
+ * cache holds, exactly; fp32 queries and weights enter them with all their bits, for
+ * bf16 the weights are rounded as in spla_attend. */
+int32_t spla_attend8(const spla_config* cfg, const spla_cache8* cache, int32_t n_tokens,
+                     const void* q, const spla_attend8_opts* opts, void* out, float* lse,
+                     void* workspace, size_t workspace_bytes, void* stream);
 
 /* --------------------------------------------- decode without a workspace */
 

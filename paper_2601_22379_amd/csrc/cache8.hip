@@ -1,0 +1,331 @@
+// The 8-bit cache's rows: quantised as they are appended (spla_append8), and read back
+// (spla_read8).
+//
+// The keys (and the values) of a block of B tokens and one KV head are e4m3 numbers times one
+// power of two 2^e, the smallest that brings the largest finite magnitude among them to 448 or
+// less. A power of two costs a floating-point number none of its significant bits, makes codes
+// times scale exact in bf16, and lets the scale of a block in progress grow under its older rows:
+// their codes move by whole exponents, and only what falls below the new smallest step is rounded
+// again. So appending row by row gives the codes of appending at once, but for those.
+//
+// Both directions are one read and one write of the rows.
+#include "spla_fp8.h"
+#include "spla_kernels.h"
+
+namespace spla {
+
+struct Append8Args {
+  Dims m;
+  uint8_t *k, *v;
+  float* scales;
+  int32_t *seq_lens, *counters, *err;
+  const int32_t *table, *n_new;
+  const void *kx, *vx;
+  int64_t k_stride, v_stride;  // elements between the rows of (t, b) and (t, b + 1)
+  int max_new;
+  int blk0;     // first of the touched blocks of this launch
+  int arrive;   // workgroups per sequence that count themselves, the last of which advances its
+                // length; 0: a launch behind this one does
+};
+
+struct Append8Seq {
+  int len, n;    // tokens held, tokens appended
+  bool clipped;  // more were asked for
+};
+__device__ __forceinline__ Append8Seq append8_seq(const Append8Args& a, int b) {
+  Append8Seq s;
+  s.len = min(max(a.seq_lens[b], 0), a.m.cap);
+  const int want = a.n_new ? min(max(a.n_new[b], 0), a.max_new) : a.max_new;
+  s.n = min(want, a.m.cap - s.len);
+  s.clipped = s.n < want;
+  return s;
+}
+
+// Magnitude bits of an fp32 number's, zero for infinities and NaN.
+__device__ __forceinline__ uint32_t finite_bits(uint32_t x) {
+  const uint32_t m = x & 0x7FFFFFFFu;
+  return m < 0x7F800000u ? m : 0u;
+}
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = max(v, lane_xor32(v));
+  v = max(v, lane_xor16(v));
+  v = max(v, dpp_u32<0x128, 0xF>(0u, v));
+  v = max(v, dpp_u32<0x124, 0xF>(0u, v));
+  v = max(v, dpp_u32<0x4E, 0xF>(0u, v));
+  v = max(v, dpp_u32<0xB1, 0xF>(0u, v));
+  return v;
+}
+
+template <typename T>
+struct Piece;  // 16 bytes of a row
+template <>
+struct Piece<bf16_t> {
+  static constexpr int N = 8;
+  uint4 w;
+  __device__ __forceinline__ float get(int i) const {
+    const uint32_t x = i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w;
+    return __uint_as_float(i & 1 ? x & 0xFFFF0000u : x << 16);
+  }
+};
+template <>
+struct Piece<float> {
+  static constexpr int N = 4;
+  uint4 w;
+  __device__ __forceinline__ float get(int i) const {
+    return __uint_as_float(i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w);
+  }
+};
+
+// One block's keys or values of one KV head: the new rows in registers, their largest
+// magnitude, the scale; then the codes of the touched steps are put together in LDS, in the
+// cache's order, with those of older rows (all of the block's, where the scale grows), and
+// written 16 bytes at a time.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void append8_kernel(Append8Args a) {
+  constexpr int N = Piece<T>::N;
+  constexpr int PR = D / N;             // pieces per row
+  constexpr int RPP = 256 / PR;         // rows per pass of the workgroup
+  constexpr int PASSES = 128 / RPP;     // of the largest block
+  __shared__ __align__(16) uint8_t img[128 * D];
+  __shared__ uint32_t s_max[4];
+  __shared__ int s_last;
+  const Dims& m = a.m;
+  const int bh = (int)(blockIdx.x % (unsigned)m.bh), rest = (int)(blockIdx.x / (unsigned)m.bh);
+  const int kv = rest & 1, tid = threadIdx.x;
+  const int b = bh / m.hkv, h = bh % m.hkv;
+  const Append8Seq s = append8_seq(a, b);
+  const int blk = s.len / m.B + a.blk0 + (rest >> 1), t0 = blk * m.B;  // first position
+  const int r0 = max(s.len, t0) - t0, r1 = min(s.len + s.n - t0, m.B);
+  if (s.clipped && tid == 0 && rest == 0 && h == 0 && a.blk0 == 0 && a.err)
+    atomicOr(a.err, SPLA_DEVERR_CAPACITY);
+  int64_t slot = (int64_t)bh * m.nb_cap + blk;
+  bool go = r0 < r1;  // uniform (blk < nb_cap then)
+  if (go && a.table) {
+    const int p = block_page(m, a.table, bh, blk);
+    slot = (int64_t)p * m.hkv + h;
+    if (p < 0) {
+      go = false;
+      if (tid == 0 && a.err) atomicOr(a.err, SPLA_DEVERR_PAGE);
+    }
+  }
+  if (go) {
+    uint8_t* codes = (kv ? a.v : a.k) + slot * m.B * D;
+    float* scale = a.scales + 2 * slot + kv;
+    const T* x = static_cast<const T*>(kv ? a.vx : a.kx) + (int64_t)h * D;
+    const int64_t stride = kv ? a.v_stride : a.k_stride;
+    const int pr = tid % PR, rr = tid / PR;
+    Piece<T> px[PASSES];
+    uint32_t top = 0u;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int r = p * RPP + rr;
+      px[p].w = make_uint4(0u, 0u, 0u, 0u);
+      if (p * RPP < r1 && r >= r0 && r < r1)
+        px[p].w = *reinterpret_cast<const uint4*>(
+            x + ((int64_t)(t0 + r - s.len) * m.batch + b) * stride + pr * N);
+    }
+    const float was = r0 > 0 ? *scale : 0.f;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+      for (int i = 0; i < N; ++i) top = max(top, finite_bits(__float_as_uint(px[p].get(i))));
+    top = wave_max_u32(top);
+    if ((tid & 63) == 0) s_max[tid >> 6] = top;
+    __syncthreads();
+    top = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+    int e = fp8_exponent(top);
+    const int e_old = r0 > 0 ? min(max(exponent_of(was), kScale8Min), kScale8Max) : kScale8Min;
+    e = max(e, e_old);
+    const bool moved = r0 > 0 && e > e_old;
+    // chunks of the steps that are written
+    const int c_lo = (moved ? 0 : r0 / 32) * (2 * D), c_hi = (r1 + 31) / 32 * (2 * D);
+    const float shrink = exp2_int(max(e_old - e, -126));
+    for (int c = c_lo + tid; c < c_hi; c += 256) {
+      const int step = c / (2 * D), q = c % (2 * D), l = q & 63;
+      uint4 w = make_uint4(0u, 0u, 0u, 0u);
+      if (step * 32 < r0) {
+        w = reinterpret_cast<const uint4*>(codes)[c];
+        if (moved)
+          w = make_uint4(fp8_rescale4(w.x, shrink), fp8_rescale4(w.y, shrink),
+                         fp8_rescale4(w.z, shrink), fp8_rescale4(w.w, shrink));
+      }
+      reinterpret_cast<uint4*>(img)[c] = w;
+    }
+    __syncthreads();
+    const float inv = exp2_int(-e);
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+      const int r = p * RPP + rr;
+      if (r >= r0 && r < r1) {
+        uint32_t w[N / 4];
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+          const float f[4] = {px[p].get(4 * i), px[p].get(4 * i + 1), px[p].get(4 * i + 2),
+                              px[p].get(4 * i + 3)};
+          w[i] = fp8_round4(f, inv);
+        }
+        if (kv == 0) {
+          uint32_t* y = reinterpret_cast<uint32_t*>(img + k8_off(m, 0, r, pr * N));
+#pragma unroll
+          for (int i = 0; i < N / 4; ++i) y[i] = w[i];
+        } else {
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            img[v8_off(m, 0, r, pr * N + i)] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+        }
+      }
+    }
+    __syncthreads();
+    for (int c = c_lo + tid; c < c_hi; c += 256)
+      reinterpret_cast<uint4*>(codes)[c] = reinterpret_cast<const uint4*>(img)[c];
+    if (tid == 0) *scale = exp2_int(e);
+  }
+  if (a.arrive) {  // everyone of the sequence has read its length: the last one advances it
+    if (arrive_last(a.counters + (int64_t)b * kSyncLine, a.arrive, &s_last) && tid == 0) {
+      a.seq_lens[b] = s.len + s.n;
+      store_agent(a.counters + (int64_t)b * kSyncLine, 0);  // zero again for the next call
+    }
+  }
+}
+
+hipError_t launch_append8(const Dims& m, const spla_cache8& c, int max_new, const void* k,
+                          int64_t k_stride, const void* v, int64_t v_stride, const int32_t* n_new,
+                          hipStream_t st) {
+  Append8Args a;
+  a.m = m;
+  a.k = c.k_codes;
+  a.v = c.v_codes;
+  a.scales = c.scales;
+  a.seq_lens = c.seq_lens;
+  a.counters = c.counters;
+  a.err = c.err_flags;
+  a.table = m.pages > 0 ? c.block_table : nullptr;
+  a.n_new = n_new;
+  a.kx = k;
+  a.vx = v;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.max_new = max_new;
+  // blocks that rows from anywhere in a block touch
+  const int64_t n_blk = (int64_t)(max_new + m.B - 2) / m.B + 1;
+  const int64_t most = (1 << 22) / (2 * (int64_t)m.bh) > 0 ? (1 << 22) / (2 * (int64_t)m.bh) : 1;
+  a.arrive = n_blk <= kAppend8Arrive ? (int)(2 * n_blk * m.hkv) : 0;
+  auto kern = m.elem == 4 ? (m.d == 64 ? append8_kernel<float, 64> : append8_kernel<float, 128>)
+                          : (m.d == 64 ? append8_kernel<bf16_t, 64> : append8_kernel<bf16_t, 128>);
+  for (int64_t i = 0; i < n_blk; i += most) {
+    a.blk0 = (int)i;
+    const int64_t n = n_blk - i < most ? n_blk - i : most;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(2 * n * m.bh)), dim3(256), 0, st, a);
+  }
+  if (!a.arrive) {
+    spla_cache lens{};
+    lens.seq_lens = c.seq_lens;
+    return launch_append_finish(m, lens, max_new, n_new, st);
+  }
+  return hipGetLastError();
+}
+
+// ---- read back
+struct Read8Args {
+  Dims m;
+  const uint8_t *k, *v;
+  const float* scales;
+  const int32_t *seq_lens, *table, *first;
+  void *ko, *vo;
+  int n_tokens, step0;  // first 32-token step of this launch
+};
+
+// A 32-token step of one KV head (of the cache's, so that its chunks are whole): keys straight
+// from registers, 16 coordinates of a token each; values by way of LDS.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void read8_kernel(Read8Args a) {
+  __shared__ __align__(16) uint8_t img[2][32 * D];
+  const Dims& m = a.m;
+  const int bh = (int)(blockIdx.x % (unsigned)m.bh), tid = threadIdx.x;
+  const int b = bh / m.hkv, h = bh % m.hkv;
+  const int64_t f = a.first ? a.first[b] : 0;
+  const int64_t p0 = (f >> 5 << 5) + 32 * ((int64_t)a.step0 + blockIdx.x / (unsigned)m.bh);
+  const int64_t r0 = p0 - f;  // row of the step's first token
+  if (r0 >= a.n_tokens) return;
+  const int len = min(max(a.seq_lens[b], 0), m.cap);
+  const bool any = p0 >= 0 && p0 < len;  // uniform
+  float ks = 0.f, vs = 0.f;
+  if (any) {
+    const int blk = (int)p0 / m.B;
+    int64_t slot = (int64_t)bh * m.nb_cap + blk;
+    if (a.table) slot = (int64_t)max(block_page(m, a.table, bh, blk), 0) * m.hkv + h;
+    ks = a.scales[2 * slot];
+    vs = a.scales[2 * slot + 1];
+    const int64_t o = (slot * m.B + (int)p0 % m.B) * D;
+    for (int c = tid; c < 2 * D; c += 256) {
+      reinterpret_cast<uint4*>(img[0])[c] = reinterpret_cast<const uint4*>(a.k + o)[c];
+      reinterpret_cast<uint4*>(img[1])[c] = reinterpret_cast<const uint4*>(a.v + o)[c];
+    }
+  }
+  __syncthreads();
+  constexpr int N = 16 / (int)sizeof(T), PR = D / N;
+  for (int e = tid; e < 32 * PR; e += 256) {
+    const int tt = e / PR, c0 = e % PR * N;
+    const int64_t r = r0 + tt;
+    if (r < 0 || r >= a.n_tokens) continue;
+    const bool live = any && p0 + tt < len;
+    const int64_t at = (r * m.batch + b) * m.hkv * D + (int64_t)h * D + c0;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      T* out = static_cast<T*>(kv ? a.vo : a.ko);
+      if (!out) continue;
+      uint32_t w[N / 4];
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        if (kv == 0) {
+          w[i] = *reinterpret_cast<const uint32_t*>(img[0] + k8_off(m, 0, tt, c0 + 4 * i));
+        } else {
+          w[i] = 0u;
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            w[i] |= (uint32_t)img[1][v8_off(m, 0, tt, c0 + 4 * i + x)] << (8 * x);
+        }
+        if (!live) w[i] = 0u;
+      }
+      const float s = live ? (kv ? vs : ks) : 1.f;
+      uint4 y;
+      if constexpr (N == 8) {
+        y = fp8_to_bf16(w[0], w[1], s);
+      } else {
+        const float2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[0], false);
+        const float2_t hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[0], true);
+        y = make_uint4(__float_as_uint(lo[0] * s), __float_as_uint(lo[1] * s),
+                       __float_as_uint(hi[0] * s), __float_as_uint(hi[1] * s));
+      }
+      *reinterpret_cast<uint4*>(out + at) = y;
+    }
+  }
+}
+
+hipError_t launch_read8(const Dims& m, const spla_cache8& c, int n_tokens, const int32_t* first,
+                        void* k_out, void* v_out, hipStream_t st) {
+  Read8Args a;
+  a.m = m;
+  a.k = c.k_codes;
+  a.v = c.v_codes;
+  a.scales = c.scales;
+  a.seq_lens = c.seq_lens;
+  a.table = m.pages > 0 ? c.block_table : nullptr;
+  a.first = first;
+  a.ko = k_out;
+  a.vo = v_out;
+  a.n_tokens = n_tokens;
+  // steps that rows from anywhere in a step touch
+  const int64_t n = ((int64_t)n_tokens + (first ? 30 : -1)) / 32 + 1;
+  const int64_t most = (1 << 22) / (int64_t)m.bh > 0 ? (1 << 22) / (int64_t)m.bh : 1;
+  auto kern = m.elem == 4 ? (m.d == 64 ? read8_kernel<float, 64> : read8_kernel<float, 128>)
+                          : (m.d == 64 ? read8_kernel<bf16_t, 64> : read8_kernel<bf16_t, 128>);
+  for (int64_t i = 0; i < n; i += most) {
+    a.step0 = (int)i;
+    const int64_t k = n - i < most ? n - i : most;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(k * m.bh)), dim3(256), 0, st, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace spla

@@ -1,0 +1,344 @@
+// Per-head RMS norms of queries and keys with the rotary positions in the same pass
+// (spla_norm_rotate), and their gradients (spla_norm_rotate_grad).
+//   y = R_p (w x r),  r = (mean x^2 + eps)^(-1/2) over the head's d coordinates,
+// R_p the rotation of its leading coordinates. With g = R_p^T dy (the rotation by the negated
+// angles, with the same gain), u = g w and n = x r:
+//   dx = r (u - n mean(u n)),  dw = sum over rows of g n.
+//
+// One read and one write of the rows (the gradients read two arrays), so the arithmetic is free
+// to be exact: a head lies in 4 to 16 neighbouring lanes, its squares are summed over them, and
+// norm, weight, sine, cosine and turn are fp64, rounded to fp32 and then to the element type.
+// Squares of finite values cannot overflow, and no input bits are lost before the one rounding.
+#include "spla_device.h"
+#include "spla_kernels.h"
+#include "spla_rope.h"
+
+namespace spla {
+
+// Sum over aligned groups of 2^n neighbouring lanes; the same bits in each.
+template <int LANES>
+__device__ __forceinline__ double group_sum(double v) {
+  v += dpp_f64<0xB1, 0xF>(0.0, v);                     // quad_perm [1,0,3,2]
+  v += dpp_f64<0x4E, 0xF>(0.0, v);                     // quad_perm [2,3,0,1]
+  if (LANES >= 8) v += dpp_f64<0x141, 0xF>(0.0, v);    // row_half_mirror
+  if (LANES >= 16) v += dpp_f64<0x140, 0xF>(0.0, v);   // row_mirror
+  if (LANES >= 32) v += xor16(v);
+  if (LANES >= 64) v += xor32(v);
+  return v;
+}
+
+// What one lane holds of a head: two pieces of VEC coordinates, c0 .. and c1 .., which hold both
+// coordinates of VEC pairs, p0 .. (or of none). VEC = 16 bytes' worth where the rotated
+// coordinates fill pieces, one otherwise.
+template <typename T, int D, int VEC>
+struct HeadUnit {
+  static constexpr int E = 2 * VEC, LANES = D / E;
+  int c0, c1, p0;
+  bool turned;
+  __device__ __forceinline__ HeadUnit(int i, int np, bool half) {
+    turned = i * VEC < np;
+    p0 = i * VEC;
+    if (half && turned) {
+      c0 = p0;
+      c1 = c0 + np;
+    } else {
+      c0 = 2 * i * VEC;
+      c1 = c0 + VEC;
+    }
+  }
+  template <typename U>
+  static __device__ __forceinline__ void piece(const U* p, double* x) {
+    constexpr int B = VEC * (int)sizeof(U);
+    U v[VEC];
+    if constexpr (B >= 16) {
+#pragma unroll
+      for (int i = 0; i < B / 16; ++i)
+        reinterpret_cast<uint4*>(v)[i] = reinterpret_cast<const uint4*>(p)[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) x[i] = (double)Elem<U>::load(v, i);
+  }
+  __device__ __forceinline__ void load(const T* row, double (&x)[E]) const {
+    piece(row + c0, x);
+    piece(row + c1, x + VEC);
+  }
+  __device__ __forceinline__ void weights(const float* w, double (&x)[E]) const {
+    if (w) {
+      piece(w + c0, x);
+      piece(w + c1, x + VEC);
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) x[i] = 1.0;
+    }
+  }
+  __device__ __forceinline__ void store(T* row, const double (&y)[E]) const {
+    __align__(16) T v[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) Elem<T>::store(v, i, (float)y[i]);
+    if constexpr (VEC * sizeof(T) == 16) {
+      *reinterpret_cast<uint4*>(row + c0) = reinterpret_cast<const uint4*>(v)[0];
+      *reinterpret_cast<uint4*>(row + c1) = reinterpret_cast<const uint4*>(v)[1];
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        row[c0 + i] = v[i];
+        row[c1 + i] = v[VEC + i];
+      }
+    }
+  }
+  static __device__ __forceinline__ void turn2(double& a, double& b, double2 w) {
+    const double x = a, y = b;
+    a = fma(x, w.x, -(y * w.y));
+    b = fma(y, w.x, x * w.y);
+  }
+  // cs: the cosines and sines of the row's pairs
+  __device__ __forceinline__ void turn(double (&x)[E], const double2* cs, bool half) const {
+    if (!turned) return;
+    const double2* w = cs + p0;
+    if (half) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) turn2(x[i], x[i + VEC], w[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) turn2(x[2 * i], x[2 * i + 1], w[i]);
+    }
+  }
+};
+
+template <typename T, int D, int VEC>
+__device__ __forceinline__ double inverse_size(const double (&x)[2 * VEC], double eps) {
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < 2 * VEC; ++i) s = fma(x[i], x[i], s);
+  return rsqrt(group_sum<D / (2 * VEC)>(s) * (1.0 / D) + eps);
+}
+
+// R whole rows (a position of a sequence with all its heads) per workgroup, as in the rotation.
+template <typename T, int D, int VEC, int R>
+__global__ __launch_bounds__(256) void norm_rotate_kernel(RotateRows rows, NormSet sa, NormSet sb,
+                                                          spla_rope rope, double eps) {
+  using Unit = HeadUnit<T, D, VEC>;
+  constexpr int UPH = Unit::LANES;
+  __shared__ double2 cs[R][D / 2];
+  const int np = rope.rot_dim / 2;
+  const bool half = rope.layout == SPLA_ROPE_HALF;
+  const int64_t row0 = rows.first + (int64_t)blockIdx.x * R, n_rows = (int64_t)rows.n_tokens * rows.batch;
+  rope_angles<R>(rows, rope, false, row0, cs);
+  __syncthreads();
+  const int units = (sa.r.heads + sb.r.heads) * UPH;
+  for (int e = threadIdx.x; e < R * units; e += 256) {
+    const int rr = e / units, u = e % units, hh = u / UPH;
+    const int64_t row = row0 + rr;
+    if (row >= n_rows) break;  // (the lanes of a head together)
+    const int t = (int)(row / rows.batch), b = (int)(row % rows.batch);
+    const bool first = hh < sa.r.heads;
+    const NormSet& s = first ? sa : sb;
+    const int h = first ? hh : hh - sa.r.heads;
+    const Unit un(u % UPH, np, half);
+    double x[Unit::E], w[Unit::E];
+    un.load(static_cast<const T*>(s.r.x) + t * s.r.xs_t + b * s.r.xs_b + h * s.r.xs_h, x);
+    un.weights(s.w ? s.w + (int64_t)h * s.w_stride : nullptr, w);
+    const double r = inverse_size<T, D, VEC>(x, eps);
+#pragma unroll
+    for (int i = 0; i < Unit::E; ++i) x[i] *= r * w[i];
+    un.turn(x, cs[rr], half);
+    un.store(static_cast<T*>(s.r.y) + t * s.r.ys_t + b * s.r.ys_b + h * s.r.ys_h, x);
+  }
+}
+
+// Gradients. A workgroup takes up to 256 units (blockIdx.y: which) of a run of rows, several
+// rows at a time where they are fewer; a thread keeps its head and coordinates, so that its sums
+// of g n stay in registers. They are summed over the workgroup's rows (and heads, where one
+// weight serves all) in a fixed order and left as a record of the run.
+template <typename T, int D, int VEC>
+__global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, NormSet sa,
+                                                               NormSet sb, spla_rope rope,
+                                                               double eps, double* part) {
+  using Unit = HeadUnit<T, D, VEC>;
+  constexpr int UPH = Unit::LANES, E = Unit::E;
+  constexpr int kRows = 32;  // at most, of those whose angles are formed at once
+  __shared__ union {
+    double2 cs[kRows][D / 2];
+    double sum[256][E];
+  } sh;
+  const int np = rope.rot_dim / 2, tid = threadIdx.x;
+  const bool half = rope.layout == SPLA_ROPE_HALF;
+  const int units = (sa.r.heads + sb.r.heads) * UPH, u0 = (int)blockIdx.y * 256;
+  const int nu = min(256, units - u0), at_once = min(256 / nu, kRows);
+  const int per = at_once * max(1, min(4, kRows / at_once));  // rows whose angles are formed at once
+  const int64_t n_rows = (int64_t)rows.n_tokens * rows.batch;
+  const int64_t begin = n_rows * blockIdx.x / gridDim.x, end = n_rows * (blockIdx.x + 1) / gridDim.x;
+  const bool busy = tid < at_once * nu;
+  const int slot = tid / nu, u = u0 + tid % nu, hh = u / UPH;
+  const bool first = hh < sa.r.heads;
+  const NormSet& s = first ? sa : sb;
+  const int h = first ? hh : hh - sa.r.heads;
+  const Unit un(u % UPH, np, half);
+  double w[E], sum[E];
+  un.weights(s.w && busy ? s.w + (int64_t)h * s.w_stride : nullptr, w);
+#pragma unroll
+  for (int i = 0; i < E; ++i) sum[i] = 0.0;
+  for (int64_t r0 = begin; r0 < end; r0 += per) {
+    __syncthreads();
+    const int n = (int)(end - r0 < per ? end - r0 : per);
+    for (int e = tid; e < n * np; e += 256) {
+      const int rr = e / np, i = e % np;
+      double2 c = rope_cos_sin(row_position(rows, r0 + rr), rope.turns[i], rope.gain);
+      c.y = -c.y;
+      sh.cs[rr][i] = c;
+    }
+    __syncthreads();
+    if (!busy) continue;
+    for (int rr = slot; rr < n; rr += at_once) {
+      const int64_t row = r0 + rr;
+      const int t = (int)(row / rows.batch), b = (int)(row % rows.batch);
+      double x[E], g[E];
+      un.load(static_cast<const T*>(s.r.x) + t * s.r.xs_t + b * s.r.xs_b + h * s.r.xs_h, x);
+      un.load(static_cast<const T*>(s.g) + t * s.gs_t + b * s.gs_b + h * s.r.xs_h, g);
+      un.turn(g, sh.cs[rr], half);
+      const double r = inverse_size<T, D, VEC>(x, eps);
+      double dot = 0.0;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        x[i] *= r;  // n
+        sum[i] = fma(g[i], x[i], sum[i]);
+        g[i] *= w[i];  // u
+        dot = fma(g[i], x[i], dot);
+      }
+      dot = group_sum<UPH>(dot) * (1.0 / D);
+#pragma unroll
+      for (int i = 0; i < E; ++i) x[i] = r * fma(-x[i], dot, g[i]);
+      un.store(static_cast<T*>(s.r.y) + t * s.r.ys_t + b * s.r.ys_b + h * s.r.ys_h, x);
+    }
+  }
+  if (!part) return;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < E; ++i) sh.sum[tid][i] = busy ? sum[i] : 0.0;
+  __syncthreads();
+  // coordinate c of a head: unit and element that hold it
+  const auto held = [&](int c, int& unit, int& el) {
+    const bool t = c < 2 * np;
+    const int j = !half || !t ? c : c % np;  // half: pieces of the first coordinates, then of theirs
+    if (half && t) {
+      unit = j / VEC;
+      el = j % VEC + (c < np ? 0 : VEC);
+    } else {
+      unit = c / (2 * VEC);
+      el = c % (2 * VEC);
+    }
+  };
+  if (sa.w_stride || sb.w_stride) {  // a weight per head
+    double* out = part + ((int64_t)blockIdx.x * (units / UPH) + u0 / UPH) * D;
+    for (int e = tid; e < nu / UPH * D; e += 256) {
+      int unit, el;
+      held(e % D, unit, el);
+      double v = 0.0;
+      for (int k = 0; k < at_once; ++k) v += sh.sum[k * nu + e / D * UPH + unit][el];
+      out[e] = v;
+    }
+    return;
+  }
+  double* out = part + ((int64_t)blockIdx.x * gridDim.y + blockIdx.y) * 2 * D;
+  for (int e = tid; e < 2 * D; e += 256) {
+    int unit, el;
+    held(e % D, unit, el);
+    const int h0 = u0 / UPH, h1 = h0 + nu / UPH;  // heads here: those of the first set, then
+    const int lo = e < D ? h0 : max(h0, sa.r.heads), hi = e < D ? min(h1, sa.r.heads) : h1;
+    double v = 0.0;
+    for (int k = 0; k < at_once; ++k)
+      for (int x = lo; x < hi; ++x) v += sh.sum[k * nu + (x - h0) * UPH + unit][el];
+    out[e] = v;
+  }
+}
+
+// Sums n records of `cols` columns, 16 columns per workgroup by 16 parts of the records, in a
+// fixed order; the first `split` columns go to da, the others to db (NULL: nowhere).
+__global__ __launch_bounds__(256) void norm_grad_reduce_kernel(const double* part, int n, int cols,
+                                                               int split, float* da, float* db) {
+  __shared__ double s[16][16];
+  const int c = (int)blockIdx.x * 16 + (threadIdx.x & 15), p = threadIdx.x >> 4;
+  double v = 0.0;
+#pragma unroll 8
+  for (int i = p; i < n; i += 16) v += part[(int64_t)i * cols + c];
+  s[p][threadIdx.x & 15] = v;
+  __syncthreads();
+  if (p > 0) return;
+  for (int i = 1; i < 16; ++i) v += s[i][threadIdx.x];
+  float* out = c < split ? da : db;
+  if (out) out[c < split ? c : c - split] = (float)v;
+}
+
+namespace {
+constexpr int64_t kMost = 1 << 22;  // workgroups per launch (a grid holds 2^32 threads)
+}
+
+hipError_t launch_norm_rotate(const Dims& m, const spla_rope& rope, double eps,
+                              const RotateRows& rows, const NormSet& a, const NormSet& b,
+                              hipStream_t st) {
+  const int64_t n = (int64_t)rows.n_tokens * rows.batch;
+  if (n == 0) return hipSuccess;
+  const int vec = 16 / m.elem;
+  const bool pieces = rope.rot_dim % (2 * vec) == 0;
+  const bool many = n >= 1024 && (a.r.heads + b.r.heads) * (m.d / (2 * vec)) < 256;
+  auto go = [&](auto one, auto four, auto any) {
+    const int per = pieces && many ? 4 : 1;
+    auto kern = !pieces ? any : many ? four : one;
+    RotateRows part = rows;
+    for (part.first = 0; part.first < n; part.first += kMost * per) {
+      const int64_t wgs = ceil_div(n - part.first, per);
+      hipLaunchKernelGGL(kern, dim3((unsigned)(wgs < kMost ? wgs : kMost)), dim3(256), 0, st, part,
+                         a, b, rope, eps);
+    }
+  };
+  if (m.elem == 4) {
+    if (m.d == 64) go(norm_rotate_kernel<float, 64, 4, 1>, norm_rotate_kernel<float, 64, 4, 4>,
+                      norm_rotate_kernel<float, 64, 1, 1>);
+    else go(norm_rotate_kernel<float, 128, 4, 1>, norm_rotate_kernel<float, 128, 4, 4>,
+            norm_rotate_kernel<float, 128, 1, 1>);
+  } else {
+    if (m.d == 64) go(norm_rotate_kernel<bf16_t, 64, 8, 1>, norm_rotate_kernel<bf16_t, 64, 8, 4>,
+                      norm_rotate_kernel<bf16_t, 64, 1, 1>);
+    else go(norm_rotate_kernel<bf16_t, 128, 8, 1>, norm_rotate_kernel<bf16_t, 128, 8, 4>,
+            norm_rotate_kernel<bf16_t, 128, 1, 1>);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_norm_rotate_grad(const Dims& m, const spla_rope& rope, double eps,
+                                   const RotateRows& rows, const NormSet& a, const NormSet& b,
+                                   float* da, float* db, const NormGradWs& ws, char* base,
+                                   hipStream_t st) {
+  const int64_t n = (int64_t)rows.n_tokens * rows.batch;
+  const int heads_a = n > 0 ? a.r.heads : m.hq, heads = n > 0 ? heads_a + b.r.heads : m.hq + m.hkv;
+  const bool pieces = rope.rot_dim % (32 / m.elem) == 0;
+  const int uph = pieces ? m.d * m.elem / 32 : m.d / 2;
+  const int runs = norm_grad_runs(m, rows.n_tokens), chunks = (int)ceil_div(heads * uph, 256);
+  double* part = da || db ? reinterpret_cast<double*>(base + ws.part) : nullptr;
+  if (n > 0) {
+    auto go = [&](auto kern) {
+      hipLaunchKernelGGL(kern, dim3((unsigned)runs, (unsigned)chunks), dim3(256), 0, st, rows, a, b,
+                         rope, eps, part);
+    };
+    if (m.elem == 4) {
+      if (m.d == 64) pieces ? go(norm_rotate_grad_kernel<float, 64, 4>) : go(norm_rotate_grad_kernel<float, 64, 1>);
+      else pieces ? go(norm_rotate_grad_kernel<float, 128, 4>) : go(norm_rotate_grad_kernel<float, 128, 1>);
+    } else {
+      if (m.d == 64) pieces ? go(norm_rotate_grad_kernel<bf16_t, 64, 8>) : go(norm_rotate_grad_kernel<bf16_t, 64, 1>);
+      else pieces ? go(norm_rotate_grad_kernel<bf16_t, 128, 8>) : go(norm_rotate_grad_kernel<bf16_t, 128, 1>);
+    }
+  }
+  if (part) {
+    const bool per_head = a.w_stride || b.w_stride;
+    const int cols = per_head ? heads * m.d : 2 * m.d, split = per_head ? heads_a * m.d : m.d;
+    const int records = n > 0 ? (per_head ? runs : runs * chunks) : 0;
+    hipLaunchKernelGGL(norm_grad_reduce_kernel, dim3((unsigned)(cols / 16)), dim3(256), 0, st, part,
+                       records, cols, split, da, db);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace spla

@@ -401,6 +401,178 @@ extern "C" int32_t spla_attend(const spla_config* cfg, const spla_cache* cache, 
   return SPLA_OK;
 }
 
+// ---- per-head norms with the rotation, the 8-bit cache -------------------------
+namespace {
+
+// What spla_norm_rotate and its gradients check alike.
+int32_t check_norm(const spla_config* cfg, const spla_rope* rope, int32_t n_tokens,
+                   const float* q_weight, const float* k_weight, int32_t per_head, double eps) {
+  int32_t s = spla_validate(cfg);
+  if (s != SPLA_OK) return s;
+  if ((s = spla::check_rope(*cfg, rope)) != SPLA_OK) return s;
+  if (n_tokens < 0 || (per_head != 0 && per_head != 1)) return SPLA_ERR_INVALID_ARG;
+  if (!(eps >= 0.0) || !(eps <= 1.7976931348623157e308)) return SPLA_ERR_INVALID_ARG;  // (NaN too)
+  if (!aligned16(q_weight) || !aligned16(k_weight)) return SPLA_ERR_INVALID_ARG;
+  return SPLA_OK;
+}
+
+spla::NormSet norm_set(const Dims& m, const void* x, int64_t xs, void* y, int64_t ys, int heads,
+                       const float* w, bool per_head, const void* g, int64_t gs) {
+  const int64_t nb = m.batch;
+  return spla::NormSet{{x, y, nb * xs, xs, m.d, nb * ys, ys, m.d, x ? heads : 0},
+                       w, per_head ? m.d : 0, g, nb * gs, gs};
+}
+
+int32_t check_cache8(const spla_config* cfg, const spla_cache8* c) {
+  if (!c) return SPLA_ERR_INVALID_ARG;
+  if (!c->k_codes || !c->v_codes || !c->scales || !c->seq_lens || !c->counters)
+    return SPLA_ERR_INVALID_ARG;
+  if (!aligned16(c->k_codes) || !aligned16(c->v_codes)) return SPLA_ERR_INVALID_ARG;
+  if ((cfg->kv_pages > 0) != (c->block_table != nullptr)) return SPLA_ERR_INVALID_ARG;
+  return SPLA_OK;
+}
+
+}  // namespace
+
+extern "C" int32_t spla_norm_rotate(const spla_config* cfg, const spla_rope* rope,
+                                    int32_t n_tokens, const int32_t* positions,
+                                    const int32_t* seq_lens, const float* q_weight,
+                                    const float* k_weight, int32_t weight_per_head, double eps,
+                                    const void* q, int64_t q_stride, void* q_out,
+                                    int64_t q_out_stride, const void* k, int64_t k_stride,
+                                    void* k_out, int64_t k_out_stride, void* stream) {
+  int32_t s = check_norm(cfg, rope, n_tokens, q_weight, k_weight, weight_per_head, eps);
+  if (s != SPLA_OK) return s;
+  if (n_tokens == 0) return SPLA_OK;
+  if ((!q && !k) || (q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr))
+    return SPLA_ERR_INVALID_ARG;
+  const Dims m = spla::make_dims(*cfg);
+  if (q && (!good_rows(m, q, q_stride, m.hq) || !good_rows(m, q_out, q_out_stride, m.hq)))
+    return SPLA_ERR_INVALID_ARG;
+  if (k && (!good_rows(m, k, k_stride, m.hkv) || !good_rows(m, k_out, k_out_stride, m.hkv)))
+    return SPLA_ERR_INVALID_ARG;
+  if ((q == q_out && q_stride != q_out_stride) || (k == k_out && k_stride != k_out_stride))
+    return SPLA_ERR_INVALID_ARG;
+  const spla::NormSet a = norm_set(m, q, q_stride, q_out, q_out_stride, m.hq, q_weight,
+                                   weight_per_head, nullptr, 0);
+  const spla::NormSet b = norm_set(m, k, k_stride, k_out, k_out_stride, m.hkv, k_weight,
+                                   weight_per_head, nullptr, 0);
+  const spla::RotateRows rows{n_tokens, m.batch, positions, positions ? nullptr : seq_lens, nullptr,
+                              nullptr};
+  SPLA_TRY(spla::launch_norm_rotate(m, *rope, eps, rows, a, b, static_cast<hipStream_t>(stream)));
+  return SPLA_OK;
+}
+
+extern "C" int32_t spla_norm_rotate_grad(
+    const spla_config* cfg, const spla_rope* rope, int32_t n_tokens, const int32_t* positions,
+    const int32_t* seq_lens, const float* q_weight, const float* k_weight, int32_t weight_per_head,
+    double eps, const void* q, int64_t q_stride, const void* q_grad, int64_t q_grad_stride,
+    void* q_out, int64_t q_out_stride, const void* k, int64_t k_stride, const void* k_grad,
+    int64_t k_grad_stride, void* k_out, int64_t k_out_stride, float* q_weight_grad,
+    float* k_weight_grad, void* workspace, size_t workspace_bytes, void* stream) {
+  int32_t s = check_norm(cfg, rope, n_tokens, q_weight, k_weight, weight_per_head, eps);
+  if (s != SPLA_OK) return s;
+  const Dims m = spla::make_dims(*cfg);
+  if (n_tokens > 0) {
+    if ((!q && !k) || (q != nullptr) != (q_out != nullptr) ||
+        (k != nullptr) != (k_out != nullptr) || (q != nullptr) != (q_grad != nullptr) ||
+        (k != nullptr) != (k_grad != nullptr))
+      return SPLA_ERR_INVALID_ARG;
+    if (q && (!good_rows(m, q, q_stride, m.hq) || !good_rows(m, q_out, q_out_stride, m.hq) ||
+              !good_rows(m, q_grad, q_grad_stride, m.hq)))
+      return SPLA_ERR_INVALID_ARG;
+    if (k && (!good_rows(m, k, k_stride, m.hkv) || !good_rows(m, k_out, k_out_stride, m.hkv) ||
+              !good_rows(m, k_grad, k_grad_stride, m.hkv)))
+      return SPLA_ERR_INVALID_ARG;
+    if ((q && q == q_out && q_stride != q_out_stride) ||
+        (k && k == k_out && k_stride != k_out_stride) ||
+        (q && q_grad == q_out && q_grad_stride != q_out_stride) ||
+        (k && k_grad == k_out && k_grad_stride != k_out_stride))
+      return SPLA_ERR_INVALID_ARG;
+    // a weight's gradient goes with its rows
+    if ((q_weight_grad && !q) || (k_weight_grad && !k)) return SPLA_ERR_INVALID_ARG;
+  }
+  const spla::NormGradWs L = spla::norm_grad_ws_layout(m, n_tokens);
+  const bool sums = q_weight_grad || k_weight_grad;
+  if (sums && (s = check_ws(workspace, workspace_bytes, (size_t)L.total)) != SPLA_OK) return s;
+  if (n_tokens == 0 && !sums) return SPLA_OK;
+  const spla::NormSet a = norm_set(m, q, q_stride, q_out, q_out_stride, m.hq, q_weight,
+                                   weight_per_head, q_grad, q_grad_stride);
+  const spla::NormSet b = norm_set(m, k, k_stride, k_out, k_out_stride, m.hkv, k_weight,
+                                   weight_per_head, k_grad, k_grad_stride);
+  const spla::RotateRows rows{n_tokens, m.batch, positions, positions ? nullptr : seq_lens, nullptr,
+                              nullptr};
+  SPLA_TRY(spla::launch_norm_rotate_grad(m, *rope, eps, rows, a, b, q_weight_grad, k_weight_grad, L,
+                                         static_cast<char*>(workspace),
+                                         static_cast<hipStream_t>(stream)));
+  return SPLA_OK;
+}
+
+extern "C" int32_t spla_reset8(const spla_config* cfg, const spla_cache8* cache, void* stream) {
+  int32_t s = spla_validate(cfg);
+  if (s != SPLA_OK) return s;
+  if ((s = check_cache8(cfg, cache)) != SPLA_OK) return s;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  SPLA_TRY(spla::launch_fill_zero(cache->seq_lens, (size_t)cfg->batch * 4, st));
+  SPLA_TRY(spla::launch_fill_zero(cache->counters, (size_t)cfg->batch * spla::kSyncLine * 4, st));
+  return SPLA_OK;
+}
+
+extern "C" int32_t spla_append8(const spla_config* cfg, const spla_cache8* cache, int32_t n_tokens,
+                                const void* k_new, int64_t k_stride, const void* v_new,
+                                int64_t v_stride, const int32_t* n_new, void* stream) {
+  int32_t s = spla_validate(cfg);
+  if (s != SPLA_OK) return s;
+  if ((s = check_cache8(cfg, cache)) != SPLA_OK) return s;
+  if (n_tokens < 0) return SPLA_ERR_INVALID_ARG;
+  if (n_tokens > cfg->max_seq_len) return SPLA_ERR_CAPACITY;
+  if (n_tokens == 0) return SPLA_OK;
+  const Dims m = spla::make_dims(*cfg);
+  if (!good_rows(m, k_new, k_stride, m.hkv) || !good_rows(m, v_new, v_stride, m.hkv))
+    return SPLA_ERR_INVALID_ARG;
+  SPLA_TRY(spla::launch_append8(m, *cache, n_tokens, k_new, k_stride, v_new, v_stride, n_new,
+                                static_cast<hipStream_t>(stream)));
+  return SPLA_OK;
+}
+
+extern "C" int32_t spla_read8(const spla_config* cfg, const spla_cache8* cache, int32_t n_tokens,
+                              const int32_t* first, void* k_out, void* v_out, void* stream) {
+  int32_t s = spla_validate(cfg);
+  if (s != SPLA_OK) return s;
+  if ((s = check_cache8(cfg, cache)) != SPLA_OK) return s;
+  if (n_tokens < 0) return SPLA_ERR_INVALID_ARG;
+  if (n_tokens == 0) return SPLA_OK;
+  if ((!k_out && !v_out) || !aligned16(k_out) || !aligned16(v_out) || k_out == v_out)
+    return SPLA_ERR_INVALID_ARG;
+  SPLA_TRY(spla::launch_read8(spla::make_dims(*cfg), *cache, n_tokens, first, k_out, v_out,
+                              static_cast<hipStream_t>(stream)));
+  return SPLA_OK;
+}
+
+extern "C" int32_t spla_attend8(const spla_config* cfg, const spla_cache8* cache, int32_t n_tokens,
+                                const void* q, const spla_attend8_opts* opts, void* out,
+                                float* lse, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  int32_t s = spla_validate(cfg);
+  if (s != SPLA_OK) return s;
+  if ((s = check_cache8(cfg, cache)) != SPLA_OK) return s;
+  if (n_tokens < 0) return SPLA_ERR_INVALID_ARG;
+  if (n_tokens > cfg->max_seq_len) return SPLA_ERR_CAPACITY;
+  const spla_attend8_opts o = opts ? *opts : spla_attend8_opts{};
+  const float c = o.attend.softcap;
+  if (c != 0.f && !(c >= SPLA_SOFTCAP_MIN && c <= SPLA_SOFTCAP_MAX))
+    return SPLA_ERR_INVALID_ARG;  // (NaN too)
+  if (o.window < 0 || o.sinks < 0) return SPLA_ERR_INVALID_ARG;
+  if (n_tokens == 0) return SPLA_OK;
+  if (!q || !out || out == q || !aligned16(q) || !aligned16(out)) return SPLA_ERR_INVALID_ARG;
+  const Dims m = spla::make_dims(*cfg);
+  const spla::AttendWs L = spla::attend8_ws_layout(m, n_tokens);
+  if ((s = check_ws(workspace, workspace_bytes, (size_t)L.total)) != SPLA_OK) return s;
+  SPLA_TRY(spla::launch_attend8(m, *cfg, *cache, n_tokens, q, o, out, lse, L,
+                                static_cast<char*>(workspace), static_cast<hipStream_t>(stream)));
+  return SPLA_OK;
+}
+
 // ---- decode without a caller workspace (callers that cannot allocate) ------
 // The decode workspace of spla_decode_noalloc: one copy of this array per
 // device, held by every GPU the library runs on until the process ends. In

@@ -197,3 +197,37 @@ extern "C" int32_t spla_attend_workspace_bytes(const spla_config* c, int32_t n_t
   *out = (size_t)spla::attend_ws_layout(spla::make_dims(*c), n_tokens).total;
   return SPLA_OK;
 }
+
+extern "C" int32_t spla_cache8_bytes(const spla_config* c, size_t* out) {
+  if (!out) return SPLA_ERR_INVALID_ARG;
+  int32_t st = spla_validate(c);
+  if (st != SPLA_OK) return st;
+  const Dims m = spla::make_dims(*c);
+  const size_t slots = (size_t)spla::slots8(m);
+  out[0] = out[1] = slots * m.B * m.d;
+  out[2] = slots * 2 * 4;
+  out[3] = (size_t)m.batch * 4;
+  out[4] = (size_t)m.batch * spla::kSyncLine * 4;
+  return SPLA_OK;
+}
+
+extern "C" int32_t spla_attend8_workspace_bytes(const spla_config* c, int32_t n_tokens,
+                                                size_t* out) {
+  if (!out) return SPLA_ERR_INVALID_ARG;
+  int32_t st = spla_validate(c);
+  if (st != SPLA_OK) return st;
+  if (n_tokens < 0) return SPLA_ERR_INVALID_ARG;
+  if (n_tokens > c->max_seq_len) return SPLA_ERR_CAPACITY;
+  *out = (size_t)spla::attend8_ws_layout(spla::make_dims(*c), n_tokens).total;
+  return SPLA_OK;
+}
+
+extern "C" int32_t spla_norm_rotate_grad_workspace_bytes(const spla_config* c, int32_t n_tokens,
+                                                         size_t* out) {
+  if (!out) return SPLA_ERR_INVALID_ARG;
+  int32_t st = spla_validate(c);
+  if (st != SPLA_OK) return st;
+  if (n_tokens < 0) return SPLA_ERR_INVALID_ARG;
+  *out = (size_t)spla::norm_grad_ws_layout(spla::make_dims(*c), n_tokens).total;
+  return SPLA_OK;
+}

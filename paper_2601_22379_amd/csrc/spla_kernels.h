@@ -138,6 +138,38 @@ struct RotateRows {
 hipError_t launch_rotate(const Dims& m, const spla_rope& rope, const RotateRows& rows,
                          const RotateSet& a, const RotateSet& b, bool transpose, hipStream_t st);
 
+// norm_rotate.hip: per-head norms of the rows of r, with their weight (element i of head h at h
+// w_stride + i; NULL: ones), before the rotation; for the gradients g, laid out by its own
+// strides (its heads as those of r.x), is the gradient of the result and r.y that of the rows
+struct NormSet {
+  RotateSet r;
+  const float* w;
+  int64_t w_stride;
+  const void* g;
+  int64_t gs_t, gs_b;
+};
+hipError_t launch_norm_rotate(const Dims& m, const spla_rope& rope, double eps,
+                              const RotateRows& rows, const NormSet& a, const NormSet& b,
+                              hipStream_t st);
+// da, db: gradients of the weights (NULL where there is none); both sets have a weight per head,
+// or one for all
+hipError_t launch_norm_rotate_grad(const Dims& m, const spla_rope& rope, double eps,
+                                   const RotateRows& rows, const NormSet& a, const NormSet& b,
+                                   float* da, float* db, const NormGradWs& ws, char* wsbase,
+                                   hipStream_t st);
+
+// cache8.hip: the 8-bit cache's rows appended (k, v: row (t, b) at (t batch + b) stride) and read
+hipError_t launch_append8(const Dims& m, const spla_cache8& c, int max_new, const void* k,
+                          int64_t k_stride, const void* v, int64_t v_stride, const int32_t* n_new,
+                          hipStream_t st);
+hipError_t launch_read8(const Dims& m, const spla_cache8& c, int n_tokens, const int32_t* first,
+                        void* k_out, void* v_out, hipStream_t st);
+
+// attend8.hip: exact attention over the 8-bit cache
+hipError_t launch_attend8(const Dims& m, const spla_config& cfg, const spla_cache8& c, int n_tokens,
+                          const void* q, const spla_attend8_opts& opts, void* out, float* lse,
+                          const AttendWs& ws, char* wsbase, hipStream_t st);
+
 // attend.hip: exact attention over the cache
 hipError_t launch_attend(const Dims& m, const spla_config& cfg, const spla_cache& c, int n_tokens,
                          const void* q, const spla_attend_opts& opts, void* out, float* lse,

@@ -87,6 +87,27 @@ SPLA_HD int64_t v_off_slot(const Dims& m, int64_t slot, int tb, int c) {
   const int q = (c >> 4) * 64 + (tt >> 3) * 16 + (c & 15);
   return (slot * m.B + (tb & ~31)) * m.d + q * 8 + (tt & 7);
 }
+// The 8-bit cache: codes in 32-token steps of 32 d bytes, each in the order the matrix-core pass
+// loads it, as 16-byte chunks (chunk q at byte 16 q of its step):
+//   keys    chunk (mt * d/64 + p) * 64 + l holds token 8 (i / 4) + 4 mt + i % 4, coordinates
+//           64 p + 16 g .. + 15   (l = 16 g + i)
+//   values  chunk u * 64 + l holds coordinates 32 u + i and 32 u + 16 + i, tokens 8 g .. 8 g + 7
+//           of each
+// Slots as above, B * d bytes each; scales fp32 [slots][2]: the power of two that a slot's keys,
+// and its values, are multiples of.
+constexpr int kScale8Min = -100, kScale8Max = 119;  // its exponents
+SPLA_HD int64_t k8_off(const Dims& m, int64_t slot, int tb, int j) {
+  const int tt = tb & 31, mt = (tt >> 2) & 1, i = 4 * (tt >> 3) + (tt & 3);
+  const int q = (mt * (m.d >> 6) + (j >> 6)) * 64 + ((j >> 4) & 3) * 16 + i;
+  return (slot * m.B + (tb & ~31)) * m.d + q * 16 + (j & 15);
+}
+SPLA_HD int64_t v8_off(const Dims& m, int64_t slot, int tb, int c) {
+  const int tt = tb & 31, q = (c >> 5) * 64 + (tt >> 3) * 16 + (c & 15);
+  return (slot * m.B + (tb & ~31)) * m.d + q * 16 + ((c >> 4) & 1) * 8 + (tt & 7);
+}
+SPLA_HD int64_t slots8(const Dims& m) {
+  return m.pages > 0 ? (int64_t)m.pages * m.hkv : (int64_t)m.bh * m.nb_cap;
+}
 // Contiguous caches: token t of (sequence, kv head) bh.
 SPLA_HD int64_t k_off(const Dims& m, int64_t bh, int64_t t, int j) {
   return k_off_slot(m, bh * m.nb_cap + t / m.B, (int)(t % m.B), j);
@@ -507,9 +528,10 @@ struct AttendWs {
   int64_t total;
 };
 
-SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
+// rows: query rows per tile.
+SPLA_HD AttendWs attend_ws_of(const Dims& m, int n_tokens, int rows_per_tile) {
   AttendWs w;
-  w.rows = attend_rows(m, n_tokens);
+  w.rows = rows_per_tile;
   const bool wide = w.rows != kAttendRows;
   w.n_tiles = (int)ceil_div((int64_t)n_tokens * m.group, w.rows);
   const int64_t wgs = (int64_t)m.bh * w.n_tiles;
@@ -536,6 +558,39 @@ SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
   w.ml = take(rec * 2 * 4);
   w.n_eff = take(w.join ? wgs * 4 : 0);
   w.total = off;
+  return w;
+}
+
+SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
+  return attend_ws_of(m, n_tokens, attend_rows(m, n_tokens));
+}
+
+// ---- exact attention over the 8-bit cache: tiles of 16 rows
+SPLA_HD AttendWs attend8_ws_layout(const Dims& m, int n_tokens) {
+  return attend_ws_of(m, n_tokens, kAttendRows);
+}
+
+// Appends of up to so many blocks count their workgroups in the cache's counters, and the last
+// one advances the length; longer ones leave that to a launch of their own.
+constexpr int kAppend8Arrive = 4;
+
+// ---- gradients of the per-head norms
+// Rows of the partial weight gradients: each of a workgroup's run of positions.
+constexpr int kNormGradRuns = 512;
+
+struct NormGradWs {
+  int64_t part;  // f64 [runs][(Hq + Hkv) or 2][d] partial sums of the weights' gradients
+  int64_t total;
+};
+SPLA_HD int norm_grad_runs(const Dims& m, int n_tokens) {
+  const int64_t n = (int64_t)n_tokens * m.batch;
+  return (int)(n < kNormGradRuns ? n : kNormGradRuns);
+}
+SPLA_HD NormGradWs norm_grad_ws_layout(const Dims& m, int n_tokens) {
+  NormGradWs w;
+  w.part = 0;
+  w.total = align_up((int64_t)norm_grad_runs(m, n_tokens) * (m.hq + m.hkv) * m.d * 8,
+                     SPLA_WORKSPACE_ALIGN);
   return w;
 }
 

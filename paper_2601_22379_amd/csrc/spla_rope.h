@@ -15,6 +15,16 @@ __device__ __forceinline__ double2 rope_cos_sin(double p, double turns, double g
   return make_double2(gain * c, gain * s);
 }
 
+// Rotary position of row t batch + b.
+__device__ __forceinline__ double row_position(const RotateRows& rows, int64_t row) {
+  if (rows.positions) return rows.positions[row];
+  const int t = (int)(row / rows.batch), b = (int)(row % rows.batch);
+  double p = t;
+  if (rows.base) p += rows.base[b];
+  if (rows.shift) p += rows.shift[b];
+  return p;
+}
+
 // cs[r][i]: the cosine and sine of pair i at rows row0 + r (rows past the last,
 // and past a sequence's count, get those of some position).
 template <int R, int P>
@@ -25,16 +35,7 @@ __device__ __forceinline__ void rope_angles(const RotateRows& rows, const spla_r
   for (int e = threadIdx.x; e < R * np; e += blockDim.x) {
     const int rr = e / np, i = e % np;
     const int64_t row = row0 + rr < n_rows ? row0 + rr : n_rows - 1;
-    const int t = (int)(row / rows.batch), b = (int)(row % rows.batch);
-    double p;
-    if (rows.positions) {
-      p = rows.positions[row];
-    } else {
-      p = t;
-      if (rows.base) p += rows.base[b];
-      if (rows.shift) p += rows.shift[b];
-    }
-    double2 w = rope_cos_sin(p, rope.turns[i], rope.gain);
+    double2 w = rope_cos_sin(row_position(rows, row), rope.turns[i], rope.gain);
     if (transpose) w.y = -w.y;
     cs[rr][i] = w;
   }

@@ -40,11 +40,14 @@ HOST_EXPORTS = ["spla_status_string", "spla_phase_name", "spla_validate", "spla_
                 "spla_workspace_bytes", "spla_append_workspace_bytes", "spla_decode_phase_mask",
                 "spla_prefill_workspace_bytes", "spla_rope_init",
                 "spla_append_rope_workspace_bytes", "spla_append_rope_workspace_bytes_ex",
-                "spla_attend_workspace_bytes"]
+                "spla_attend_workspace_bytes", "spla_cache8_bytes", "spla_attend8_workspace_bytes",
+                "spla_norm_rotate_grad_workspace_bytes"]
 EXPORTS = HOST_EXPORTS + ["spla_workspace_init", "spla_reset", "spla_append", "spla_decode",
                           "spla_decode_ex", "spla_step", "spla_step_ex", "spla_prefill",
                           "spla_prefill_ex", "spla_decode_noalloc", "spla_rotate",
-                          "spla_append_rope", "spla_attend"]
+                          "spla_append_rope", "spla_attend", "spla_norm_rotate",
+                          "spla_norm_rotate_grad", "spla_reset8", "spla_append8", "spla_read8",
+                          "spla_attend8"]
 
 
 class SplaError(RuntimeError):
@@ -89,6 +92,16 @@ class SplaAttendOpts(ctypes.Structure):
                 ("first_key", c_void_p), ("prefix_len", c_void_p), ("n_new", c_void_p)]
 
 
+class SplaCache8Struct(ctypes.Structure):
+    _fields_ = [("k_codes", c_void_p), ("v_codes", c_void_p), ("scales", c_void_p),
+                ("seq_lens", c_void_p), ("counters", c_void_p), ("err_flags", c_void_p),
+                ("block_table", c_void_p)]
+
+
+class SplaAttend8Opts(ctypes.Structure):
+    _fields_ = [("attend", SplaAttendOpts), ("window", c_int32), ("sinks", c_int32)]
+
+
 def _declare(lib, host_only=False):
     cfgp = POINTER(SplaConfig)
     cachep = POINTER(SplaCacheStruct)
@@ -117,8 +130,32 @@ def _declare(lib, host_only=False):
                                                         POINTER(c_size_t)]
     lib.spla_attend_workspace_bytes.restype = c_int32
     lib.spla_attend_workspace_bytes.argtypes = [cfgp, c_int32, POINTER(c_size_t)]
+    lib.spla_cache8_bytes.restype = c_int32
+    lib.spla_cache8_bytes.argtypes = [cfgp, POINTER(c_size_t)]
+    lib.spla_attend8_workspace_bytes.restype = c_int32
+    lib.spla_attend8_workspace_bytes.argtypes = [cfgp, c_int32, POINTER(c_size_t)]
+    lib.spla_norm_rotate_grad_workspace_bytes.restype = c_int32
+    lib.spla_norm_rotate_grad_workspace_bytes.argtypes = [cfgp, c_int32, POINTER(c_size_t)]
     if host_only:
         return lib
+    cache8p = POINTER(SplaCache8Struct)
+    rows = [c_void_p, c_int64]  # an address and the stride of its rows
+    lib.spla_norm_rotate.restype = c_int32
+    lib.spla_norm_rotate.argtypes = [cfgp, POINTER(SplaRope), c_int32, c_void_p, c_void_p, c_void_p,
+                                     c_void_p, c_int32, c_double, *rows * 4, c_void_p]
+    lib.spla_norm_rotate_grad.restype = c_int32
+    lib.spla_norm_rotate_grad.argtypes = [cfgp, POINTER(SplaRope), c_int32, c_void_p, c_void_p,
+                                          c_void_p, c_void_p, c_int32, c_double, *rows * 6, c_void_p,
+                                          c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.spla_reset8.restype = c_int32
+    lib.spla_reset8.argtypes = [cfgp, cache8p, c_void_p]
+    lib.spla_append8.restype = c_int32
+    lib.spla_append8.argtypes = [cfgp, cache8p, c_int32, *rows * 2, c_void_p, c_void_p]
+    lib.spla_read8.restype = c_int32
+    lib.spla_read8.argtypes = [cfgp, cache8p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.spla_attend8.restype = c_int32
+    lib.spla_attend8.argtypes = [cfgp, cache8p, c_int32, c_void_p, POINTER(SplaAttend8Opts),
+                                 c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.spla_rotate.restype = c_int32
     lib.spla_rotate.argtypes = [cfgp, POINTER(SplaRope), c_int32, c_void_p, c_void_p,
                                 c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
@@ -248,6 +285,28 @@ def attend_workspace_bytes(cfg: SplaConfig, n_tokens: int, library=None) -> int:
     _check((library or lib()).spla_attend_workspace_bytes(ctypes.byref(cfg), int(n_tokens),
                                                           ctypes.byref(n)),
            "spla_attend_workspace_bytes")
+    return int(n.value)
+
+
+def cache8_bytes(cfg: SplaConfig, library=None) -> list:
+    out = (c_size_t * 5)()
+    _check((library or lib()).spla_cache8_bytes(ctypes.byref(cfg), out), "spla_cache8_bytes")
+    return list(out)
+
+
+def attend8_workspace_bytes(cfg: SplaConfig, n_tokens: int, library=None) -> int:
+    n = c_size_t(0)
+    _check((library or lib()).spla_attend8_workspace_bytes(ctypes.byref(cfg), int(n_tokens),
+                                                           ctypes.byref(n)),
+           "spla_attend8_workspace_bytes")
+    return int(n.value)
+
+
+def norm_rotate_grad_workspace_bytes(cfg: SplaConfig, n_tokens: int, library=None) -> int:
+    n = c_size_t(0)
+    _check((library or lib()).spla_norm_rotate_grad_workspace_bytes(ctypes.byref(cfg),
+                                                                    int(n_tokens), ctypes.byref(n)),
+           "spla_norm_rotate_grad_workspace_bytes")
     return int(n.value)
 
 
@@ -396,7 +455,198 @@ def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_
     return q_out, k_out
 
 
-class SplaCache:
+def _rotated_rows(cfg, q, k, positions, seq_lens):
+    """What the calls that rotate rows have in common: (T, the rows' leading sizes, dtype,
+    device, address of positions, of seq_lens)."""
+    x = k if q is None else q
+    if x is None:
+        raise ValueError("q or k is needed")
+    n, batch = x.dim(), cfg.batch
+    if n not in (3, 4):
+        raise ValueError(f"rows of [T, {batch}] or [{batch}] positions are needed")
+    T = x.shape[0] if n == 4 else 1
+    lead = (T, batch) if n == 4 else (batch,)
+    device = x.device
+    at = None
+    if positions is not None:
+        at = _row_words("positions", positions, (T, batch) if positions.dim() == 2 else lead, device)
+    lens = None if seq_lens is None else _row_words("seq_lens", seq_lens, (batch,), device)
+    if device.type != "cuda":
+        raise ValueError("tensors on a GPU are needed")
+    return T, lead, torch_dtype(cfg), device, at, lens
+
+
+def _head_weights(cfg, q_weight, k_weight, device):
+    """Whether the weights are one per head, and their addresses."""
+    kinds = set()
+    for name, w, h in (("q_weight", q_weight, cfg.n_q_heads), ("k_weight", k_weight,
+                                                               cfg.n_kv_heads)):
+        if w is None:
+            continue
+        if (w.dtype is not torch.float32 or not w.is_contiguous() or w.device != device
+                or w.shape not in ((cfg.head_dim,), (h, cfg.head_dim))):
+            raise ValueError(f"{name}: a contiguous fp32 tensor [{cfg.head_dim}] or "
+                             f"[{h}, {cfg.head_dim}] on the rows' device is needed")
+        if w.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name}: no gradient is recorded here (detach it, or "
+                             "torch.no_grad(); norm_rotate_grad gives it)")
+        kinds.add(w.dim())
+    if len(kinds) > 1:
+        raise ValueError("q_weight and k_weight: a weight per head for both, or one for all heads")
+    return (int(kinds == {2}), None if q_weight is None else q_weight.data_ptr(),
+            None if k_weight is None else k_weight.data_ptr())
+
+
+def _written(*pairs):
+    """Counts the writes to (x, y) where y is x, for products that kept x."""
+    same = [x for x, y in pairs if x is not None and y is x]
+    if same:
+        torch.autograd.graph.increment_version(same)
+
+
+def norm_rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, q_weight=None, k_weight=None,
+                eps=1e-6, positions=None, seq_lens=None, q_out=None, k_out=None):
+    """rotate() of rows whose heads are normed first: x / sqrt(mean(x^2) + eps) times the weight
+    (fp32, [d] for all heads or [Hq, d] and [Hkv, d]; None: ones). Rows, positions and outputs as
+    rotate() takes them; nothing is recorded for autograd (norm_rotate_grad gives the
+    gradients)."""
+    if (q is None and q_out is not None) or (k is None and k_out is not None):
+        raise ValueError("no output without its input")
+    T, lead, dtype, device, at, lens = _rotated_rows(cfg, q, k, positions, seq_lens)
+    qp = qs = op = os_ = kp = ks = tp = ts = 0
+    if q is not None:
+        q_out, qp, qs, op, os_ = _rows("q", q, q_out, lead + (cfg.n_q_heads, cfg.head_dim), dtype,
+                                       device)
+    if k is not None:
+        k_out, kp, ks, tp, ts = _rows("k", k, k_out, lead + (cfg.n_kv_heads, cfg.head_dim), dtype,
+                                      device)
+    per_head, qw, kw = _head_weights(cfg, q_weight, k_weight, device)
+    _launch(lib().spla_norm_rotate, "spla_norm_rotate", device,
+            (ctypes.byref(cfg), ctypes.byref(rope), T, at, lens, qw, kw, per_head, eps, qp, qs, op,
+             os_, kp, ks, tp, ts))
+    _written((q, q_out), (k, k_out))
+    return q_out, k_out
+
+
+def norm_rotate_grad(cfg: SplaConfig, rope: SplaRope, q=None, k=None, q_grad=None, k_grad=None,
+                     q_weight=None, k_weight=None, eps=1e-6, positions=None, seq_lens=None,
+                     q_out=None, k_out=None):
+    """Gradients of norm_rotate(cfg, rope, q, k, ...) from those of its results, q_grad and k_grad
+    (laid out like q and k, with row strides of their own): (with respect to q, to k, to
+    q_weight, to k_weight), None for what was not given. q_out, k_out: where the first two go (new
+    tensors by default; the rows' or the gradients' own are allowed); the weights' are new fp32
+    tensors, sums over the rows (and the heads that share a weight)."""
+    if ((q is None) != (q_grad is None) or (k is None) != (k_grad is None)
+            or (q is None and (q_out is not None or q_weight is not None))
+            or (k is None and (k_out is not None or k_weight is not None))):
+        raise ValueError("rows and their gradients go together, outputs and weights with them")
+    T, lead, dtype, device, at, lens = _rotated_rows(cfg, q, k, positions, seq_lens)
+    per_head, qw, kw = _head_weights(cfg, q_weight, k_weight, device)
+    args, outs = [], []
+    for name, x, g, y, h in (("q", q, q_grad, q_out, cfg.n_q_heads),
+                             ("k", k, k_grad, k_out, cfg.n_kv_heads)):
+        if x is None:
+            args += [0] * 6
+            outs.append(None)
+            continue
+        shape = lead + (h, cfg.head_dim)
+        y, xp, xs, yp, ys = _rows(name, x, y, shape, dtype, device)
+        _, gp, gs, _, _ = _rows(f"{name}_grad", g, g, shape, dtype, device)
+        args += [xp, xs, gp, gs, yp, ys]
+        outs.append(y)
+    qwg, kwg = (None if w is None else torch.empty_like(w) for w in (q_weight, k_weight))
+    ws = None
+    if qwg is not None or kwg is not None:
+        ws = _aligned_workspace(norm_rotate_grad_workspace_bytes(cfg, T), device)
+    _launch(lib().spla_norm_rotate_grad, "spla_norm_rotate_grad", device,
+            (ctypes.byref(cfg), ctypes.byref(rope), T, at, lens, qw, kw, per_head, eps, *args,
+             None if qwg is None else qwg.data_ptr(), None if kwg is None else kwg.data_ptr(),
+             None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel()))
+    _written((q, outs[0]), (q_grad, outs[0]), (k, outs[1]), (k_grad, outs[1]))
+    return outs[0], outs[1], qwg, kwg
+
+
+class _DeviceCache:
+    """What the caches have in common: the error word, workspaces, checks."""
+
+    _outgrown: list  # workspaces that captured graphs name
+    _ws_sizes: dict
+
+    def device_errors(self) -> int:
+        """The SPLA_DEVERR_* bits the device has set in this cache's error
+        word (waits for the work queued on the current stream)."""
+        return int(self.err.item())
+
+    def clear_device_errors(self):
+        self.err.zero_()
+
+    def check_device_errors(self, allowed: int = 0):
+        """Raises SplaError when a bit outside `allowed` is set: after a
+        SPLA_DEVERR_SYNC the outputs of the call that set it are undefined."""
+        e = self.device_errors()
+        if e & ~allowed:
+            names = [n for n, v in (("CAPACITY", DEVERR_CAPACITY), ("SYNC", DEVERR_SYNC),
+                                    ("PAGE", DEVERR_PAGE)) if e & v]
+            raise SplaError(-5, "device error word: " + "|".join(names))
+
+    def _workspace(self, kind, n, sizes, ws):
+        """The workspace ws, or a larger one in its place (zeros: its counters), for a call of
+        n tokens; the sizes of earlier calls are remembered. It grows by half at least, so that
+        calls that get longer one by one seldom make a new one, and one that a capture has used
+        is kept."""
+        need = self._ws_sizes.get((kind, n))
+        if need is None:
+            need = self._ws_sizes[kind, n] = sizes(self.cfg, n)
+        capturing = torch.cuda.is_current_stream_capturing()
+        if ws is None or ws.numel() < need:
+            if capturing:  # its zeros would come with a replay only
+                raise RuntimeError("a capture needs a call of its sizes ahead of it, which makes "
+                                   "the workspace")
+            if ws is not None:
+                need = max(need, ws.numel() * 3 // 2)
+                if ws.is_cuda:  # calls on this stream, not its own, may still use it
+                    ws.record_stream(torch.cuda.current_stream(ws.device))
+            ws = _aligned_workspace(need, self.device).zero_()
+        elif capturing and not any(ws is kept for kept in self._outgrown):
+            self._outgrown.append(ws)
+        return ws
+
+    def _given(self, name, t, shape, dtype):
+        """The address of t, checked."""
+        if (t.shape != shape or t.dtype is not dtype or not t.is_contiguous()
+                or t.device != self.seq_lens.device):
+            raise ValueError(f"{name}: a contiguous {dtype} tensor {list(shape)} on the cache's "
+                             "device is needed")
+        return t.data_ptr()
+
+    def _attend_args(self, q, out, lse, softcap, slopes, first_key, prefix_len, n_new):
+        """Checked arguments of attend(): (T, address of q, out, its address, lse, its address,
+        SplaAttendOpts)."""
+        c, shape, dtype = self.cfg, q.shape, torch_dtype(self.cfg)
+        if len(shape) not in (3, 4):
+            raise ValueError("q: [T, batch, Hq, d] is needed")
+        T = shape[0] if len(shape) == 4 else 1
+        lead = (T, c.batch) if len(shape) == 4 else (c.batch,)
+        qp = self._given("q", q, lead + (c.n_q_heads, c.head_dim), dtype)
+        new = torch.empty if n_new is None else torch.zeros
+        if out is None:
+            out = new(shape, dtype=dtype, device=q.device)
+        if lse is None:
+            lse = new(shape[:-1], dtype=torch.float32, device=q.device)
+        op = self._given("out", out, shape, dtype)
+        lp = self._given("lse", lse, shape[:-1], torch.float32)
+        opts = SplaAttendOpts(softcap)
+        if slopes is not None:
+            opts.slopes = self._given("slopes", slopes, (c.n_q_heads,), torch.float32)
+        if first_key is not None:
+            opts.first_key = self._given("first_key", first_key, lead, torch.int32)
+        if prefix_len is not None:
+            opts.prefix_len = self._given("prefix_len", prefix_len, (c.batch,), torch.int32)
+        if n_new is not None:
+            opts.n_new = self._given("n_new", n_new, (c.batch,), torch.int32)
+        return T, qp, out, op, lse, lp, opts
+
+class SplaCache(_DeviceCache):
     """Device buffers of one SPLA cache, allocated with torch, plus the
     workspaces the calls need. Thin wrapper over the C ABI."""
 
@@ -441,23 +691,6 @@ class SplaCache:
     @property
     def struct(self) -> SplaCacheStruct:
         return self._struct
-
-    def device_errors(self) -> int:
-        """The SPLA_DEVERR_* bits the device has set in this cache's error
-        word (waits for the work queued on the current stream)."""
-        return int(self.err.item())
-
-    def clear_device_errors(self):
-        self.err.zero_()
-
-    def check_device_errors(self, allowed: int = 0):
-        """Raises SplaError when a bit outside `allowed` is set: after a
-        SPLA_DEVERR_SYNC the outputs of the call that set it are undefined."""
-        e = self.device_errors()
-        if e & ~allowed:
-            names = [n for n, v in (("CAPACITY", DEVERR_CAPACITY), ("SYNC", DEVERR_SYNC),
-                                    ("PAGE", DEVERR_PAGE)) if e & v]
-            raise SplaError(-5, "device error word: " + "|".join(names))
 
     def reset(self):
         _check(lib().spla_reset(ctypes.byref(self.cfg), ctypes.byref(self._struct),
@@ -563,36 +796,6 @@ class SplaCache:
                                      _stream(self.device)), "spla_prefill")
         return out, sel
 
-    def _workspace(self, kind, n, sizes, ws):
-        """The workspace ws, or a larger one in its place (zeros: its counters), for a call of
-        n tokens; the sizes of earlier calls are remembered. It grows by half at least, so that
-        calls that get longer one by one seldom make a new one, and one that a capture has used
-        is kept."""
-        need = self._ws_sizes.get((kind, n))
-        if need is None:
-            need = self._ws_sizes[kind, n] = sizes(self.cfg, n)
-        capturing = torch.cuda.is_current_stream_capturing()
-        if ws is None or ws.numel() < need:
-            if capturing:  # its zeros would come with a replay only
-                raise RuntimeError("a capture needs a call of its sizes ahead of it, which makes "
-                                   "the workspace")
-            if ws is not None:
-                need = max(need, ws.numel() * 3 // 2)
-                if ws.is_cuda:  # calls on this stream, not its own, may still use it
-                    ws.record_stream(torch.cuda.current_stream(ws.device))
-            ws = _aligned_workspace(need, self.device).zero_()
-        elif capturing and not any(ws is kept for kept in self._outgrown):
-            self._outgrown.append(ws)
-        return ws
-
-    def _given(self, name, t, shape, dtype):
-        """The address of t, checked."""
-        if (t.shape != shape or t.dtype is not dtype or not t.is_contiguous()
-                or t.device != self.seq_lens.device):
-            raise ValueError(f"{name}: a contiguous {dtype} tensor {list(shape)} on the cache's "
-                             "device is needed")
-        return t.data_ptr()
-
     def rotate(self, rope: SplaRope, q=None, k=None, positions=None, q_out=None, k_out=None,
                transpose=False):
         """rotate() of rows that stand at the positions after the tokens the cache holds (the
@@ -633,34 +836,21 @@ class SplaCache:
         every query sees. n_new int32 [batch]: the queries each sequence really has; the
         rows of out and lse past them are left as they are (zeros in tensors made here). Ahead
         of a graph capture a call of the same T makes the workspace."""
-        c, shape, dtype = self.cfg, q.shape, torch_dtype(self.cfg)
-        if len(shape) not in (3, 4):
-            raise ValueError("q: [T, batch, Hq, d] is needed")
-        T = shape[0] if len(shape) == 4 else 1
-        lead = (T, c.batch) if len(shape) == 4 else (c.batch,)
-        qp = self._given("q", q, lead + (c.n_q_heads, c.head_dim), dtype)
-        new = torch.empty if n_new is None else torch.zeros
-        if out is None:
-            out = new(shape, dtype=dtype, device=q.device)
-        if lse is None:
-            lse = new(shape[:-1], dtype=torch.float32, device=q.device)
-        op = self._given("out", out, shape, dtype)
-        lp = self._given("lse", lse, shape[:-1], torch.float32)
-        opts = SplaAttendOpts(softcap)
-        if slopes is not None:
-            opts.slopes = self._given("slopes", slopes, (c.n_q_heads,), torch.float32)
-        if first_key is not None:
-            opts.first_key = self._given("first_key", first_key, lead, torch.int32)
-        if prefix_len is not None:
-            opts.prefix_len = self._given("prefix_len", prefix_len, (c.batch,), torch.int32)
-        if n_new is not None:
-            opts.n_new = self._given("n_new", n_new, (c.batch,), torch.int32)
+        T, qp, out, op, lse, lp, opts = self._attend_args(q, out, lse, softcap, slopes, first_key,
+                                                          prefix_len, n_new)
         ws = self._attend_ws = self._workspace("attend", T, attend_workspace_bytes,
                                                self._attend_ws)
         _launch(lib().spla_attend, "spla_attend", self.device,
-                (ctypes.byref(c), ctypes.byref(self._struct), T, qp, ctypes.byref(opts), op, lp,
-                 ws.data_ptr(), ws.numel()))
+                (ctypes.byref(self.cfg), ctypes.byref(self._struct), T, qp, ctypes.byref(opts), op,
+                 lp, ws.data_ptr(), ws.numel()))
         return out, lse
+
+    def norm_rotate(self, rope: SplaRope, q=None, k=None, q_weight=None, k_weight=None, eps=1e-6,
+                    positions=None, q_out=None, k_out=None):
+        """norm_rotate() of rows that stand at the positions after the tokens the cache holds, or
+        at `positions`."""
+        return norm_rotate(self.cfg, rope, q, k, q_weight, k_weight, eps, positions,
+                           None if positions is not None else self.seq_lens, q_out, k_out)
 
     # ---- layout views (for checks; pure indexing) ----
     def stats_logical(self):
@@ -715,6 +905,116 @@ class SplaCache:
         c = self.cfg
         return (self.state.view(c.batch, c.n_kv_heads, c.head_dim, c.head_dim),
                 self.norm.view(c.batch, c.n_kv_heads, c.head_dim))
+
+
+class SplaCache8(_DeviceCache):
+    """Device buffers of one 8-bit cache for exact attention (codes, a power of two per block and
+    KV head, lengths), allocated with torch. Thin wrapper over the C ABI."""
+
+    def __init__(self, cfg: SplaConfig, device="cuda", block_table: Optional[torch.Tensor] = None):
+        """block_table: int32 [batch, max_seq_len / block_size] on the device, page of each block,
+        required when cfg.kv_pages > 0 (paged pool)."""
+        self.cfg = cfg
+        self.device = _indexed(device)
+        if (cfg.kv_pages > 0) != (block_table is not None):
+            raise ValueError("a block table goes with kv_pages > 0, and only then")
+        sz = cache8_bytes(cfg)
+        self.seq_lens = torch.zeros(cfg.batch, dtype=torch.int32, device=self.device)
+        if block_table is not None:
+            self._given("block_table", block_table,
+                        (cfg.batch, cfg.max_seq_len // cfg.block_size), torch.int32)
+        self.block_table = block_table
+        self.k = torch.zeros(sz[0], dtype=torch.uint8, device=self.device)
+        self.v = torch.zeros(sz[1], dtype=torch.uint8, device=self.device)
+        self.scales = torch.zeros(sz[2] // 4, dtype=torch.float32, device=self.device)
+        self.counters = torch.zeros(sz[4] // 4, dtype=torch.int32, device=self.device)
+        self.err = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._attend_ws = None
+        self._outgrown = []
+        self._ws_sizes = {}
+        self._struct = SplaCache8Struct(self.k.data_ptr(), self.v.data_ptr(),
+                                        self.scales.data_ptr(), self.seq_lens.data_ptr(),
+                                        self.counters.data_ptr(), self.err.data_ptr(),
+                                        None if block_table is None else block_table.data_ptr())
+
+    @property
+    def struct(self) -> SplaCache8Struct:
+        return self._struct
+
+    def reset(self):
+        _launch(lib().spla_reset8, "spla_reset8", self.device,
+                (ctypes.byref(self.cfg), ctypes.byref(self._struct)))
+
+    def _new_rows(self, name, x, shape):
+        """Address and row stride of new rows, checked."""
+        if (x.shape != shape or x.dtype is not torch_dtype(self.cfg)
+                or x.device != self.seq_lens.device):
+            raise ValueError(f"{name}: a {torch_dtype(self.cfg)} tensor {list(shape)} on the "
+                             "cache's device is needed")
+        return x.data_ptr(), _row_stride(x, shape[-2] * shape[-1])
+
+    def append(self, k_new: torch.Tensor, v_new: torch.Tensor,
+               n_new: Optional[torch.Tensor] = None):
+        """k_new, v_new: [T, batch, Hkv, d] (or [batch, Hkv, d]: one token) in the cfg's dtype, as
+        norm_rotate() and rotate() give them; rows may be slices of wider ones (a fused
+        projection's). n_new int32 [batch]: the tokens each sequence really has."""
+        c = self.cfg
+        if k_new.dim() not in (3, 4):
+            raise ValueError("k_new: [T, batch, Hkv, d] is needed")
+        T = k_new.shape[0] if k_new.dim() == 4 else 1
+        shape = k_new.shape[:-3] + (c.batch, c.n_kv_heads, c.head_dim)
+        kp, ks = self._new_rows("k_new", k_new, shape)
+        vp, vs = self._new_rows("v_new", v_new, shape)
+        np_ = None if n_new is None else self._given("n_new", n_new, (c.batch,), torch.int32)
+        _launch(lib().spla_append8, "spla_append8", self.device,
+                (ctypes.byref(c), ctypes.byref(self._struct), T, kp, ks, vp, vs, np_))
+
+    def read(self, n_tokens: int, first: Optional[torch.Tensor] = None, k_out=None, v_out=None):
+        """Keys and values [n_tokens, batch, Hkv, d], the numbers the cache holds of the tokens at
+        positions first[b] + t (first int32 [batch], or 0); zeros where a sequence holds none."""
+        c, dtype = self.cfg, torch_dtype(self.cfg)
+        shape = (int(n_tokens), c.batch, c.n_kv_heads, c.head_dim)
+        if n_tokens < 0:
+            raise ValueError("n_tokens: a count is needed")
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=dtype, device=self.device)
+        if v_out is None:
+            v_out = torch.empty(shape, dtype=dtype, device=self.device)
+        kp = self._given("k_out", k_out, shape, dtype)
+        vp = self._given("v_out", v_out, shape, dtype)
+        fp = None if first is None else self._given("first", first, (c.batch,), torch.int32)
+        _launch(lib().spla_read8, "spla_read8", self.device,
+                (ctypes.byref(c), ctypes.byref(self._struct), shape[0], fp, kp, vp))
+        return k_out, v_out
+
+    def rotate(self, rope: SplaRope, q=None, k=None, positions=None, q_out=None, k_out=None,
+               transpose=False):
+        """rotate() of rows that stand at the positions after the tokens the cache holds, or at
+        `positions`."""
+        return rotate(self.cfg, rope, q, k, positions, None if positions is not None
+                      else self.seq_lens, q_out, k_out, transpose)
+
+    def norm_rotate(self, rope: SplaRope, q=None, k=None, q_weight=None, k_weight=None, eps=1e-6,
+                    positions=None, q_out=None, k_out=None):
+        """norm_rotate() of rows that stand at the positions after the tokens the cache holds, or
+        at `positions`."""
+        return norm_rotate(self.cfg, rope, q, k, q_weight, k_weight, eps, positions,
+                           None if positions is not None else self.seq_lens, q_out, k_out)
+
+    def attend(self, q: torch.Tensor, out=None, lse=None, softcap=0.0, slopes=None,
+               first_key=None, prefix_len=None, n_new=None, window=0, sinks=0):
+        """Exact attention of the last T tokens of every sequence over the cache, as
+        SplaCache.attend; window > 0: the query at position p sees the keys after p - window, and
+        beside them the first `sinks` of the sequence (from first_key on where it is given)."""
+        T, qp, out, op, lse, lp, base = self._attend_args(q, out, lse, softcap, slopes, first_key,
+                                                          prefix_len, n_new)
+        opts = SplaAttend8Opts(base, window, sinks)
+        ws = self._attend_ws = self._workspace("attend8", T, attend8_workspace_bytes,
+                                               self._attend_ws)
+        _launch(lib().spla_attend8, "spla_attend8", self.device,
+                (ctypes.byref(self.cfg), ctypes.byref(self._struct), T, qp, ctypes.byref(opts), op,
+                 lp, ws.data_ptr(), ws.numel()))
+        return out, lse
 
 
 def make_events(phases: Sequence[str] = ("score", "select", "sparse", "merge", "decode",
