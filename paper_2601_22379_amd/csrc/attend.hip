@@ -15,31 +15,6 @@
 
 namespace spla {
 
-// Infinities and NaN among values that some query does not see: a zero weight
-// times such a value is NaN. They are taken out of the product, and a product of
-// marks with the queries' visibility says which queries see which: 1 for each +
-// infinity, 128 for each - infinity, 129 for each NaN (fewer than 128 per product).
-// odd_marks: the marks of a pair of bf16 values, which lose their odd ones.
-__device__ __forceinline__ uint32_t odd_marks(uint32_t& w) {
-  uint32_t fin = 0u, mark = 0u;
-#pragma unroll
-  for (int k = 0; k < 32; k += 16) {
-    const uint32_t b = (w >> k) & 0xFFFFu, mag = b & 0x7FFFu;
-    const uint32_t x = mag > 0x7F80u ? 0x4301u : b == 0x7F80u ? 0x3F80u : b == 0xFF80u ? 0x4300u : 0u;
-    mark |= x << k;
-    fin |= (mag < 0x7F80u ? b : 0u) << k;
-  }
-  w = fin;
-  return mark;
-}
-// What the values counted in n add to a sum.
-__device__ __forceinline__ float odd_sum(float n) {
-  const float neg = floorf(n * (1.f / 128.f));
-  float x = neg > 0.f ? -INFINITY : 0.f;
-  if (n - 128.f * neg > 0.f) x += INFINITY;
-  return x;
-}
-
 // ---- operands of a 32-token step on 16 x 16 tiles, straight from the cache
 // bf16 (v_mfma_f32_16x16x32_bf16): the cache holds a step in operand order, each
 // load one piece of 1 KiB. Score tile mt, row 4 a + i is token 8 a + 4 mt + i, so
@@ -360,8 +335,7 @@ __global__ __launch_bounds__(256, 2) void attend_stream_kernel(AttendArgs a) {
     if (st + 4 < last) slot = attend_slot(a, bh, (st + 4) >> sh);
     ps.step(st * 32, g);
   }
-  stream_finish<T, D>(a, seq, bh, tile, split, n_eff, ps.o, ps.mx, ps.sum(), ps.row.valid, s_m, s_l,
-                      s_o, s_last);
+  stream_finish<T, D>(a, seq, bh, tile, split, n_eff, ps, s_m, s_l, s_o, s_last);
 }
 
 // Many fp32 rows: 64 per workgroup, 16 per wavefront, and the keys and values by way of
@@ -455,155 +429,6 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a) {
 // group 2 e + h) lie one after the other over 16 coordinates. So LDS holds the
 // cache's bytes as they are, every operand read is runs of 512 bytes, and the
 // weights never leave their lane.
-template <int D>
-struct alignas(16) TileBuf {
-  uint4 k[D * 4];  // a step: 32 D elements
-  uint4 v[D * 4];
-};
-
-// kCapped: a cap that bounds all scores, no bias; kBiased: no cap, and no prefix; kGeneral:
-// any. (Packed documents, 2 x 4096 tokens of 32 heads: kBiased 137 us, kGeneral 178.)
-enum { kPlain = 0, kCapped = 1, kBiased = 2, kGeneral = 3 };
-
-// Up to this cap, scores of many rows do without the series of cap_score (1024 queries of 4
-// heads on each of 8 KV heads, 8000 tokens: 202 us without, 249 with it).
-constexpr float kSeriesCap = 64.f;
-
-template <int D, int KIND>
-struct TilePass {
-  static constexpr int KS = D / 16, CT = D / 32;
-  bf16x8 q[KS];
-  floatx16 o[CT];
-  float ref, l;       // reference of the weights (base 2), their sum (this lane's tokens)
-  int pos, lo, hi;    // this column's query
-  float mul, cap2, slope2;
-
-  // cap_score without its series (kCapped: less the reference), for caps up to kSeriesCap: off
-  // by c 2^-21, 2^-15 at most
-  __device__ __forceinline__ float capped(float z) const {
-    return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z) + 1.f),
-                KIND == kCapped ? 0.5f * cap2 : cap2);
-  }
-
-  // x[4 (2 mt + e) + b]: score of token 16 e + 8 h + 4 mt + b; here for h = 0
-  static __device__ __forceinline__ int token(int i) {
-    return 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3);
-  }
-
-  __device__ __forceinline__ void step(const TileBuf<D>& buf, int t0, bool inner, int lane) {
-    const int r = lane & 31, h = lane >> 5;
-    // pieces of this lane's score row and of its value coordinate: coordinates 16 s
-    // + 8 h .. + 7 at + 32 s, coordinate 32 c + r, tokens 16 e + 8 h .. at + 128 c + 32 e
-    const int at_k = (r >> 4) * (D * 2) + 16 * h + (r & 15), at_v = (r >> 4) * 64 + 16 * h + (r & 15);
-    floatx16 x = floatx16{};
-#pragma unroll
-    for (int s = 0; s < KS; ++s)
-      x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, buf.k[at_k + 32 * s]),
-                                                  q[s], x, 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    const float base = (float)(pos - t0 - 8 * h);
-    if constexpr (KIND == kBiased) {  // no token after the query's is seen: |p - j| = p - j
-      const float c = -slope2 * base;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = fmaf(x[i], mul, fmaf(slope2, (float)token(i), c));
-    }
-    if constexpr (KIND == kGeneral) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float y = x[i] * mul;
-        if (cap2 > kSeriesCap * kLog2e) y = cap_score(y, cap2);
-        else if (cap2 > 0.f) y = capped(y);
-        x[i] = fmaf(-slope2, fabsf(base - (float)token(i)), y);
-      }
-    }
-    if constexpr (KIND == kCapped) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = capped(x[i] * mul);
-    }
-    if (!inner) {
-      const uint32_t a = (uint32_t)(t0 + 8 * h - lo), n = (uint32_t)(hi - lo);
-#pragma unroll
-      for (int i = 0; i < 16; ++i)  // lo <= token < hi
-        x[i] = a + (uint32_t)token(i) < n ? x[i] : -INFINITY;
-    }
-    if constexpr (KIND != kCapped) {
-      float nm = x[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) nm = fmaxf(nm, x[i]);
-      nm = fmaxf(nm, xor32(nm));
-      if constexpr (KIND == kPlain) nm *= mul;
-      // the reference moves only when a score passes it by 2^8: weights up to there are as
-      // exact in bf16 and fp32, and the outputs are scaled a few times only (each query's
-      // by its own scores, so that no query's rounding hangs on another's)
-      const bool move = nm > ref + 8.f;
-      if (__any(move)) {
-        const float alpha = move ? rescale(ref, nm) : 1.f;
-        ref = move ? nm : ref;
-        l *= alpha;
-        scale_sums(alpha, [&](float f) {
-#pragma unroll
-          for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[c][i] *= f;
-        });
-      }
-    }
-    const float rf = ref == -INFINITY ? 0.f : ref;
-    bf16x8 p[2];
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float y = x[i];
-      const float w = __builtin_amdgcn_exp2f(KIND == kPlain ? fmaf(y, mul, -rf)
-                                             : KIND == kCapped ? y : y - rf);
-      sum += w;
-      // weights rounded to bf16 for the product (the sum keeps fp32): 2^-9 of each, beside the
-      // output's own rounding; a second term as in the tiles of 16 rows is half as many products
-      // again (8192 tokens: 764 us against 558)
-      p[(i >> 2) & 1][4 * (i >> 3) + (i & 3)] = (__bf16)w;
-    }
-    l += sum;
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int e = 0; e < 2; ++e)  // tokens 16 e .. + 15 of the step
-#pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        const uint4 a = buf.v[at_v + 128 * c + 32 * e];
-        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), p[e], o[c], 0,
-                                                       0, 0);
-      }
-  }
-
-  // What the infinities and NaN among a tile's values add to the queries that see them
-  // (see odd_marks), ahead of the product with the values without them.
-  __device__ __forceinline__ void odd_values(const TileBuf<D>& buf, int t0, int lane) {
-    const int r = lane & 31, h = lane >> 5;
-    const int at_v = (r >> 4) * 64 + 16 * h + (r & 15);
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      floatx16 n = floatx16{};
-#pragma unroll 1
-      for (int e = 0; e < 2; ++e) {
-        const uint4 v = buf.v[at_v + 128 * c + 32 * e];
-        uint32_t w[4] = {v.x, v.y, v.z, v.w}, u[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = odd_marks(w[i]);
-        bf16x8 seen;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int t = t0 + 16 * e + 8 * h + k;
-          seen[k] = (__bf16)(t >= lo && t < hi ? 1.f : 0.f);
-        }
-        n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), seen, n, 0, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[c][i] += odd_sum(n[i]);
-      asm volatile("" : "+v"(o[c]));  // done here, before the next coordinates' counts
-    }
-  }
-};
-
 template <int D, int KIND>
 __global__ __launch_bounds__(256, 3) void attend_tile_kernel(AttendArgs a) {
   __shared__ TileBuf<D> buf0, buf1;
@@ -623,7 +448,7 @@ __global__ __launch_bounds__(256, 3) void attend_tile_kernel(AttendArgs a) {
                        attend_q_at(a, (int64_t)tile * kTileRows + rr, bh) + 8 * h;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)
-      ps.q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + 16 * s));
+      ps.q[0][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + 16 * s));
   }
   const AttendSeq seq = attend_seq(a, bh);
   const AttendRow row = attend_row(a, seq, tile * kTileRows + rr, bh);
@@ -722,7 +547,7 @@ __global__ __launch_bounds__(256, 3) void attend_tile_kernel(AttendArgs a) {
 
   const int64_t u = (int64_t)bh * a.n_tiles + tile;
   if (a.join && split == 0 && tid == 0) a.n_eff[u] = n_eff;
-  tile_write<D>(a, row, bh, h, ps.o, ps.ref, ps.l, n_eff,
+  tile_write<bf16_t, D>(a, row, bh, h, ps.o, ps.ref, ps.l, n_eff,
                 (u * a.n_split + split) * kTileRows + rr);
 }
 

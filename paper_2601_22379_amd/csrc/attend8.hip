@@ -79,16 +79,6 @@ __device__ __forceinline__ float2 slot_scales(const Attend8Args& a, int64_t slot
   return make_float2(p[2 * slot], p[2 * slot + 1]);
 }
 
-// x as N bf16 terms, largest first.
-template <int N>
-__device__ __forceinline__ void split_bf16(float x, __bf16 (&t)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    t[i] = (__bf16)x;
-    x -= (float)t[i];
-  }
-}
-
 // ---- operands of a 32-token step on 16 x 16 x 32 tiles, straight from the cache. A key chunk
 // is 16 coordinates of one token, two products' worth; a value chunk 8 tokens of two coordinate
 // tiles. Tokens lie as in the bf16 cache's steps: score tile mt, row 4 a + i is token
@@ -326,8 +316,177 @@ __global__ __launch_bounds__(256, 2) void attend8_stream_kernel(Attend8Args a) {
     if (i + 4 < last) slot = attend_slot(a, bh, steps[i + 4] >> sh);
     ps.step(st * 32, g);
   }
-  stream_finish<T, D>(a, seq, bh, tile, split, n_eff, ps.o, ps.mx, ps.sum(), ps.row.valid, s_m, s_l,
-                      s_o, s_last);
+  stream_finish<T, D>(a, seq, bh, tile, split, n_eff, ps, s_m, s_l, s_o, s_last);
+}
+
+// ---------------------------------------------------------------- many rows
+// Calls of many query rows are bound by the matrix cores: a workgroup takes 128 rows, 32 per
+// wavefront, and a step's keys and values become bf16 once for all four: each thread loads its
+// chunks of the next step's codes while this one is used, then converts them into LDS, where the
+// step has the layout of the bf16 cache, and the products are those of its tiles.
+template <int D>
+struct StepCodes {  // a thread's chunks of a step: keys and values (d 64: one or the other)
+  static constexpr int N = D / 64;
+  uint4 c[N];
+  float2 scale;
+  __device__ __forceinline__ void load(const Attend8Args& a, int64_t slot, int tb, int tid) {
+    const int64_t o = (slot * a.m.B + tb) * D;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool val = D == 64 ? tid >= 128 : i == 1;
+      c[i] = reinterpret_cast<const uint4*>(static_cast<const char*>(val ? a.v : a.k) +
+                                            o)[D == 64 ? tid & 127 : tid];
+    }
+    scale = slot_scales(a, slot);
+  }
+  // Into buf; true where a value is NaN.
+  __device__ __forceinline__ bool store(TileBuf<D>& buf, int tid) const {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool val = D == 64 ? tid >= 128 : i == 1;
+      const uint4 w = c[i];
+      const float s = val ? scale.y : scale.x;
+      const uint4 lo = fp8_to_bf16(w.x, w.y, s), hi = fp8_to_bf16(w.z, w.w, s);
+      const int l = tid & 63, piece = (D == 64 ? tid & 127 : tid) >> 6;
+      if (val) {  // coordinate tiles 2 piece and 2 piece + 1
+        buf.v[128 * piece + l] = lo;
+        buf.v[128 * piece + 64 + l] = hi;
+        bad = (fp8_nan(w.x) | fp8_nan(w.y) | fp8_nan(w.z) | fp8_nan(w.w)) != 0u;
+      } else {  // 16 coordinates: 64 p + 16 g .. of token tile mt
+        const int mt = piece / (D / 64), p = piece % (D / 64);
+        uint4* k = buf.k + mt * 2 * D + 32 * (4 * p + (l >> 4)) + (l & 15);
+        k[0] = lo;
+        k[16] = hi;
+      }
+    }
+    return bad;
+  }
+};
+
+template <typename T, int D, int KIND, bool SINKS>
+__global__ __launch_bounds__(256, (std::is_same<T, float>::value ? 2 : 3)) void
+attend8_tile_kernel(Attend8Args a) {
+  constexpr int TERMS = std::is_same<T, float>::value ? 3 : 1;
+  __shared__ TileBuf<D> buf[2];
+  __shared__ int4 s_range[4];
+  __shared__ int2 s_sink[4];
+  __shared__ int s_odd[2][4];
+  const Dims& m = a.m;
+  const int bh = (int)(blockIdx.x % (unsigned)m.bh);
+  // tiles of late queries, which see the most keys, first
+  const int tile = a.n_tiles - 1 - (a.tile0 + (int)(blockIdx.x / (unsigned)m.bh));
+  const int split = (int)blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rr = w * 32 + (lane & 31), h = lane >> 5;  // this lane's row of the tile
+  TilePass<D, KIND, TERMS, SINKS> ps;
+  {  // the queries first: their loads wait for nothing
+    const T* qp = static_cast<const T*>(a.q) +
+                  attend_q_at(a, (int64_t)tile * kTileRows + rr, bh) + 8 * h;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      if constexpr (TERMS == 1) {
+        ps.q[0][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + 16 * s));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          __bf16 t[TERMS];
+          split_bf16<TERMS>((float)qp[16 * s + i], t);
+#pragma unroll
+          for (int n = 0; n < TERMS; ++n) ps.q[n][s][i] = t[n];
+        }
+      }
+    }
+  }
+  const AttendSeq seq = attend_seq(a, bh);
+  const Attend8Row row = attend8_row(a, seq, tile * kTileRows + rr, bh);
+  const bool any = row.hi > row.lo;
+  // keys of this wavefront's queries, and those that all of its (non-empty) ones see
+  const int lo_min = -cols_max<32>(any ? -row.lo : -INT32_MAX), hi_max = cols_max<32>(row.hi);
+  const int lo_max = cols_max<32>(any ? row.lo : 0);
+  const int hi_min = -cols_max<32>(any ? -row.hi : -INT32_MAX);
+  int slo_min = 0, shi_max = 0;
+  if constexpr (SINKS) {
+    slo_min = -cols_max<32>(row.shi > 0 ? -row.slo : -INT32_MAX);
+    shi_max = cols_max<32>(row.shi);
+  }
+  if (lane == 0) {
+    s_range[w] = make_int4(lo_min, hi_max, lo_max, hi_min);
+    s_sink[w] = make_int2(slo_min, shi_max);
+  }
+  __syncthreads();
+  int4 g = s_range[0];  // of the workgroup's
+  int2 gs = s_sink[0];
+#pragma unroll
+  for (int i = 1; i < 4; ++i) {
+    const int4 x = s_range[i];
+    g = make_int4(min(g.x, x.x), max(g.y, x.y), max(g.z, x.z), min(g.w, x.w));
+    gs = make_int2(min(gs.x, s_sink[i].x), max(gs.y, s_sink[i].y));
+  }
+  const int g_lo_max = __builtin_amdgcn_readfirstlane(g.z);
+  const int g_hi_min = __builtin_amdgcn_readfirstlane(g.w);
+  const StepList steps(__builtin_amdgcn_readfirstlane(g.x), __builtin_amdgcn_readfirstlane(g.y),
+                       __builtin_amdgcn_readfirstlane(gs.x), __builtin_amdgcn_readfirstlane(gs.y));
+  const int per = max((steps.n + a.n_split - 1) / a.n_split, kTileMinSplit);
+  const int n_eff = (steps.n + per - 1) / per;
+  if (split > 0 && split >= n_eff) return;
+  const int first = split * per, last = min(first + per, steps.n);
+
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) ps.o[c] = floatx16{};
+  const ScoreMap map(a, row.valid ? row.head : 0);
+  ps.mul = map.mul;
+  ps.cap2 = map.cap2;
+  ps.slope2 = map.slope2;
+  ps.ref = KIND == kCapped ? 0.5f * map.cap2 : -INFINITY;
+  ps.l = 0.f;
+  ps.pos = row.pos;
+  ps.lo = row.lo;
+  ps.hi = row.hi;
+  ps.slo = row.slo;
+  ps.shi = row.shi;
+
+  const int sh = m.B == 32 ? 0 : m.B == 64 ? 1 : 2;  // log2 of the steps per block
+  StepCodes<D> codes;
+  const auto load = [&](int st) {
+    codes.load(a, attend_slot(a, bh, st >> sh), (st & ((1 << sh) - 1)) * 32, tid);
+  };
+  if (first < last) load(steps[first]);
+#pragma unroll 1
+  for (int i = first; i < last; ++i) {
+    const int t0 = steps[i] * 32, x = (i - first) & 1;
+    const bool bad = codes.store(buf[x], tid);
+    // values that some query may not see (the same for all wavefronts)
+    const bool g_inner = t0 >= g_lo_max && t0 + 32 <= g_hi_min;
+    if (!g_inner) {
+      const bool one = __any(bad);
+      if (lane == 0) s_odd[x][w] = one;
+    }
+    __syncthreads();
+    if (i + 1 < last) load(steps[i + 1]);
+    if (__builtin_expect(!g_inner && (s_odd[x][0] | s_odd[x][1] | s_odd[x][2] | s_odd[x][3]), 0)) {
+      ps.odd_values(buf[x], t0, lane);  // (the same for all wavefronts)
+      __syncthreads();                  // then the values lose them
+      for (int c = tid; c < 4 * D; c += 256) {
+        uint4& v = buf[x].v[c];
+        uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) odd_marks(u[k]);
+        v = make_uint4(u[0], u[1], u[2], u[3]);
+      }
+      __syncthreads();
+    }
+    // nothing here for this wavefront
+    const bool out = t0 >= hi_max || t0 + 32 <= lo_min;
+    if (out && (!SINKS || t0 >= shi_max || t0 + 32 <= slo_min)) continue;
+    ps.step(buf[x], t0, t0 >= lo_max && t0 + 32 <= hi_min, lane);
+  }
+
+  const int64_t u = (int64_t)bh * a.n_tiles + tile;
+  if (a.join && split == 0 && tid == 0) a.n_eff[u] = n_eff;
+  tile_write<T, D>(a, row, bh, h, ps.o, ps.ref, ps.l, n_eff,
+                   (u * a.n_split + split) * kTileRows + rr);
 }
 
 static hipError_t attend8_launches(Attend8Args a, hipStream_t st) {
@@ -343,7 +502,29 @@ static hipError_t attend8_launches(Attend8Args a, hipStream_t st) {
                            static_cast<const AttendArgs&>(a));
     }
   };
-  if (a.m.elem == 4) {
+  const bool cap = a.o.softcap > 0.f, bias = a.o.slopes != nullptr;
+  const bool bounded = cap && !bias && a.o.softcap * kLog2e <= 60.f;  // (as over the bf16 cache)
+  const auto tile = [&](auto d, auto sinks) {
+    constexpr int D = decltype(d)::value;
+    constexpr bool S = decltype(sinks)::value;
+    if (a.m.elem == 4) {
+      if (cap || bias) go(attend8_tile_kernel<float, D, kGeneral, S>, attend_join_kernel<float, D>);
+      else go(attend8_tile_kernel<float, D, kPlain, S>, attend_join_kernel<float, D>);
+    } else if (bounded) {
+      go(attend8_tile_kernel<bf16_t, D, kCapped, S>, attend_join_kernel<bf16_t, D>);
+    } else if (cap || bias) {
+      go(attend8_tile_kernel<bf16_t, D, kGeneral, S>, attend_join_kernel<bf16_t, D>);
+    } else {
+      go(attend8_tile_kernel<bf16_t, D, kPlain, S>, attend_join_kernel<bf16_t, D>);
+    }
+  };
+  if (a.rows == kTileRows) {
+    const bool sinks = a.window > 0 && a.sinks > 0;
+    const std::integral_constant<int, 64> d64{};
+    const std::integral_constant<int, 128> d128{};
+    if (a.m.d == 64) sinks ? tile(d64, std::true_type{}) : tile(d64, std::false_type{});
+    else sinks ? tile(d128, std::true_type{}) : tile(d128, std::false_type{});
+  } else if (a.m.elem == 4) {
     if (a.m.d == 64) go(attend8_stream_kernel<float, 64>, attend_join_kernel<float, 64>);
     else go(attend8_stream_kernel<float, 128>, attend_join_kernel<float, 128>);
   } else {

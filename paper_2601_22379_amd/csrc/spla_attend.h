@@ -279,18 +279,19 @@ __device__ __forceinline__ void join_parts(float (&s_m)[16], float (&s_l)[16],
   }
 }
 
-// The end of a workgroup's split of a tile of 16 rows: the four wavefronts' sums o (coordinates
-// 16 t + 4 g .. of column j), references mx and weights' sums l joined, then written, or left as
-// a record that attend_join_kernel or the tile's last workgroup to arrive joins. valid: whether
-// this lane's column is a query.
-template <typename T, int D>
+// The end of a workgroup's split of a tile of 16 rows: the sums of its wavefronts' passes (ps.o:
+// coordinates 16 t + 4 g .. of column j, reference ps.mx, weights' sum ps.sum()) joined, then
+// written, or left as a record that attend_join_kernel or the tile's last workgroup to arrive
+// joins.
+template <typename T, int D, typename Pass>
 __device__ __forceinline__ void stream_finish(const AttendArgs& a, const AttendSeq& seq, int bh,
-                                              int tile, int split, int n_eff,
-                                              const floatx4 (&o)[D / 16], float mx, float l,
-                                              bool valid, float (&s_m)[4][16], float (&s_l)[4][16],
+                                              int tile, int split, int n_eff, const Pass& ps,
+                                              float (&s_m)[4][16], float (&s_l)[4][16],
                                               float (&s_o)[4][16][D + 4], int& s_last) {
   constexpr int OT = D / 16;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, j = lane & 15, g = lane >> 4;
+  const float l = ps.sum(), mx = ps.mx;
+  const auto& o = ps.o;
   if (g == 0) {
     s_m[w][j] = mx;
     s_l[w][j] = l;
@@ -347,7 +348,7 @@ __device__ __forceinline__ void stream_finish(const AttendArgs& a, const AttendS
   if (tid == 0) store_agent(ctr, 0);  // zero again for the next call
   // the valid rows are the first ones: R of them (a power of two) by 16 threads
   // each, in P = 16 / R parts that take every P-th record
-  const int nv = __popcll(__ballot(valid && lane < 16));
+  const int nv = __popcll(__ballot(ps.row.valid && lane < 16));
   int R = 1;
   while (R < nv) R *= 2;
   const int P = 16 / R, p = tid / (16 * R), jr = (tid >> 4) % R;
@@ -403,9 +404,215 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
+// x as N bf16 terms, largest first.
+template <int N>
+__device__ __forceinline__ void split_bf16(float x, __bf16 (&t)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    t[i] = (__bf16)x;
+    if (i + 1 < N) x -= (float)t[i];
+  }
+}
+
+// ---------------------------------------------------------------- many rows
+// Infinities and NaN among values that some query does not see: a zero weight
+// times such a value is NaN. They are taken out of the product, and a product of
+// marks with the queries' visibility says which queries see which: 1 for each +
+// infinity, 128 for each - infinity, 129 for each NaN (fewer than 128 per product).
+// odd_marks: the marks of a pair of bf16 values, which lose their odd ones.
+__device__ __forceinline__ uint32_t odd_marks(uint32_t& w) {
+  uint32_t fin = 0u, mark = 0u;
+#pragma unroll
+  for (int k = 0; k < 32; k += 16) {
+    const uint32_t b = (w >> k) & 0xFFFFu, mag = b & 0x7FFFu;
+    const uint32_t x = mag > 0x7F80u ? 0x4301u : b == 0x7F80u ? 0x3F80u : b == 0xFF80u ? 0x4300u : 0u;
+    mark |= x << k;
+    fin |= (mag < 0x7F80u ? b : 0u) << k;
+  }
+  w = fin;
+  return mark;
+}
+// What the values counted in n add to a sum.
+__device__ __forceinline__ float odd_sum(float n) {
+  const float neg = floorf(n * (1.f / 128.f));
+  float x = neg > 0.f ? -INFINITY : 0.f;
+  if (n - 128.f * neg > 0.f) x += INFINITY;
+  return x;
+}
+
+template <int D>
+struct alignas(16) TileBuf {
+  uint4 k[D * 4];  // a step: 32 D elements
+  uint4 v[D * 4];
+};
+
+// kCapped: a cap that bounds all scores, no bias; kBiased: no cap, and no prefix; kGeneral:
+// any. (Packed documents, 2 x 4096 tokens of 32 heads: kBiased 137 us, kGeneral 178.)
+enum { kPlain = 0, kCapped = 1, kBiased = 2, kGeneral = 3 };
+
+// Up to this cap, scores of many rows do without the series of cap_score (1024 queries of 4
+// heads on each of 8 KV heads, 8000 tokens: 202 us without, 249 with it).
+constexpr float kSeriesCap = 64.f;
+
+// TERMS: the bf16 terms that queries and weights go in with (3: all 24 bits of fp32 ones); SINKS:
+// a second run of keys, [slo, shi), for each query.
+template <int D, int KIND, int TERMS = 1, bool SINKS = false>
+struct TilePass {
+  static constexpr int KS = D / 16, CT = D / 32;
+  bf16x8 q[TERMS][KS];
+  floatx16 o[CT];
+  float ref, l;       // reference of the weights (base 2), their sum (this lane's tokens)
+  int pos, lo, hi;    // this column's query
+  int slo, shi;
+  float mul, cap2, slope2;
+
+  __device__ __forceinline__ bool sees(int t) const {
+    return (t >= lo && t < hi) || (SINKS && t >= slo && t < shi);
+  }
+
+  // cap_score without its series (kCapped: less the reference), for caps up to kSeriesCap: off
+  // by c 2^-21, 2^-15 at most
+  __device__ __forceinline__ float capped(float z) const {
+    return fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z) + 1.f),
+                KIND == kCapped ? 0.5f * cap2 : cap2);
+  }
+
+  // x[4 (2 mt + e) + b]: score of token 16 e + 8 h + 4 mt + b; here for h = 0
+  static __device__ __forceinline__ int token(int i) {
+    return 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3);
+  }
+
+  __device__ __forceinline__ void step(const TileBuf<D>& buf, int t0, bool inner, int lane) {
+    const int r = lane & 31, h = lane >> 5;
+    // pieces of this lane's score row and of its value coordinate: coordinates 16 s
+    // + 8 h .. + 7 at + 32 s, coordinate 32 c + r, tokens 16 e + 8 h .. at + 128 c + 32 e
+    const int at_k = (r >> 4) * (D * 2) + 16 * h + (r & 15), at_v = (r >> 4) * 64 + 16 * h + (r & 15);
+    floatx16 x = floatx16{};
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int n = TERMS - 1; n >= 0; --n)  // the smallest term first
+        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, buf.k[at_k + 32 * s]), q[n][s], x, 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    const float base = (float)(pos - t0 - 8 * h);
+    if constexpr (KIND == kBiased) {  // no token after the query's is seen: |p - j| = p - j
+      const float c = -slope2 * base;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = fmaf(x[i], mul, fmaf(slope2, (float)token(i), c));
+    }
+    if constexpr (KIND == kGeneral) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float y = x[i] * mul;
+        if (TERMS == 1 ? cap2 > kSeriesCap * kLog2e : cap2 > 0.f) y = cap_score(y, cap2);
+        else if (cap2 > 0.f) y = capped(y);
+        x[i] = fmaf(-slope2, fabsf(base - (float)token(i)), y);
+      }
+    }
+    if constexpr (KIND == kCapped) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = capped(x[i] * mul);
+    }
+    if (!inner) {
+      const uint32_t a = (uint32_t)(t0 + 8 * h - lo), n = (uint32_t)(hi - lo);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)  // lo <= token < hi
+        x[i] = a + (uint32_t)token(i) < n ||
+                       (SINKS && (uint32_t)(t0 + 8 * h + token(i) - slo) < (uint32_t)(shi - slo))
+                   ? x[i]
+                   : -INFINITY;
+    }
+    if constexpr (KIND != kCapped) {
+      float nm = x[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) nm = fmaxf(nm, x[i]);
+      nm = fmaxf(nm, xor32(nm));
+      if constexpr (KIND == kPlain) nm *= mul;
+      // the reference moves only when a score passes it by 2^8: weights up to there are as
+      // exact in bf16 and fp32, and the outputs are scaled a few times only (each query's
+      // by its own scores, so that no query's rounding hangs on another's)
+      const bool move = nm > ref + 8.f;
+      if (__any(move)) {
+        const float alpha = move ? rescale(ref, nm) : 1.f;
+        ref = move ? nm : ref;
+        l *= alpha;
+        scale_sums(alpha, [&](float f) {
+#pragma unroll
+          for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[c][i] *= f;
+        });
+      }
+    }
+    const float rf = ref == -INFINITY ? 0.f : ref;
+    bf16x8 p[TERMS][2];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float y = x[i];
+      const float w = __builtin_amdgcn_exp2f(KIND == kPlain ? fmaf(y, mul, -rf)
+                                             : KIND == kCapped ? y : y - rf);
+      sum += w;
+      // weights rounded to bf16 for the product (the sum keeps fp32): 2^-9 of each, beside the
+      // output's own rounding; a second term as in the tiles of 16 rows is half as many products
+      // again (8192 tokens: 764 us against 558)
+      if constexpr (TERMS == 1) {
+        p[0][(i >> 2) & 1][4 * (i >> 3) + (i & 3)] = (__bf16)w;
+      } else {
+        __bf16 term[TERMS];
+        split_bf16<TERMS>(w, term);
+#pragma unroll
+        for (int n = 0; n < TERMS; ++n) p[n][(i >> 2) & 1][4 * (i >> 3) + (i & 3)] = term[n];
+      }
+    }
+    l += sum;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)  // tokens 16 e .. + 15 of the step
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const uint4 a = buf.v[at_v + 128 * c + 32 * e];
+#pragma unroll
+        for (int n = TERMS - 1; n >= 0; --n)
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), p[n][e],
+                                                         o[c], 0, 0, 0);
+      }
+  }
+
+  // What the infinities and NaN among a tile's values add to the queries that see them
+  // (see odd_marks), ahead of the product with the values without them.
+  __device__ __forceinline__ void odd_values(const TileBuf<D>& buf, int t0, int lane) {
+    const int r = lane & 31, h = lane >> 5;
+    const int at_v = (r >> 4) * 64 + 16 * h + (r & 15);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      floatx16 n = floatx16{};
+#pragma unroll 1
+      for (int e = 0; e < 2; ++e) {
+        const uint4 v = buf.v[at_v + 128 * c + 32 * e];
+        uint32_t w[4] = {v.x, v.y, v.z, v.w}, u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = odd_marks(w[i]);
+        bf16x8 seen;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int t = t0 + 16 * e + 8 * h + k;
+          seen[k] = (__bf16)(sees(t) ? 1.f : 0.f);
+        }
+        n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, make_uint4(u[0], u[1], u[2], u[3])), seen, n, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[c][i] += odd_sum(n[i]);
+      asm volatile("" : "+v"(o[c]));  // done here, before the next coordinates' counts
+    }
+  }
+};
+
 // A lane's half of its column's outputs (unnormalised, o[c][4 i + k]: coordinate 32 c +
 // 8 i + 4 h + k) written out, or as record rec where the keys are split.
-template <int D>
+template <typename T, int D>
 __device__ __forceinline__ void tile_write(const AttendArgs& a, const AttendRow& row, int bh, int h,
                                            const floatx16 (&o)[D / 32], float ref, float lane_sum,
                                            int n_eff, int64_t rec) {
@@ -431,7 +638,7 @@ __device__ __forceinline__ void tile_write(const AttendArgs& a, const AttendRow&
       float y[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) y[k] = any ? o[c][4 * i + k] * inv : 0.f;
-      Elem<bf16_t>::store4(static_cast<bf16_t*>(a.out), at * D + 32 * c + 8 * i + 4 * h, y);
+      Elem<T>::store4(static_cast<T*>(a.out), at * D + 32 * c + 8 * i + 4 * h, y);
     }
   if (a.lse && h == 0) a.lse[at] = any ? (ref + log2f(l)) * kLn2 : -INFINITY;
 }

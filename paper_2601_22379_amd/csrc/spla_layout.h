@@ -565,9 +565,12 @@ SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
   return attend_ws_of(m, n_tokens, attend_rows(m, n_tokens));
 }
 
-// ---- exact attention over the 8-bit cache: tiles of 16 rows
+// ---- exact attention over the 8-bit cache: tiles of 16 rows, or of 128
+SPLA_HD int attend8_rows(const Dims& m, int n_tokens) {
+  return (int64_t)n_tokens * m.group <= 64 ? kAttendRows : kTileRows;
+}
 SPLA_HD AttendWs attend8_ws_layout(const Dims& m, int n_tokens) {
-  return attend_ws_of(m, n_tokens, kAttendRows);
+  return attend_ws_of(m, n_tokens, attend8_rows(m, n_tokens));
 }
 
 // Appends of up to so many blocks count their workgroups in the cache's counters, and the last

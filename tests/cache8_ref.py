@@ -111,8 +111,9 @@ def attention(q, k, v, pos, see, scale=None, softcap=0.0, slope=0.0, coarse_cap=
     # up to 3 parts of the query: 3 d + 4 at 2^-24 of the terms' magnitudes), 4 of the score's own
     # size and of the running maximum's, the cap within c 2^-21 (few rows, and caps above 64: and
     # within 2^-18 of itself), exp2 within 2 steps. A weight is off by that share of itself;
-    # weights in two bf16 terms are off by 2^-17 of themselves, in one by 2^-9; the sums of L
-    # weights take fp32 roundings; the output is rounded once.
+    # the sums of L weights take fp32 roundings; the output is rounded once. A weight enters its
+    # product in bf16 terms: half a step of bf16 is finfo.eps / 2 = 2^-8 of a number, so one term
+    # leaves up to 2^-8 of the weight, a second one 2^-8 of that rest, 2^-16, a third 2^-24.
     top = x.amax(-1, keepdim=True) if L else torch.zeros((T, 1), device=q.device)
     top = torch.where(top == -math.inf, torch.zeros_like(top), top)
     xa = torch.where(see, x, torch.zeros_like(x)).abs()
@@ -123,7 +124,7 @@ def attention(q, k, v, pos, see, scale=None, softcap=0.0, slope=0.0, coarse_cap=
         eps = eps + (cap if coarse_cap else torch.minimum(cap, 2.0 ** -18 * capped.abs()))
     eps = torch.where(see, eps, torch.zeros_like(eps))
     pe = p * (eps + min(L, 4096) * 2.0 ** -24)
-    weight = 0.0 if dt == torch.float32 else 2.0 ** -9 if one_term else 2.0 ** -17
+    weight = 2.0 ** -24 if dt == torch.float32 else 2.0 ** -8 if one_term else 2.0 ** -16
     va = vf.abs()
     tol = (pe + p * weight) @ va * 1.01 + out.abs() * (pe.sum(-1, keepdim=True) + HALF[dt]) * 1.01
     tol = tol + 1e-30
