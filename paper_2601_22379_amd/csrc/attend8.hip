@@ -364,9 +364,13 @@ struct StepCodes {  // a thread's chunks of a step: keys and values (d 64: one o
   }
 };
 
+// Workgroups per compute unit: three, where their registers suffice.
+template <typename T, int KIND, bool SINKS>
+constexpr int kTile8Wgs = std::is_same<T, float>::value || (SINKS && KIND >= kBiased) ? 2 : 3;
+
 template <typename T, int D, int KIND, bool SINKS>
-__global__ __launch_bounds__(256, (std::is_same<T, float>::value ? 2 : 3)) void
-attend8_tile_kernel(Attend8Args a) {
+__global__ __launch_bounds__(256, (kTile8Wgs<T, KIND, SINKS>)) void attend8_tile_kernel(
+    Attend8Args a) {
   constexpr int TERMS = std::is_same<T, float>::value ? 3 : 1;
   __shared__ TileBuf<D> buf[2];
   __shared__ int4 s_range[4];
@@ -512,8 +516,10 @@ static hipError_t attend8_launches(Attend8Args a, hipStream_t st) {
       else go(attend8_tile_kernel<float, D, kPlain, S>, attend_join_kernel<float, D>);
     } else if (bounded) {
       go(attend8_tile_kernel<bf16_t, D, kCapped, S>, attend_join_kernel<bf16_t, D>);
-    } else if (cap || bias) {
+    } else if (cap || (bias && a.o.prefix_len)) {
       go(attend8_tile_kernel<bf16_t, D, kGeneral, S>, attend_join_kernel<bf16_t, D>);
+    } else if (bias) {
+      go(attend8_tile_kernel<bf16_t, D, kBiased, S>, attend_join_kernel<bf16_t, D>);
     } else {
       go(attend8_tile_kernel<bf16_t, D, kPlain, S>, attend_join_kernel<bf16_t, D>);
     }

@@ -565,9 +565,21 @@ SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
   return attend_ws_of(m, n_tokens, attend_rows(m, n_tokens));
 }
 
-// ---- exact attention over the 8-bit cache: tiles of 16 rows, or of 128
+// ---- exact attention over the 8-bit cache: tiles of 16 rows (codes straight from the cache, made
+// bf16 by each wavefront for itself), or of 128 (made bf16 once, through LDS). With half the bytes
+// to read, tiles of 16 hold out longer than over the bf16 cache: until there are more than so
+// many (tile, 32-token step) pairs, 16 of which a step of 128 rows would save, though it takes
+// 1.1 us from codes to sums when it is alone. The lengths are on the device, so the capacity
+// counts. bf16, d 128: 16384 pairs 20.9 us, 24.5 in tiles of 128 (8 heads of 4096 tokens, 256
+// rows), 16.4 and 25.5 (32 of 1000), 32768 pairs 32.7 and 31.0 (one head of 32K, 512 rows),
+// 48000 pairs 51.4 and 35.3 (32 of 8000, 96 rows), 45.4 and 46.3 (32 of 16000, 40 rows); fp32, d
+// 64: 84000 pairs 39.4 and 41.7, 131072 pairs 79.0 and 64.8 (d 128: 110 and 108).
+constexpr int64_t kTile8Steps = 32768, kTile8StepsF32 = 98304;
 SPLA_HD int attend8_rows(const Dims& m, int n_tokens) {
-  return (int64_t)n_tokens * m.group <= 64 ? kAttendRows : kTileRows;
+  const int64_t rows = (int64_t)n_tokens * m.group;
+  const int64_t steps = ceil_div(rows, kAttendRows) * m.bh * (m.cap / kSubTokens);
+  return rows <= 64 || steps <= (m.elem == 2 ? kTile8Steps : kTile8StepsF32) ? kAttendRows
+                                                                             : kTileRows;
 }
 SPLA_HD AttendWs attend8_ws_layout(const Dims& m, int n_tokens) {
   return attend_ws_of(m, n_tokens, attend8_rows(m, n_tokens));

@@ -80,16 +80,32 @@ CASES = {
     "f32_rows_splits": ("f32", 128, 8, 2, 64, [2501, 0, 90], 25, False),
     "f32_splits": ("f32", 128, 4, 2, 64, [2800, 1, 70], 8, True),
 }
+
+
+def tile_cap(dtype, hkv, group, B, b, T):
+    """A capacity at which a call of T tokens goes by tiles of 128 rows (they are chosen by the
+    work that there may be)."""
+    pairs = 32768 if dtype == "bf16" else 98304
+    steps = pairs // (-(-T * group // 16) * b * hkv) + 1
+    return -(-steps * 32 // B) * B
+
+
 KINDS = ["causal", "softcap", "bias", "docs", "prefix", "ragged", "window", "window_sinks",
          "window_docs", "window_prefix", "all"]
 
 
+MANY = [n for n, c in CASES.items() if c[6] * c[2] // c[3] > 64]
+
+
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("name", list(CASES))
-def test_against_64_bits(dev, name, kind):
+@pytest.mark.parametrize("name,wide", [(n, False) for n in CASES] + [(n, True) for n in MANY])
+def test_against_64_bits(dev, name, wide, kind):
     dtype, d, hq, hkv, B, lens, T, paged = CASES[name]
-    cache, K, V = filled(dev, dtype, lens, hq, hkv, d, B, paged=paged, garbage=True)
     b = len(lens)
+    cap = tile_cap(dtype, hkv, hq // hkv, B, b, T) if wide else None
+    if cap is not None:
+        cap = max(cap, -(-max(lens) // B) * B)
+    cache, K, V = filled(dev, dtype, lens, hq, hkv, d, B, cap, paged=paged, garbage=True)
     q = randn(dev, dtype, T, b, hq, d, seed=3, scale=2.0)
     kw, ref = {}, {}
     if kind in ("softcap", "all"):
@@ -119,7 +135,7 @@ def test_against_64_bits(dev, name, kind):
     before = (out.clone(), lse.clone())
     got = cache.attend(q, out, lse, **kw)
     assert got[0] is out and got[1] is lse
-    many = dtype == "bf16" and T * (hq // hkv) > 64
+    many = dtype == "bf16" and wide
     C.check_attend(out, lse, q, K, V, lens, news, before=before, coarse_cap=many, one_term=many,
                    **ref)
 
@@ -127,33 +143,38 @@ def test_against_64_bits(dev, name, kind):
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (31, 4), (32, 32), (33, 200), (64, 1),
                                           (299, 4), (300, 0), (301, 7), (2 ** 31 - 1, 2 ** 31 - 1),
                                           (0, 9)])
-@pytest.mark.parametrize("T", [1, 16, 150])
-def test_windows(dev, T, window, sinks):
+@pytest.mark.parametrize("dtype,T,wide", [("bf16", 1, False), ("bf16", 16, False),
+                                          ("bf16", 150, False), ("bf16", 150, True),
+                                          ("f32", 3, False), ("f32", 150, True)])
+def test_windows(dev, dtype, T, wide, window, sinks):
     """Windows that end at, before and after borders of steps, blocks and sequences; sinks that
     touch and pass the window."""
     lens = [300, 31, 150]
-    cache, K, V = filled(dev, "bf16", lens, 4, 2, 128, 32, cap=512, paged=True)
-    q = randn(dev, "bf16", T, 3, 4, 128, seed=2, scale=2.0)
+    cap = tile_cap(dtype, 2, 2, 32, 3, T) if wide else 512
+    cache, K, V = filled(dev, dtype, lens, 4, 2, 128, 32, cap=cap, paged=True)
+    q = randn(dev, dtype, T, 3, 4, 128, seed=2, scale=2.0)
     news = [min(T, L) for L in lens]
     out, lse = cache.attend(q, n_new=ints(dev, news), window=window, sinks=sinks)
-    many = T > 32
+    many = dtype == "bf16" and wide
     C.check_attend(out, lse, q, K, V, lens, news, window=window, sinks=sinks, coarse_cap=many,
                    one_term=many)
 
 
-@pytest.mark.parametrize("dtype,T", [("bf16", 1), ("bf16", 70), ("f32", 3), ("f32", 60)])
-def test_unseen_nan_stays_out(dev, dtype, T):
+@pytest.mark.parametrize("dtype,T,wide", [("bf16", 1, False), ("bf16", 70, False),
+                                          ("bf16", 70, True), ("f32", 3, False),
+                                          ("f32", 60, False), ("f32", 60, True)])
+def test_unseen_nan_stays_out(dev, dtype, T, wide):
     """NaN in keys and values that a query does not see leave it alone; in values that it sees they
     reach it, and only that coordinate."""
     B, d, L = 32, 64, 200
-    cfg = spla.make_config(1, 4, 2, d, B, 8, 224, dtype)
+    cap = tile_cap(dtype, 2, 2, B, 1, T) if wide else 224
+    cfg = spla.make_config(1, 4, 2, d, B, 8, cap, dtype)
     cache = spla.SplaCache8(cfg, dev)
     k, v = (randn(dev, dtype, L, 1, 2, d, seed=s) for s in (1, 2))
     k[20:40] = math.nan  # hidden by the window of every query
     v[25:45] = math.inf
     v[L - 1, 0, 0, 5] = math.nan  # seen by the last query alone
     cache.append(k, v)
-    cache.v.view(-1)[:] = cache.v  # (buffers past the length hold zeros)
     K, V = (x.double().permute(1, 2, 0, 3) for x in cache.read(L))
     q = randn(dev, dtype, T, 1, 4, d, seed=3)
     out, lse = cache.attend(q, window=60, sinks=4)
@@ -164,7 +185,7 @@ def test_unseen_nan_stays_out(dev, dtype, T):
     Kz, Vz = torch.nan_to_num(K), torch.nan_to_num(V)
     ok = out.clone()
     ok[T - 1, 0, :2, 5] = 0.0
-    many = dtype == "bf16" and T > 32
+    many = dtype == "bf16" and wide
     # the last query's hit coordinate is taken from the reference itself
     pos, see = C.visible(L, T, None, 0, 60, 4)
     for m in range(4):
@@ -183,25 +204,25 @@ def test_extreme_values(dev):
     v[:64] *= 2.0 ** 90
     v[64:128] *= 2.0 ** -90
     k[128:192] *= 2.0 ** -60
-    cfg = spla.make_config(1, 4, 1, 128, 64, 8, 256, "bf16")
-    cache = spla.SplaCache8(cfg, dev)
-    cache.append(k, v)
-    K, V = (x.double().permute(1, 2, 0, 3) for x in cache.read(256))
-    for T in (1, 40):
+    for T, wide in ((1, False), (40, False), (40, True)):
+        cap = tile_cap("bf16", 1, 4, 64, 1, T) if wide else 256
+        cache = spla.SplaCache8(spla.make_config(1, 4, 1, 128, 64, 8, cap, "bf16"), dev)
+        cache.append(k, v)
+        K, V = (x.double().permute(1, 2, 0, 3) for x in cache.read(256))
         q = randn(dev, "bf16", T, 1, 4, 128, seed=3)
         out, lse = cache.attend(q)
-        C.check_attend(out, lse, q, K, V, [256], one_term=T > 16, coarse_cap=T > 16)
+        C.check_attend(out, lse, q, K, V, [256], one_term=wide, coarse_cap=wide)
         out, lse = cache.attend(q, window=100, sinks=2)
-        C.check_attend(out, lse, q, K, V, [256], one_term=T > 16, coarse_cap=T > 16, window=100,
+        C.check_attend(out, lse, q, K, V, [256], one_term=wide, coarse_cap=wide, window=100,
                        sinks=2)
 
 
-@pytest.mark.parametrize("T", [1, 5, 90])
-def test_captured_replays(dev, T):
+@pytest.mark.parametrize("T,cap", [(1, 2048), (5, 2048), (90, 2048), (90, 65536)])
+def test_captured_replays(dev, T, cap):
     """One graph with an append and an attention, replayed between eager calls of other sizes;
     two graphs share the cache's workspace."""
     lens = [700, 300]
-    cache, _, _ = filled(dev, "bf16", lens, 8, 2, 128, 64, cap=2048, paged=True)
+    cache, _, _ = filled(dev, "bf16", lens, 8, 2, 128, 64, cap=cap, paged=True)
     q, q2 = (randn(dev, "bf16", t, 2, 8, 128, seed=5) for t in (T, 2 * T))
     k = randn(dev, "bf16", T, 2, 2, 128, seed=6)
     outs = [torch.empty_like(q), torch.empty_like(q2)]
@@ -224,8 +245,9 @@ def test_captured_replays(dev, T):
     assert cache.seq_lens.tolist() == [L + 4 * T for L in lens]
 
 
-def test_repeats_bit_for_bit(dev):
-    cache, _, _ = filled(dev, "bf16", [5000, 1234], 8, 2, 128, 64)
+@pytest.mark.parametrize("cap", [None, 65536])
+def test_repeats_bit_for_bit(dev, cap):
+    cache, _, _ = filled(dev, "bf16", [5000, 1234], 8, 2, 128, 64, cap)
     for T in (1, 9, 200):
         q = randn(dev, "bf16", T, 2, 8, 128, seed=5)
         a, la = cache.attend(q, window=2000, sinks=4)
@@ -277,11 +299,9 @@ def test_served_sequence(dev):
         cache.append(kr, v, ints(dev, n))
         K.append(kr.cpu(), n, start)
         V.append(v.cpu(), n, start)
-        many = T * (hq // hkv) > 64
         for window, sinks in ((0, 0), (48, 4)):
             out, lse = cache.attend(qr, n_new=ints(dev, n), window=window, sinks=sinks)
-            C.check_attend(out, lse, qr, K.x, V.x, K.lens, n, window=window, sinks=sinks,
-                           coarse_cap=many, one_term=many)
+            C.check_attend(out, lse, qr, K.x, V.x, K.lens, n, window=window, sinks=sinks)
     # handed on: a 16-bit cache that attends alike
     k, v = cache.read(max(K.lens))
     cfg16 = spla.make_config(b, hq, hkv, d, B, 8, cap, "bf16")
@@ -293,3 +313,15 @@ def test_served_sequence(dev):
     C.check_attend(out8[None], lse8[None], q[None], K.x, V.x, K.lens)
     out16, lse16 = other.attend(q)
     C.check_attend(out16[None], lse16[None], q[None], K.x, V.x, K.lens)
+
+
+def test_tile_rule_is_the_librarys(dev):
+    """The capacities that tile_cap gives do reach the tiles of 128 rows: their workspaces have
+    room for records of 128 rows."""
+    for dtype, T in (("bf16", 70), ("f32", 60)):
+        cap = tile_cap(dtype, 2, 2, 32, 1, T)
+        small, large = (spla.attend8_workspace_bytes(
+            spla.make_config(1, 4, 2, 64, 32, 8, c, dtype), T) for c in (cap - 64, cap))
+        rows = 128 * -(-T * 2 // 128) * 2  # of the call
+        split = min(128, 768 // (rows // 128), cap // 512)
+        assert large >= rows * split * 66 * 4 and large != small
