@@ -335,7 +335,8 @@ __global__ __launch_bounds__(256, 2) void attend_stream_kernel(AttendArgs a) {
     if (st + 4 < last) slot = attend_slot(a, bh, (st + 4) >> sh);
     ps.step(st * 32, g);
   }
-  stream_finish<T, D>(a, seq, bh, tile, split, n_eff, ps, s_m, s_l, s_o, s_last);
+  const int64_t rec0 = ((int64_t)bh * a.n_tiles + tile) * a.n_split * kAttendRows;
+  stream_finish<T, D>(a, seq, bh, tile, split, n_eff, rec0, ps, s_m, s_l, s_o, s_last);
 }
 
 // Many fp32 rows: 64 per workgroup, 16 per wavefront, and the keys and values by way of

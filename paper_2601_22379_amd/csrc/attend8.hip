@@ -18,6 +18,8 @@ namespace spla {
 struct Attend8Args : AttendArgs {
   const float* scales;  // [slots][2]
   int window, sinks;    // 0: no window (and no sinks)
+  int shares;           // workgroups of attend8_stream_kernel that share all keys evenly; 0: n_split
+                        // for each tile
 };
 
 // One query row: its main run [lo, hi) and the sinks [slo, shi) before it, shi <= lo (none:
@@ -288,6 +290,57 @@ struct Stream8Pass {
   }
 };
 
+// A workgroup's part of the call: split `split` of up to n_split of a tile's steps, its records
+// from rec0 on.
+struct Part8 {
+  int bh, tile, split, n_split;  // bh < 0: nothing
+  int64_t rec0;
+};
+__device__ __forceinline__ int ceil_ratio(int a, int b, float inv_b) {  // a < 2^24
+  int k = (int)((float)a * inv_b);  // off by one at most
+  k += k * b < a ? 1 : 0;
+  return k - ((k - 1) * b >= a ? 1 : 0);
+}
+// Shared evenly: with `per` steps to a workgroup, ceil(steps / per) of them go to each tile of a
+// sequence, in the order of the sequences; per is the least (to 3 %) that leaves as many
+// workgroups as fill the chip, for one more would wait for a compute unit of its own or share
+// one that has two already. (16 sequences of 16K to 65K tokens, 8 KV heads, 4 splits for each:
+// the longest ones' workgroups end long after the others.) The steps are estimated by
+// the length and the window; the tile's own are what is split.
+__device__ __forceinline__ Part8 share_part(const Attend8Args& a, int x) {
+  const int lane = threadIdx.x & 63, batch = a.m.batch;
+  const int units = a.m.hkv * a.n_tiles;  // of a sequence
+  int len = a.seq_lens[min(lane, batch - 1)];
+  len = min(max(len, 0), a.m.cap);
+  if (a.window > 0) len = (int)min((int64_t)len, (int64_t)a.window + a.sinks + a.n_tokens + 32);
+  const int est = lane < batch ? max((len + 31) / 32, 1) : 0;
+  const int total = (int)lane_u32(wave_incl_scan_u32((uint32_t)est), 63);
+  const int fill = max(kAttendFill / units, batch);  // workgroups of one head and tile
+  // each lane tries a size
+  const int least = max((total + fill - 1) / fill, kAttendMinSteps);
+  const float f = lane < 32 ? 1.f + lane * (1.f / 32.f) : __builtin_amdgcn_exp2f((lane - 28) * 0.25f);
+  const int size = min((int)((float)least * f), total);
+  const float inv = 1.f / (float)size;
+  int sum = 0;
+  for (int b = 0; b < batch; ++b) sum += ceil_ratio((int)lane_u32(est, b), size, inv);
+  const uint64_t fits = __ballot(sum <= fill);
+  const int per = fits ? (int)lane_u32(size, __builtin_ctzll(fits)) : total;
+  const int n = est ? min((est + per - 1) / per, a.n_split) : 0;
+  const uint32_t end = wave_incl_scan_u32((uint32_t)(n * units));
+  const uint64_t after = __ballot(end > (uint32_t)x);
+  Part8 p;
+  p.bh = -1;
+  if (after == 0) return p;
+  const int b = __builtin_ctzll(after);
+  p.n_split = (int)lane_u32(n, b);
+  const int i = x - ((int)lane_u32(end, b) - p.n_split * units), u = i / p.n_split;
+  p.split = i - u * p.n_split;
+  p.tile = u / a.m.hkv;
+  p.bh = b * a.m.hkv + u - p.tile * a.m.hkv;
+  p.rec0 = (int64_t)(x - p.split) * kAttendRows;
+  return p;
+}
+
 // A tile of 16 query rows; the four wavefronts take every fourth 32-token step of
 // this split's keys and are joined at the end.
 template <typename T, int D>
@@ -296,13 +349,23 @@ __global__ __launch_bounds__(256, 2) void attend8_stream_kernel(Attend8Args a) {
   __shared__ __align__(16) float s_o[4][16][D + 4];
   __shared__ int s_last;
   const Dims& m = a.m;
-  const int bh = (int)(blockIdx.x % (unsigned)m.bh);
-  const int tile = a.tile0 + (int)(blockIdx.x / (unsigned)m.bh), split = (int)blockIdx.y;
+  Part8 part;
+  if (a.shares > 0) {
+    part = share_part(a, (int)blockIdx.x);
+    if (part.bh < 0) return;
+  } else {
+    part.bh = (int)(blockIdx.x % (unsigned)m.bh);
+    part.tile = a.tile0 + (int)(blockIdx.x / (unsigned)m.bh);
+    part.split = (int)blockIdx.y;
+    part.n_split = a.n_split;
+    part.rec0 = ((int64_t)part.bh * a.n_tiles + part.tile) * a.n_split * kAttendRows;
+  }
+  const int bh = part.bh, tile = part.tile, split = part.split;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4;
   Stream8Pass<T, D> ps(a, bh, (int64_t)tile * kAttendRows, lane);
   const AttendSeq seq = attend_seq(a, bh);
   const StepList steps(ps.lo_min, ps.hi_max, ps.slo_min, ps.shi_max);
-  const int per = max((steps.n + a.n_split - 1) / a.n_split, kAttendMinSteps);
+  const int per = max((steps.n + part.n_split - 1) / part.n_split, kAttendMinSteps);
   const int n_eff = (steps.n + per - 1) / per;
   if (split > 0 && split >= n_eff) return;
   const int first = split * per, last = min(first + per, steps.n);
@@ -316,7 +379,7 @@ __global__ __launch_bounds__(256, 2) void attend8_stream_kernel(Attend8Args a) {
     if (i + 4 < last) slot = attend_slot(a, bh, steps[i + 4] >> sh);
     ps.step(st * 32, g);
   }
-  stream_finish<T, D>(a, seq, bh, tile, split, n_eff, ps, s_m, s_l, s_o, s_last);
+  stream_finish<T, D>(a, seq, bh, tile, split, n_eff, part.rec0, ps, s_m, s_l, s_o, s_last);
 }
 
 // ---------------------------------------------------------------- many rows
@@ -495,6 +558,10 @@ __global__ __launch_bounds__(256, (kTile8Wgs<T, KIND, SINKS>)) void attend8_tile
 
 static hipError_t attend8_launches(Attend8Args a, hipStream_t st) {
   const auto go = [&](void (*kern)(Attend8Args), void (*join)(AttendArgs)) {
+    if (a.shares > 0) {
+      hipLaunchKernelGGL(kern, dim3((unsigned)a.shares), dim3(256), 0, st, a);
+      return;
+    }
     // a grid holds 2^32 threads: very long calls take several launches
     const int most = (int)((1 << 20) / a.m.bh) > 0 ? (1 << 20) / a.m.bh : 1;
     for (a.tile0 = 0; a.tile0 < a.n_tiles; a.tile0 += most) {
@@ -551,6 +618,7 @@ hipError_t launch_attend8(const Dims& m, const spla_config& cfg, const spla_cach
   a.scales = c.scales;
   a.window = opts.window < m.cap ? opts.window : 0;  // one that reaches all there can be: none
   a.sinks = opts.sinks < m.cap ? opts.sinks : m.cap;
+  a.shares = ws.shares;
   return attend8_launches(a, st);
 }
 

@@ -281,11 +281,12 @@ __device__ __forceinline__ void join_parts(float (&s_m)[16], float (&s_l)[16],
 
 // The end of a workgroup's split of a tile of 16 rows: the sums of its wavefronts' passes (ps.o:
 // coordinates 16 t + 4 g .. of column j, reference ps.mx, weights' sum ps.sum()) joined, then
-// written, or left as a record that attend_join_kernel or the tile's last workgroup to arrive
-// joins.
+// written, or left as a record (the split-th after rec0, the first of the tile's) that
+// attend_join_kernel or the tile's last workgroup to arrive joins.
 template <typename T, int D, typename Pass>
 __device__ __forceinline__ void stream_finish(const AttendArgs& a, const AttendSeq& seq, int bh,
-                                              int tile, int split, int n_eff, const Pass& ps,
+                                              int tile, int split, int n_eff, int64_t rec0,
+                                              const Pass& ps,
                                               float (&s_m)[4][16], float (&s_l)[4][16],
                                               float (&s_o)[4][16][D + 4], int& s_last) {
   constexpr int OT = D / 16;
@@ -324,7 +325,7 @@ __device__ __forceinline__ void stream_finish(const AttendArgs& a, const AttendS
     attend_write<T, D>(a, out_row, bh, c0, y, mt, lt);
     return;
   }
-  const int64_t u = (int64_t)bh * a.n_tiles + tile, rec0 = u * a.n_split * kAttendRows;
+  const int64_t u = (int64_t)bh * a.n_tiles + tile;
   const int64_t rec = rec0 + (int64_t)split * kAttendRows + r;
   if (a.join) {  // attend_join_kernel joins the records
     if (!out_row.valid) return;

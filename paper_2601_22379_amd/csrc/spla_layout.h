@@ -521,7 +521,10 @@ struct AttendWs {
                   //   last workgroup of the tile joins)
   // the arrival counters of split tiles of 16 rows lie first, one per line, wherever
   // the rest ends: zero between calls of any shape (i32 [kTileFill][kSyncLine])
-  int64_t part;   // f32 [bh][n_tiles][n_split][rows][d]  unnormalised outputs
+  int shares;     // 8-bit cache: workgroups that share all sequences' keys evenly (0: each tile's
+                  //   keys go to n_split of its own)
+  int64_t part;   // f32 [bh][n_tiles][n_split][rows][d]  unnormalised outputs (shares: [shares]
+                  //   [rows][d])
   int64_t ml;     // f32 [bh][n_tiles][n_split][rows][2]  reference (base 2) and sum of the weights
   int64_t n_eff;  // i32 [bh][n_tiles]  with join: splits with a record (1: none, the output is
                   //   written)
@@ -532,6 +535,7 @@ struct AttendWs {
 SPLA_HD AttendWs attend_ws_of(const Dims& m, int n_tokens, int rows_per_tile) {
   AttendWs w;
   w.rows = rows_per_tile;
+  w.shares = 0;
   const bool wide = w.rows != kAttendRows;
   w.n_tiles = (int)ceil_div((int64_t)n_tokens * m.group, w.rows);
   const int64_t wgs = (int64_t)m.bh * w.n_tiles;
@@ -581,8 +585,31 @@ SPLA_HD int attend8_rows(const Dims& m, int n_tokens) {
   return rows <= 64 || steps <= (m.elem == 2 ? kTile8Steps : kTile8StepsF32) ? kAttendRows
                                                                              : kTileRows;
 }
+// Few rows of several sequences: a long one's keys go to more workgroups than a short one's (16
+// sequences of 16K to 65K tokens, 8 KV heads: 283 us with 4 workgroups for each, 247 shared).
+// Every workgroup finds its share from all lengths, a lane for each, hence at most 64; that takes
+// 1 us for 16 of them and 4 for 64 (64 of 2000 tokens, 8 heads: 43.9 us, 50.0 shared; 4 of 8000:
+// 18.7 and 20.9), so it is left out where there are few splits or (at capacity) few steps in each.
+constexpr int kShareBatch = 64, kShareSplits = 4, kShareSteps = 64;
+// Records that a tile's last workgroup joins at most (rows times splits).
+constexpr int kShareJoin = 512;
+
 SPLA_HD AttendWs attend8_ws_layout(const Dims& m, int n_tokens) {
-  return attend_ws_of(m, n_tokens, attend8_rows(m, n_tokens));
+  AttendWs w = attend_ws_of(m, n_tokens, attend8_rows(m, n_tokens));
+  const int64_t units = (int64_t)m.bh * w.n_tiles;
+  if (w.rows != kAttendRows || m.batch < 2 || m.batch > kShareBatch || n_tokens == 0 ||
+      units > kAttendFill / kShareSplits || m.cap / kSubTokens < kShareSteps * w.n_split)
+    return w;
+  int rows = 1;
+  while (rows < kAttendRows && rows < (int64_t)n_tokens * m.group) rows *= 2;
+  w.shares = kAttendFill;
+  w.n_split = kShareJoin / rows < kAttendMaxSplit ? kShareJoin / rows : kAttendMaxSplit;
+  w.join = 0;
+  w.part = (int64_t)kTileFill * kSyncLine * 4;  // behind the counters
+  w.ml = align_up(w.part + (int64_t)w.shares * w.rows * m.d * 4, SPLA_WORKSPACE_ALIGN);
+  w.n_eff = w.total =
+      align_up(w.ml + (int64_t)w.shares * w.rows * 2 * 4, SPLA_WORKSPACE_ALIGN);
+  return w;
 }
 
 // Appends of up to so many blocks count their workgroups in the cache's counters, and the last

@@ -325,3 +325,36 @@ def test_tile_rule_is_the_librarys(dev):
         rows = 128 * -(-T * 2 // 128) * 2  # of the call
         split = min(128, 768 // (rows // 128), cap // 512)
         assert large >= rows * split * 66 * 4 and large != small
+
+
+@pytest.mark.parametrize("kind", ["causal", "window", "docs", "ragged"])
+@pytest.mark.parametrize("dtype,d,b,hkv,group,T,top,cap", [
+    ("bf16", 128, 16, 8, 2, 1, 8192, 8192), ("bf16", 64, 2, 8, 4, 4, 9000, 65536),
+    ("bf16", 128, 3, 2, 16, 1, 12000, 360448), ("f32", 64, 5, 4, 1, 7, 3000, 106496),
+    ("bf16", 64, 40, 1, 4, 9, 2000, 32768), ("bf16", 128, 2, 4, 5, 12, 2500, 32768)])
+def test_shared_lengths(dev, dtype, d, b, hkv, group, T, top, cap, kind):
+    """Batches whose long sequences take more workgroups than their short ones."""
+    g = torch.Generator().manual_seed(b)
+    lens = [int(x) for x in torch.randint(0, top // 8, (b,), generator=g)]
+    lens[0], lens[-1], lens[b // 2] = top, min(lens[-1], 1), top if b > 4 else lens[b // 2]
+    cfg = spla.make_config(b, hkv * group, hkv, d, 64, 8, cap, dtype)
+    # the workspace is that of 512 shares: counters, a record of 16 rows for each
+    assert spla.attend8_workspace_bytes(cfg, T) == 768 * 128 + 512 * 16 * (d + 2) * 4
+    cache, K, V = filled(dev, dtype, lens, hkv * group, hkv, d, 64, cap)
+    q = randn(dev, dtype, T, b, hkv * group, d, seed=3, scale=2.0)
+    news = [min(T, L) for L in lens]
+    kw, ref = {}, {}
+    if kind == "window":
+        kw = ref = dict(window=700, sinks=4)
+    if kind == "docs":
+        f = torch.randint(0, top, (T, b), generator=g).int()
+        kw, ref = dict(first_key=f.to(dev)), dict(first=f)
+    if kind == "ragged":
+        news = [min(L, i % (T + 1)) for i, L in enumerate(lens)]
+    out = randn(dev, dtype, T, b, hkv * group, d, seed=8)
+    lse = randn(dev, "f32", T, b, hkv * group, seed=9)
+    before = (out.clone(), lse.clone())
+    cache.attend(q, out, lse, n_new=ints(dev, news), **kw)
+    C.check_attend(out, lse, q, K, V, lens, news, before=before, **ref)
+    again = cache.attend(q, before[0].clone(), before[1].clone(), n_new=ints(dev, news), **kw)
+    assert torch.equal(again[0], out) and torch.equal(again[1], lse)
