@@ -616,8 +616,10 @@ int32_t spla_attend(const spla_config* cfg, const spla_cache* cache, int32_t n_t
  *  q_weight, k_weight: device fp32, or NULL (ones): [Hq][d] and [Hkv][d] with
  *              weight_per_head = 1, [d] for all heads with 0. 16-byte aligned.
  *  eps:        finite, >= 0 (a row of zeros with eps = 0 gives NaN).
- * The other arguments as spla_rotate; in place (q_out = q) too. Sums, norms and
- * products are fp64, each result is rounded to fp32, then to the element type. */
+ * The other arguments as spla_rotate; in place (q_out = q) too. Sums of squares
+ * and angles are fp64; the rest is fp64 for fp32 rows, rounded once, and fp32 for bf16
+ * rows (within 2^-19 of the head's largest result, then rounded to bf16; the root above
+ * then between 2^-120 and 2^120). */
 int32_t spla_norm_rotate(const spla_config* cfg, const spla_rope* rope, int32_t n_tokens,
                          const int32_t* positions, const int32_t* seq_lens,
                          const float* q_weight, const float* k_weight, int32_t weight_per_head,
@@ -633,7 +635,8 @@ int32_t spla_norm_rotate(const spla_config* cfg, const spla_rope* rope, int32_t 
  *                   allowed.
  *  q_weight_grad, k_weight_grad: device fp32, shaped as the weights, or NULL (not
  *                   needed); the sum over all rows (and, with weight_per_head = 0, heads),
- *                   in fp64 and in a fixed order. Zeros where there are no rows.
+ *                   in fp64 (for bf16 rows, four at a time in fp32) and in a fixed order.
+ *                   Zeros where there are no rows.
  *  workspace:       at least spla_norm_rotate_grad_workspace_bytes(cfg, n_tokens) bytes,
  *                   256-byte aligned, where a weight's gradient is given; NULL otherwise.
  * The other arguments as spla_norm_rotate. */

@@ -5,17 +5,40 @@
 // angles, with the same gain), u = g w and n = x r:
 //   dx = r (u - n mean(u n)),  dw = sum over rows of g n.
 //
-// One read and one write of the rows (the gradients read two arrays), so the arithmetic is free
-// to be exact: a head lies in 4 to 16 neighbouring lanes, its squares are summed over them, and
-// norm, weight, sine, cosine and turn are fp64, rounded to fp32 and then to the element type.
-// Squares of finite values cannot overflow, and no input bits are lost before the one rounding.
+// One read and one write of the rows (the gradients read two arrays). A head lies in 4 to 16
+// neighbouring lanes, and its squares are summed over them in fp64: those of finite values cannot
+// overflow. Angles are fp64, as everywhere here. For fp32 rows so is all the rest, rounded once;
+// for bf16 rows it is fp32, a few 2^-24 beside the result's 2^-8 (all in fp64 the conversions, at
+// a quarter of the rate, and not the bytes bound them: 8192 rows of 40 heads, d 128, 57 us).
 #include "spla_device.h"
 #include "spla_kernels.h"
 #include "spla_rope.h"
 
 namespace spla {
 
+// What rows of T are computed in, and a cosine and sine of it.
+template <typename T>
+struct Calc {
+  typedef float R;
+  typedef float2 R2;
+};
+template <>
+struct Calc<float> {
+  typedef double R;
+  typedef double2 R2;
+};
+
 // Sum over aligned groups of 2^n neighbouring lanes; the same bits in each.
+template <int LANES>
+__device__ __forceinline__ float group_sum(float v) {
+  v += dpp_f32<0xB1, 0xF>(0.f, v);                     // quad_perm [1,0,3,2]
+  v += dpp_f32<0x4E, 0xF>(0.f, v);                     // quad_perm [2,3,0,1]
+  if (LANES >= 8) v += dpp_f32<0x141, 0xF>(0.f, v);    // row_half_mirror
+  if (LANES >= 16) v += dpp_f32<0x140, 0xF>(0.f, v);   // row_mirror
+  if (LANES >= 32) v += xor16(v);
+  if (LANES >= 64) v += xor32(v);
+  return v;
+}
 template <int LANES>
 __device__ __forceinline__ double group_sum(double v) {
   v += dpp_f64<0xB1, 0xF>(0.0, v);                     // quad_perm [1,0,3,2]
@@ -32,6 +55,8 @@ __device__ __forceinline__ double group_sum(double v) {
 // coordinates fill pieces, one otherwise.
 template <typename T, int D, int VEC>
 struct HeadUnit {
+  typedef typename Calc<T>::R R;
+  typedef typename Calc<T>::R2 R2;
   static constexpr int E = 2 * VEC, LANES = D / E;
   int c0, c1, p0;
   bool turned;
@@ -47,9 +72,9 @@ struct HeadUnit {
     }
   }
   template <typename U>
-  static __device__ __forceinline__ void piece(const U* p, double* x) {
+  static __device__ __forceinline__ void piece(const U* p, R* x) {
     constexpr int B = VEC * (int)sizeof(U);
-    U v[VEC];
+    __align__(16) U v[VEC];
     if constexpr (B >= 16) {
 #pragma unroll
       for (int i = 0; i < B / 16; ++i)
@@ -59,45 +84,53 @@ struct HeadUnit {
       for (int i = 0; i < VEC; ++i) v[i] = p[i];
     }
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = (double)Elem<U>::load(v, i);
+    for (int i = 0; i < VEC; ++i) x[i] = (R)Elem<U>::load(v, i);
   }
-  __device__ __forceinline__ void load(const T* row, double (&x)[E]) const {
+  __device__ __forceinline__ void load(const T* row, R (&x)[E]) const {
     piece(row + c0, x);
     piece(row + c1, x + VEC);
   }
-  __device__ __forceinline__ void weights(const float* w, double (&x)[E]) const {
+  __device__ __forceinline__ void weights(const float* w, R (&x)[E]) const {
     if (w) {
       piece(w + c0, x);
       piece(w + c1, x + VEC);
     } else {
 #pragma unroll
-      for (int i = 0; i < E; ++i) x[i] = 1.0;
+      for (int i = 0; i < E; ++i) x[i] = (R)1;
     }
   }
-  __device__ __forceinline__ void store(T* row, const double (&y)[E]) const {
-    __align__(16) T v[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) Elem<T>::store(v, i, (float)y[i]);
+  __device__ __forceinline__ void store(T* row, const R (&y)[E]) const {
     if constexpr (VEC * sizeof(T) == 16) {
+      __align__(16) uint32_t v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4) {
+          v[i] = __float_as_uint((float)y[i]);
+        } else {
+          typedef __bf16 pair __attribute__((ext_vector_type(2)));
+          v[i] = __builtin_bit_cast(uint32_t, pair{(__bf16)(float)y[2 * i],
+                                                   (__bf16)(float)y[2 * i + 1]});
+        }
+      }
       *reinterpret_cast<uint4*>(row + c0) = reinterpret_cast<const uint4*>(v)[0];
       *reinterpret_cast<uint4*>(row + c1) = reinterpret_cast<const uint4*>(v)[1];
     } else {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        row[c0 + i] = v[i];
-        row[c1 + i] = v[VEC + i];
+        Elem<T>::store(row, c0 + i, (float)y[i]);
+        Elem<T>::store(row, c1 + i, (float)y[VEC + i]);
       }
     }
   }
-  static __device__ __forceinline__ void turn2(double& a, double& b, double2 w) {
-    const double x = a, y = b;
+  static __device__ __forceinline__ void turn2(R& a, R& b, R2 w) {
+    const R x = a, y = b;
     a = fma(x, w.x, -(y * w.y));
     b = fma(y, w.x, x * w.y);
   }
   // cs: the cosines and sines of the row's pairs
-  __device__ __forceinline__ void turn(double (&x)[E], const double2* cs, bool half) const {
+  __device__ __forceinline__ void turn(R (&x)[E], const R2* cs, bool half) const {
     if (!turned) return;
-    const double2* w = cs + p0;
+    const R2* w = cs + p0;
     if (half) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) turn2(x[i], x[i + VEC], w[i]);
@@ -106,14 +139,31 @@ struct HeadUnit {
       for (int i = 0; i < VEC; ++i) turn2(x[2 * i], x[2 * i + 1], w[i]);
     }
   }
+  // (mean x^2 + eps)^(-1/2) of the head whose coordinates these are
+  static __device__ __forceinline__ R inverse_size(const R (&x)[E], double eps) {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) s = fma((double)x[i], (double)x[i], s);
+    s = group_sum<LANES>(s) * (1.0 / D) + eps;
+    if constexpr (sizeof(R) == 8) return rsqrt(s);
+    // fp32: s as m 4^k, whose root has no range to leave
+    int k = (int)(__double_as_longlong(s) >> 52) - 1023;  // (s >= 0)
+    k = (k + 1024) / 2 - 512;
+    k = s > 0.0 && k < 512 ? k : 0;  // zero, infinity and NaN as they are
+    const float m = (float)ldexp(s, -2 * k);
+    return (R)ldexpf(__builtin_amdgcn_rsqf(m), -k);  // (a step of 2^-23 at most)
+  }
 };
 
-template <typename T, int D, int VEC>
-__device__ __forceinline__ double inverse_size(const double (&x)[2 * VEC], double eps) {
-  double s = 0.0;
-#pragma unroll
-  for (int i = 0; i < 2 * VEC; ++i) s = fma(x[i], x[i], s);
-  return rsqrt(group_sum<D / (2 * VEC)>(s) * (1.0 / D) + eps);
+// The angle of pair i of row `row`, as rope_angles forms it.
+template <typename R2>
+__device__ __forceinline__ R2 turn_of(const RotateRows& rows, const spla_rope& rope, int64_t row,
+                                      int i, bool transpose) {
+  const double2 c = rope_cos_sin(row_position(rows, row), rope.turns[i], rope.gain);
+  R2 w;
+  w.x = c.x;
+  w.y = transpose ? -c.y : c.y;
+  return w;
 }
 
 // R whole rows (a position of a sequence with all its heads) per workgroup, as in the rotation.
@@ -122,11 +172,13 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(RotateRows rows, NormS
                                                           spla_rope rope, double eps) {
   using Unit = HeadUnit<T, D, VEC>;
   constexpr int UPH = Unit::LANES;
-  __shared__ double2 cs[R][D / 2];
+  __shared__ typename Unit::R2 cs[R][D / 2];
   const int np = rope.rot_dim / 2;
   const bool half = rope.layout == SPLA_ROPE_HALF;
   const int64_t row0 = rows.first + (int64_t)blockIdx.x * R, n_rows = (int64_t)rows.n_tokens * rows.batch;
-  rope_angles<R>(rows, rope, false, row0, cs);
+  for (int e = threadIdx.x; e < R * np; e += 256)
+    cs[e / np][e % np] =
+        turn_of<typename Unit::R2>(rows, rope, min(row0 + e / np, n_rows - 1), e % np, false);
   __syncthreads();
   const int units = (sa.r.heads + sb.r.heads) * UPH;
   for (int e = threadIdx.x; e < R * units; e += 256) {
@@ -138,12 +190,12 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(RotateRows rows, NormS
     const NormSet& s = first ? sa : sb;
     const int h = first ? hh : hh - sa.r.heads;
     const Unit un(u % UPH, np, half);
-    double x[Unit::E], w[Unit::E];
+    typename Unit::R x[Unit::E], w[Unit::E];
     un.load(static_cast<const T*>(s.r.x) + t * s.r.xs_t + b * s.r.xs_b + h * s.r.xs_h, x);
     un.weights(s.w ? s.w + (int64_t)h * s.w_stride : nullptr, w);
-    const double r = inverse_size<T, D, VEC>(x, eps);
+    const typename Unit::R r = Unit::inverse_size(x, eps);
 #pragma unroll
-    for (int i = 0; i < Unit::E; ++i) x[i] *= r * w[i];
+    for (int i = 0; i < Unit::E; ++i) x[i] = x[i] * r * w[i];
     un.turn(x, cs[rr], half);
     un.store(static_cast<T*>(s.r.y) + t * s.r.ys_t + b * s.r.ys_b + h * s.r.ys_h, x);
   }
@@ -160,8 +212,10 @@ __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, 
   using Unit = HeadUnit<T, D, VEC>;
   constexpr int UPH = Unit::LANES, E = Unit::E;
   constexpr int kRows = 32;  // at most, of those whose angles are formed at once
+  typedef typename Unit::R R;
+  typedef typename Unit::R2 R2;
   __shared__ union {
-    double2 cs[kRows][D / 2];
+    R2 cs[kRows][D / 2];
     double sum[256][E];
   } sh;
   const int np = rope.rot_dim / 2, tid = threadIdx.x;
@@ -177,7 +231,8 @@ __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, 
   const NormSet& s = first ? sa : sb;
   const int h = first ? hh : hh - sa.r.heads;
   const Unit un(u % UPH, np, half);
-  double w[E], sum[E];
+  R w[E];
+  double sum[E];
   un.weights(s.w && busy ? s.w + (int64_t)h * s.w_stride : nullptr, w);
 #pragma unroll
   for (int i = 0; i < E; ++i) sum[i] = 0.0;
@@ -186,33 +241,36 @@ __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, 
     const int n = (int)(end - r0 < per ? end - r0 : per);
     for (int e = tid; e < n * np; e += 256) {
       const int rr = e / np, i = e % np;
-      double2 c = rope_cos_sin(row_position(rows, r0 + rr), rope.turns[i], rope.gain);
-      c.y = -c.y;
-      sh.cs[rr][i] = c;
+      sh.cs[rr][i] = turn_of<R2>(rows, rope, r0 + rr, i, true);
     }
     __syncthreads();
     if (!busy) continue;
+    R part_sum[E];  // of these rows, up to four
+#pragma unroll
+    for (int i = 0; i < E; ++i) part_sum[i] = (R)0;
     for (int rr = slot; rr < n; rr += at_once) {
       const int64_t row = r0 + rr;
       const int t = (int)(row / rows.batch), b = (int)(row % rows.batch);
-      double x[E], g[E];
+      R x[E], g[E];
       un.load(static_cast<const T*>(s.r.x) + t * s.r.xs_t + b * s.r.xs_b + h * s.r.xs_h, x);
       un.load(static_cast<const T*>(s.g) + t * s.gs_t + b * s.gs_b + h * s.r.xs_h, g);
       un.turn(g, sh.cs[rr], half);
-      const double r = inverse_size<T, D, VEC>(x, eps);
-      double dot = 0.0;
+      const R r = Unit::inverse_size(x, eps);
+      R dot = (R)0;
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         x[i] *= r;  // n
-        sum[i] = fma(g[i], x[i], sum[i]);
+        part_sum[i] = fma(g[i], x[i], part_sum[i]);
         g[i] *= w[i];  // u
         dot = fma(g[i], x[i], dot);
       }
-      dot = group_sum<UPH>(dot) * (1.0 / D);
+      dot = group_sum<UPH>(dot) * (R)(1.0 / D);
 #pragma unroll
       for (int i = 0; i < E; ++i) x[i] = r * fma(-x[i], dot, g[i]);
       un.store(static_cast<T*>(s.r.y) + t * s.r.ys_t + b * s.r.ys_b + h * s.r.ys_h, x);
     }
+#pragma unroll
+    for (int i = 0; i < E; ++i) sum[i] += (double)part_sum[i];
   }
   if (!part) return;
   __syncthreads();

@@ -70,10 +70,14 @@ def inputs(dev, name, scale=2.0):
 
 def tolerance(dtype, ref, x, angle):
     """One rounding to fp32 and one to the type, and fp64 steps: d + 16 of the head's largest, and
-    of the angle in turns."""
-    size = ref.abs().amax(-1, keepdim=True)
+    of the angle in turns. bf16 rows are computed in fp32: each of a pair's two products is off by
+    at most 8 steps of 2^-24 (root 2, r, x r, w, cosine, product, sum) of itself, and a product is
+    at most the head's largest |w x r| gain, which the turned head's largest is at least 1 / sqrt 2
+    of (a turn keeps a pair's length)."""
+    size = ref.abs().amax(-1, keepdim=True) * 2.0 ** 0.5
+    own = 16 * 2.0 ** -24 if dtype == "bf16" else 0.0
     return ((C.HALF[DT[dtype]] + 2.0 ** -24) * ref.abs() * 1.001
-            + size * 2.0 ** -52 * (8 * angle + x.shape[-1] + 16))
+            + size * (own + 2.0 ** -52 * (8 * angle + x.shape[-1] + 16)))
 
 
 def check(got, ref, dtype, angle):
@@ -110,13 +114,17 @@ def test_gradients(dev, name):
     assert (dwq is None) == (wq is None) == (dwk is None)
     for dx, dw, x, g, weight in ((dq, dwq, q, gq, wq), (dk, dwk, k, gk, wk)):
         ref, rw = C.norm_rotate_grad(x, g, weight, eps, pos[..., None], w, layout=layout, gain=gain)
-        # fp64 steps of the gradient's two terms, which may cancel
+        # steps of the gradient's two terms, which may cancel; bf16 rows in fp32: u by 8 steps of
+        # its size as in the forward pass, n by 6, their products' mean by 16 more (a sum of d
+        # terms over lanes and by fives and sixes within them), the last two operations by 2:
+        # 40 in all of (1 + n^2) |u| r
         y, n, r = C.norm(x, weight, eps)
         u = R.turn(g, pos[..., None], w, layout=layout, gain=gain, transpose=True)
         size = (u if weight is None else u * weight.double()).abs().amax(-1, keepdim=True) * r
         size = size * (1 + n.abs().amax(-1, keepdim=True))
-        tol = ((C.HALF[DT[dtype]] + 2.0 ** -24) * ref.abs() * 1.001
-               + size * 2.0 ** -52 * (8 * (float(pos.max()) + 1) + 2 * d + 32))
+        steps = 2.0 ** -52 * (8 * (float(pos.max()) + 1) + 2 * d + 32)
+        own = 40 * 2.0 ** -24 if dtype == "bf16" else 0.0
+        tol = (C.HALF[DT[dtype]] + 2.0 ** -24) * ref.abs() * 1.001 + size * (steps + own)
         err = (dx.double() - ref).abs()
         assert bool((err <= tol).all()), float((err / tol).max())
         if weight is None:
@@ -125,8 +133,13 @@ def test_gradients(dev, name):
         if weight.dim() == 1:
             rw, terms = rw.sum(0), terms.sum(0)
         assert dw.shape == weight.shape and dw.dtype is torch.float32
+        # bf16 rows: g by 8 steps of a pair's size, n by 6, product and the sum of four terms by 5
+        pairs = (g.double().abs().amax(-1, keepdim=True) * 2.0 ** 0.5 * abs(gain) * n.abs())
+        pairs = pairs.flatten(0, -3).sum(0)
+        pairs = pairs.sum(0) if weight.dim() == 1 else pairs
         tol = 2.0 ** -24 * rw.abs() * 1.001 + terms * 2.0 ** -52 * (
-            8 * (float(pos.max()) + 1) + d + T * b * hq)
+            8 * (float(pos.max()) + 1) + d + T * b * hq) + pairs * (
+                24 * 2.0 ** -24 if dtype == "bf16" else 0.0)
         assert bool(((dw.double() - rw).abs() <= tol).all())
     # the same bits again, and in place of the rows or of the gradients
     again = spla.norm_rotate_grad(cfg, rope, q, k, gq, gk, wq, wk, eps, positions=pos, q_out=gq,
