@@ -635,7 +635,7 @@ int32_t spla_norm_rotate(const spla_config* cfg, const spla_rope* rope, int32_t 
  *                   allowed.
  *  q_weight_grad, k_weight_grad: device fp32, shaped as the weights, or NULL (not
  *                   needed); the sum over all rows (and, with weight_per_head = 0, heads),
- *                   in fp64 (for bf16 rows, four at a time in fp32) and in a fixed order.
+ *                   in fp64 (for bf16 rows, up to 19 at a time in fp32) and in a fixed order.
  *                   Zeros where there are no rows.
  *  workspace:       at least spla_norm_rotate_grad_workspace_bytes(cfg, n_tokens) bytes,
  *                   256-byte aligned, where a weight's gradient is given; NULL otherwise.

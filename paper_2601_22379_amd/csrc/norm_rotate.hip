@@ -211,13 +211,12 @@ __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, 
                                                                double eps, double* part) {
   using Unit = HeadUnit<T, D, VEC>;
   constexpr int UPH = Unit::LANES, E = Unit::E;
-  constexpr int kRows = 32;  // at most, of those whose angles are formed at once
+  constexpr int kRows = 32;      // at most, of those whose angles are formed at once
+  constexpr int kHeldRows = 16;  // that a thread sums before it turns to fp64
   typedef typename Unit::R R;
   typedef typename Unit::R2 R2;
-  __shared__ union {
-    R2 cs[kRows][D / 2];
-    double sum[256][E];
-  } sh;
+  __shared__ R2 cs[kRows][D / 2];
+  __shared__ double sums[E][256];  // of each thread, in fp64
   const int np = rope.rot_dim / 2, tid = threadIdx.x;
   const bool half = rope.layout == SPLA_ROPE_HALF;
   const int units = (sa.r.heads + sb.r.heads) * UPH, u0 = (int)blockIdx.y * 256;
@@ -231,36 +230,36 @@ __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, 
   const NormSet& s = first ? sa : sb;
   const int h = first ? hh : hh - sa.r.heads;
   const Unit un(u % UPH, np, half);
-  R w[E];
-  double sum[E];
+  R w[E], sum[E];
   un.weights(s.w && busy ? s.w + (int64_t)h * s.w_stride : nullptr, w);
 #pragma unroll
-  for (int i = 0; i < E; ++i) sum[i] = 0.0;
+  for (int i = 0; i < E; ++i) {
+    sum[i] = (R)0;
+    sums[i][tid] = 0.0;
+  }
+  int held_rows = 0;
   for (int64_t r0 = begin; r0 < end; r0 += per) {
     __syncthreads();
     const int n = (int)(end - r0 < per ? end - r0 : per);
     for (int e = tid; e < n * np; e += 256) {
       const int rr = e / np, i = e % np;
-      sh.cs[rr][i] = turn_of<R2>(rows, rope, r0 + rr, i, true);
+      cs[rr][i] = turn_of<R2>(rows, rope, r0 + rr, i, true);
     }
     __syncthreads();
     if (!busy) continue;
-    R part_sum[E];  // of these rows, up to four
-#pragma unroll
-    for (int i = 0; i < E; ++i) part_sum[i] = (R)0;
     for (int rr = slot; rr < n; rr += at_once) {
       const int64_t row = r0 + rr;
       const int t = (int)(row / rows.batch), b = (int)(row % rows.batch);
       R x[E], g[E];
       un.load(static_cast<const T*>(s.r.x) + t * s.r.xs_t + b * s.r.xs_b + h * s.r.xs_h, x);
       un.load(static_cast<const T*>(s.g) + t * s.gs_t + b * s.gs_b + h * s.r.xs_h, g);
-      un.turn(g, sh.cs[rr], half);
+      un.turn(g, cs[rr], half);
       const R r = Unit::inverse_size(x, eps);
       R dot = (R)0;
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         x[i] *= r;  // n
-        part_sum[i] = fma(g[i], x[i], part_sum[i]);
+        sum[i] = fma(g[i], x[i], sum[i]);
         g[i] *= w[i];  // u
         dot = fma(g[i], x[i], dot);
       }
@@ -269,13 +268,17 @@ __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, 
       for (int i = 0; i < E; ++i) x[i] = r * fma(-x[i], dot, g[i]);
       un.store(static_cast<T*>(s.r.y) + t * s.r.ys_t + b * s.r.ys_b + h * s.r.ys_h, x);
     }
+    held_rows += per / at_once;
+    if (held_rows >= kHeldRows || r0 + per >= end) {
+      held_rows = 0;
 #pragma unroll
-    for (int i = 0; i < E; ++i) sum[i] += (double)part_sum[i];
+      for (int i = 0; i < E; ++i) {
+        sums[i][tid] += (double)sum[i];
+        sum[i] = (R)0;
+      }
+    }
   }
   if (!part) return;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < E; ++i) sh.sum[tid][i] = busy ? sum[i] : 0.0;
   __syncthreads();
   // coordinate c of a head: unit and element that hold it
   const auto held = [&](int c, int& unit, int& el) {
@@ -295,7 +298,7 @@ __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, 
       int unit, el;
       held(e % D, unit, el);
       double v = 0.0;
-      for (int k = 0; k < at_once; ++k) v += sh.sum[k * nu + e / D * UPH + unit][el];
+      for (int k = 0; k < at_once; ++k) v += sums[el][k * nu + e / D * UPH + unit];
       out[e] = v;
     }
     return;
@@ -308,7 +311,7 @@ __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, 
     const int lo = e < D ? h0 : max(h0, sa.r.heads), hi = e < D ? min(h1, sa.r.heads) : h1;
     double v = 0.0;
     for (int k = 0; k < at_once; ++k)
-      for (int x = lo; x < hi; ++x) v += sh.sum[k * nu + (x - h0) * UPH + unit][el];
+      for (int x = lo; x < hi; ++x) v += sums[el][k * nu + (x - h0) * UPH + unit];
     out[e] = v;
   }
 }
