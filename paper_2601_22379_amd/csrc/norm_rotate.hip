@@ -316,19 +316,22 @@ __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, 
   }
 }
 
-// Sums n records of `cols` columns, 16 columns per workgroup by 16 parts of the records, in a
+// Sums n records of `cols` columns, 8 columns per workgroup by 32 parts of the records, in a
 // fixed order; the first `split` columns go to da, the others to db (NULL: nowhere).
+constexpr int kReduceCols = 8;
 __global__ __launch_bounds__(256) void norm_grad_reduce_kernel(const double* part, int n, int cols,
                                                                int split, float* da, float* db) {
-  __shared__ double s[16][16];
-  const int c = (int)blockIdx.x * 16 + (threadIdx.x & 15), p = threadIdx.x >> 4;
+  constexpr int P = 256 / kReduceCols;
+  __shared__ double s[P][kReduceCols];
+  const int x = threadIdx.x % kReduceCols, c = (int)blockIdx.x * kReduceCols + x;
+  const int p = threadIdx.x / kReduceCols;
   double v = 0.0;
 #pragma unroll 8
-  for (int i = p; i < n; i += 16) v += part[(int64_t)i * cols + c];
-  s[p][threadIdx.x & 15] = v;
+  for (int i = p; i < n; i += P) v += part[(int64_t)i * cols + c];
+  s[p][x] = v;
   __syncthreads();
   if (p > 0) return;
-  for (int i = 1; i < 16; ++i) v += s[i][threadIdx.x];
+  for (int i = 1; i < P; ++i) v += s[i][x];
   float* out = c < split ? da : db;
   if (out) out[c < split ? c : c - split] = (float)v;
 }
@@ -396,7 +399,7 @@ hipError_t launch_norm_rotate_grad(const Dims& m, const spla_rope& rope, double 
     const bool per_head = a.w_stride || b.w_stride;
     const int cols = per_head ? heads * m.d : 2 * m.d, split = per_head ? heads_a * m.d : m.d;
     const int records = n > 0 ? (per_head ? runs : runs * chunks) : 0;
-    hipLaunchKernelGGL(norm_grad_reduce_kernel, dim3((unsigned)(cols / 16)), dim3(256), 0, st, part,
+    hipLaunchKernelGGL(norm_grad_reduce_kernel, dim3((unsigned)(cols / kReduceCols)), dim3(256), 0, st, part,
                        records, cols, split, da, db);
   }
   return hipGetLastError();

@@ -531,7 +531,7 @@ struct AttendWs {
   int64_t total;
 };
 
-// rows: query rows per tile.
+// rows_per_tile: query rows per tile.
 SPLA_HD AttendWs attend_ws_of(const Dims& m, int n_tokens, int rows_per_tile) {
   AttendWs w;
   w.rows = rows_per_tile;

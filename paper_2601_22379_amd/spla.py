@@ -456,52 +456,61 @@ def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_
 
 
 def _rotated_rows(cfg, q, k, positions, seq_lens):
-    """What the calls that rotate rows have in common: (T, the rows' leading sizes, dtype,
+    """What the calls that rotate rows have in common: (T, the rows' leading sizes, d, dtype,
     device, address of positions, of seq_lens)."""
     x = k if q is None else q
     if x is None:
         raise ValueError("q or k is needed")
-    n, batch = x.dim(), cfg.batch
-    if n not in (3, 4):
+    shape, batch, device = x.shape, cfg.batch, x.device
+    n = len(shape)
+    if n == 4:
+        T = shape[0]
+        lead = (T, batch)
+    elif n == 3:
+        T, lead = 1, (batch,)
+    else:
         raise ValueError(f"rows of [T, {batch}] or [{batch}] positions are needed")
-    T = x.shape[0] if n == 4 else 1
-    lead = (T, batch) if n == 4 else (batch,)
-    device = x.device
-    at = None
+    at = lens = None
     if positions is not None:
         at = _row_words("positions", positions, (T, batch) if positions.dim() == 2 else lead, device)
-    lens = None if seq_lens is None else _row_words("seq_lens", seq_lens, (batch,), device)
+    if seq_lens is not None:
+        lens = _row_words("seq_lens", seq_lens, (batch,), device)
     if device.type != "cuda":
         raise ValueError("tensors on a GPU are needed")
-    return T, lead, torch_dtype(cfg), device, at, lens
+    return T, lead, cfg.head_dim, torch_dtype(cfg), device, at, lens
 
 
-def _head_weights(cfg, q_weight, k_weight, device):
+def _head_weight(name, w, heads, d, device):
+    """The address of a weight, and whether it is one per head; checked."""
+    shape = w.shape
+    per_head = len(shape) == 2
+    if (w.dtype is not torch.float32 or (shape != (heads, d) if per_head else shape != (d,))
+            or not w.is_contiguous() or w.device != device):
+        raise ValueError(f"{name}: a contiguous fp32 tensor [{d}] or [{heads}, {d}] on the rows' "
+                         "device is needed")
+    if w.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name}: no gradient is recorded here (detach it, or torch.no_grad(); "
+                         "norm_rotate_grad gives it)")
+    return w.data_ptr(), per_head
+
+
+def _head_weights(cfg, q_weight, k_weight, d, device):
     """Whether the weights are one per head, and their addresses."""
-    kinds = set()
-    for name, w, h in (("q_weight", q_weight, cfg.n_q_heads), ("k_weight", k_weight,
-                                                               cfg.n_kv_heads)):
-        if w is None:
-            continue
-        if (w.dtype is not torch.float32 or not w.is_contiguous() or w.device != device
-                or w.shape not in ((cfg.head_dim,), (h, cfg.head_dim))):
-            raise ValueError(f"{name}: a contiguous fp32 tensor [{cfg.head_dim}] or "
-                             f"[{h}, {cfg.head_dim}] on the rows' device is needed")
-        if w.requires_grad and torch.is_grad_enabled():
-            raise ValueError(f"{name}: no gradient is recorded here (detach it, or "
-                             "torch.no_grad(); norm_rotate_grad gives it)")
-        kinds.add(w.dim())
-    if len(kinds) > 1:
+    qw = kw = qh = kh = None
+    if q_weight is not None:
+        qw, qh = _head_weight("q_weight", q_weight, cfg.n_q_heads, d, device)
+    if k_weight is not None:
+        kw, kh = _head_weight("k_weight", k_weight, cfg.n_kv_heads, d, device)
+    if qh is not None and kh is not None and qh is not kh:
         raise ValueError("q_weight and k_weight: a weight per head for both, or one for all heads")
-    return (int(kinds == {2}), None if q_weight is None else q_weight.data_ptr(),
-            None if k_weight is None else k_weight.data_ptr())
+    return 1 if qh or kh else 0, qw, kw
 
 
 def _written(*pairs):
     """Counts the writes to (x, y) where y is x, for products that kept x."""
-    same = [x for x, y in pairs if x is not None and y is x]
-    if same:
-        torch.autograd.graph.increment_version(same)
+    for x, y in pairs:
+        if y is x and x is not None:
+            torch.autograd.graph.increment_version(x)
 
 
 def norm_rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, q_weight=None, k_weight=None,
@@ -512,15 +521,13 @@ def norm_rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, q_weight=None, 
     gradients)."""
     if (q is None and q_out is not None) or (k is None and k_out is not None):
         raise ValueError("no output without its input")
-    T, lead, dtype, device, at, lens = _rotated_rows(cfg, q, k, positions, seq_lens)
+    T, lead, d, dtype, device, at, lens = _rotated_rows(cfg, q, k, positions, seq_lens)
     qp = qs = op = os_ = kp = ks = tp = ts = 0
     if q is not None:
-        q_out, qp, qs, op, os_ = _rows("q", q, q_out, lead + (cfg.n_q_heads, cfg.head_dim), dtype,
-                                       device)
+        q_out, qp, qs, op, os_ = _rows("q", q, q_out, lead + (cfg.n_q_heads, d), dtype, device)
     if k is not None:
-        k_out, kp, ks, tp, ts = _rows("k", k, k_out, lead + (cfg.n_kv_heads, cfg.head_dim), dtype,
-                                      device)
-    per_head, qw, kw = _head_weights(cfg, q_weight, k_weight, device)
+        k_out, kp, ks, tp, ts = _rows("k", k, k_out, lead + (cfg.n_kv_heads, d), dtype, device)
+    per_head, qw, kw = _head_weights(cfg, q_weight, k_weight, d, device)
     _launch(lib().spla_norm_rotate, "spla_norm_rotate", device,
             (ctypes.byref(cfg), ctypes.byref(rope), T, at, lens, qw, kw, per_head, eps, qp, qs, op,
              os_, kp, ks, tp, ts))
@@ -540,8 +547,8 @@ def norm_rotate_grad(cfg: SplaConfig, rope: SplaRope, q=None, k=None, q_grad=Non
             or (q is None and (q_out is not None or q_weight is not None))
             or (k is None and (k_out is not None or k_weight is not None))):
         raise ValueError("rows and their gradients go together, outputs and weights with them")
-    T, lead, dtype, device, at, lens = _rotated_rows(cfg, q, k, positions, seq_lens)
-    per_head, qw, kw = _head_weights(cfg, q_weight, k_weight, device)
+    T, lead, d, dtype, device, at, lens = _rotated_rows(cfg, q, k, positions, seq_lens)
+    per_head, qw, kw = _head_weights(cfg, q_weight, k_weight, d, device)
     args, outs = [], []
     for name, x, g, y, h in (("q", q, q_grad, q_out, cfg.n_q_heads),
                              ("k", k, k_grad, k_out, cfg.n_kv_heads)):
@@ -549,7 +556,7 @@ def norm_rotate_grad(cfg: SplaConfig, rope: SplaRope, q=None, k=None, q_grad=Non
             args += [0] * 6
             outs.append(None)
             continue
-        shape = lead + (h, cfg.head_dim)
+        shape = lead + (h, d)
         y, xp, xs, yp, ys = _rows(name, x, y, shape, dtype, device)
         _, gp, gs, _, _ = _rows(f"{name}_grad", g, g, shape, dtype, device)
         args += [xp, xs, gp, gs, yp, ys]
@@ -936,55 +943,55 @@ class SplaCache8(_DeviceCache):
                                         self.scales.data_ptr(), self.seq_lens.data_ptr(),
                                         self.counters.data_ptr(), self.err.data_ptr(),
                                         None if block_table is None else block_table.data_ptr())
+        self._refs = (ctypes.byref(self.cfg), ctypes.byref(self._struct))
+        self._dtype = torch_dtype(cfg)
+        self._heads = (cfg.batch, cfg.n_kv_heads, cfg.head_dim)  # of a position's rows
+        self._row = cfg.n_kv_heads * cfg.head_dim
 
     @property
     def struct(self) -> SplaCache8Struct:
         return self._struct
 
     def reset(self):
-        _launch(lib().spla_reset8, "spla_reset8", self.device,
-                (ctypes.byref(self.cfg), ctypes.byref(self._struct)))
+        _launch(lib().spla_reset8, "spla_reset8", self.device, self._refs)
 
     def _new_rows(self, name, x, shape):
         """Address and row stride of new rows, checked."""
-        if (x.shape != shape or x.dtype is not torch_dtype(self.cfg)
-                or x.device != self.seq_lens.device):
-            raise ValueError(f"{name}: a {torch_dtype(self.cfg)} tensor {list(shape)} on the "
-                             "cache's device is needed")
-        return x.data_ptr(), _row_stride(x, shape[-2] * shape[-1])
+        if x.shape != shape or x.dtype is not self._dtype or x.device != self.device:
+            raise ValueError(f"{name}: a {self._dtype} tensor {list(shape)} on the cache's device "
+                             "is needed")
+        return x.data_ptr(), _row_stride(x, self._row)
 
     def append(self, k_new: torch.Tensor, v_new: torch.Tensor,
                n_new: Optional[torch.Tensor] = None):
         """k_new, v_new: [T, batch, Hkv, d] (or [batch, Hkv, d]: one token) in the cfg's dtype, as
         norm_rotate() and rotate() give them; rows may be slices of wider ones (a fused
         projection's). n_new int32 [batch]: the tokens each sequence really has."""
-        c = self.cfg
-        if k_new.dim() not in (3, 4):
+        n = k_new.dim()
+        if n not in (3, 4):
             raise ValueError("k_new: [T, batch, Hkv, d] is needed")
-        T = k_new.shape[0] if k_new.dim() == 4 else 1
-        shape = k_new.shape[:-3] + (c.batch, c.n_kv_heads, c.head_dim)
+        T = k_new.shape[0] if n == 4 else 1
+        shape = (T,) + self._heads if n == 4 else self._heads
         kp, ks = self._new_rows("k_new", k_new, shape)
         vp, vs = self._new_rows("v_new", v_new, shape)
-        np_ = None if n_new is None else self._given("n_new", n_new, (c.batch,), torch.int32)
+        np_ = None if n_new is None else self._given("n_new", n_new, self._heads[:1], torch.int32)
         _launch(lib().spla_append8, "spla_append8", self.device,
-                (ctypes.byref(c), ctypes.byref(self._struct), T, kp, ks, vp, vs, np_))
+                self._refs + (T, kp, ks, vp, vs, np_))
 
     def read(self, n_tokens: int, first: Optional[torch.Tensor] = None, k_out=None, v_out=None):
         """Keys and values [n_tokens, batch, Hkv, d], the numbers the cache holds of the tokens at
         positions first[b] + t (first int32 [batch], or 0); zeros where a sequence holds none."""
-        c, dtype = self.cfg, torch_dtype(self.cfg)
-        shape = (int(n_tokens), c.batch, c.n_kv_heads, c.head_dim)
         if n_tokens < 0:
             raise ValueError("n_tokens: a count is needed")
+        shape, dtype = (int(n_tokens),) + self._heads, self._dtype
         if k_out is None:
             k_out = torch.empty(shape, dtype=dtype, device=self.device)
         if v_out is None:
             v_out = torch.empty(shape, dtype=dtype, device=self.device)
         kp = self._given("k_out", k_out, shape, dtype)
         vp = self._given("v_out", v_out, shape, dtype)
-        fp = None if first is None else self._given("first", first, (c.batch,), torch.int32)
-        _launch(lib().spla_read8, "spla_read8", self.device,
-                (ctypes.byref(c), ctypes.byref(self._struct), shape[0], fp, kp, vp))
+        fp = None if first is None else self._given("first", first, self._heads[:1], torch.int32)
+        _launch(lib().spla_read8, "spla_read8", self.device, self._refs + (shape[0], fp, kp, vp))
         return k_out, v_out
 
     def rotate(self, rope: SplaRope, q=None, k=None, positions=None, q_out=None, k_out=None,
@@ -1012,8 +1019,7 @@ class SplaCache8(_DeviceCache):
         ws = self._attend_ws = self._workspace("attend8", T, attend8_workspace_bytes,
                                                self._attend_ws)
         _launch(lib().spla_attend8, "spla_attend8", self.device,
-                (ctypes.byref(self.cfg), ctypes.byref(self._struct), T, qp, ctypes.byref(opts), op,
-                 lp, ws.data_ptr(), ws.numel()))
+                self._refs + (T, qp, ctypes.byref(opts), op, lp, ws.data_ptr(), ws.numel()))
         return out, lse
 
 
