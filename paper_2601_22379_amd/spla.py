@@ -1015,6 +1015,8 @@ class SplaCache8(_DeviceCache):
         beside them the first `sinks` of the sequence (from first_key on where it is given)."""
         T, qp, out, op, lse, lp, base = self._attend_args(q, out, lse, softcap, slopes, first_key,
                                                           prefix_len, n_new)
+        if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
+            raise ValueError("window and sinks: counts of tokens are needed")
         opts = SplaAttend8Opts(base, window, sinks)
         ws = self._attend_ws = self._workspace("attend8", T, attend8_workspace_bytes,
                                                self._attend_ws)

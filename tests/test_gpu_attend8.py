@@ -91,7 +91,7 @@ def tile_cap(dtype, hkv, group, B, b, T):
 
 
 KINDS = ["causal", "softcap", "bias", "docs", "prefix", "ragged", "window", "window_sinks",
-         "window_docs", "window_prefix", "all"]
+         "window_docs", "window_prefix", "window_softcap", "window_bias", "softcap_large", "all"]
 
 
 MANY = [n for n, c in CASES.items() if c[6] * c[2] // c[3] > 64]
@@ -108,9 +108,11 @@ def test_against_64_bits(dev, name, wide, kind):
     cache, K, V = filled(dev, dtype, lens, hq, hkv, d, B, cap, paged=paged, garbage=True)
     q = randn(dev, dtype, T, b, hq, d, seed=3, scale=2.0)
     kw, ref = {}, {}
-    if kind in ("softcap", "all"):
+    if kind in ("softcap", "window_softcap", "all"):
         kw["softcap"] = ref["softcap"] = 7.0
-    if kind in ("bias", "all"):
+    if kind == "softcap_large":
+        kw["softcap"] = ref["softcap"] = 200.0
+    if kind in ("bias", "window_bias", "all"):
         kw["slopes"] = ref["slopes"] = torch.exp2(-torch.arange(1.0, hq + 1, device=dev) * 8 / hq)
     if kind in ("docs", "window_docs", "all"):
         g = torch.Generator().manual_seed(5)
@@ -125,8 +127,9 @@ def test_against_64_bits(dev, name, wide, kind):
         news = [min(L, (T + i) // (i + 1)) for i, L in enumerate(lens)]
         news[-1] = min(lens[-1], T)
     if kind.startswith("window") or kind == "all":
-        w = {"window": 1, "window_sinks": 40, "window_docs": 33, "window_prefix": 100, "all": 70}[kind]
-        s = {"window": 0, "window_sinks": 4, "window_docs": 3, "window_prefix": 37, "all": 1}[kind]
+        w, s = {"window": (1, 0), "window_sinks": (40, 4), "window_docs": (33, 3),
+                "window_prefix": (100, 37), "window_softcap": (90, 2), "window_bias": (65, 6),
+                "all": (70, 1)}[kind]
         kw |= dict(window=w, sinks=s)
         ref |= dict(window=w, sinks=s)
     kw["n_new"] = ints(dev, news)
@@ -254,6 +257,14 @@ def test_repeats_bit_for_bit(dev, cap):
         for _ in range(3):
             o, l = cache.attend(q, window=2000, sinks=4)
             assert torch.equal(a, o) and torch.equal(la, l)
+
+
+def test_window_counts_are_refused(dev):
+    cache, _, _ = filled(dev, "bf16", [40], 2, 1, 64, 32)
+    q = randn(dev, "bf16", 1, 1, 2, 64)
+    for window, sinks in ((-1, 0), (4, -1), (2 ** 31, 0), (2 ** 32 + 4, 0), (4, 2 ** 32)):
+        with pytest.raises(ValueError):
+            cache.attend(q, window=window, sinks=sinks)
 
 
 def test_other_stream(dev):
