@@ -9,7 +9,8 @@
 // neighbouring lanes, and its squares are summed over them in fp64: those of finite values cannot
 // overflow. Angles are fp64, as everywhere here. For fp32 rows so is all the rest, rounded once;
 // for bf16 rows it is fp32, a few 2^-24 beside the result's 2^-8 (all in fp64 the conversions, at
-// a quarter of the rate, and not the bytes bound them: 8192 rows of 40 heads, d 128, 57 us).
+// a quarter of the rate, and not the bytes bound them: 8192 rows of 40 heads, d 128, 57 us per
+// call against 41.6, of which the kernel takes 33, 5.1 TB/s; one row 4.7 us).
 #include "spla_device.h"
 #include "spla_kernels.h"
 #include "spla_rope.h"
@@ -204,7 +205,8 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(RotateRows rows, NormS
 // Gradients. A workgroup takes up to 256 units (blockIdx.y: which) of a run of rows, several
 // rows at a time where they are fewer; a thread keeps its head and coordinates, so that its sums
 // of g n stay in registers. They are summed over the workgroup's rows (and heads, where one
-// weight serves all) in a fixed order and left as a record of the run.
+// weight serves all) in a fixed order and left as a record of the run. 8192 rows of 40 heads (bf16,
+// d 128, 252 MB): 46.5 us, 5.4 TB/s, and 4.8 for the sum of the runs.
 template <typename T, int D, int VEC>
 __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, NormSet sa,
                                                                NormSet sb, spla_rope rope,

@@ -613,7 +613,8 @@ SPLA_HD AttendWs attend8_ws_layout(const Dims& m, int n_tokens) {
 }
 
 // Appends of up to so many blocks count their workgroups in the cache's counters, and the last
-// one advances the length; longer ones leave that to a launch of their own.
+// one advances the length; longer ones leave that to a launch of their own (11003 and 16384 tokens
+// of 8 KV heads, with the read-back: 86 us, 97 where 4112 workgroups of a sequence count themselves).
 constexpr int kAppend8Arrive = 4;
 
 // ---- gradients of the per-head norms
