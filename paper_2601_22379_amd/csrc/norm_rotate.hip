@@ -383,7 +383,8 @@ hipError_t launch_norm_rotate_grad(const Dims& m, const spla_rope& rope, double 
   const bool pieces = rope.rot_dim % (32 / m.elem) == 0;
   const int uph = pieces ? m.d * m.elem / 32 : m.d / 2;
   const int runs = norm_grad_runs(m, rows.n_tokens), chunks = (int)ceil_div(heads * uph, 256);
-  double* part = da || db ? reinterpret_cast<double*>(base + ws.part) : nullptr;
+  const bool sums = da || db;
+  double* part = sums && n > 0 ? reinterpret_cast<double*>(base + ws.part) : nullptr;
   if (n > 0) {
     auto go = [&](auto kern) {
       hipLaunchKernelGGL(kern, dim3((unsigned)runs, (unsigned)chunks), dim3(256), 0, st, rows, a, b,
@@ -397,7 +398,7 @@ hipError_t launch_norm_rotate_grad(const Dims& m, const spla_rope& rope, double 
       else pieces ? go(norm_rotate_grad_kernel<bf16_t, 128, 8>) : go(norm_rotate_grad_kernel<bf16_t, 128, 1>);
     }
   }
-  if (part) {
+  if (sums) {
     const bool per_head = a.w_stride || b.w_stride;
     const int cols = per_head ? heads * m.d : 2 * m.d, split = per_head ? heads_a * m.d : m.d;
     const int records = n > 0 ? (per_head ? runs : runs * chunks) : 0;

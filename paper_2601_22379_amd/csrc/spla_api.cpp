@@ -566,8 +566,10 @@ extern "C" int32_t spla_attend8(const spla_config* cfg, const spla_cache8* cache
   if (n_tokens == 0) return SPLA_OK;
   if (!q || !out || out == q || !aligned16(q) || !aligned16(out)) return SPLA_ERR_INVALID_ARG;
   const Dims m = spla::make_dims(*cfg);
-  const spla::AttendWs L = spla::attend8_ws_layout(m, n_tokens);
-  if ((s = check_ws(workspace, workspace_bytes, (size_t)L.total)) != SPLA_OK) return s;
+  const size_t need = (size_t)spla::attend8_ws_bytes(m, n_tokens);
+  if ((s = check_ws(workspace, workspace_bytes, need)) != SPLA_OK) return s;
+  const spla::AttendWs L =
+      spla::attend8_ws_layout(m, n_tokens, spla::attend8_keys(m, n_tokens, o));
   SPLA_TRY(spla::launch_attend8(m, *cfg, *cache, n_tokens, q, o, out, lse, L,
                                 static_cast<char*>(workspace), static_cast<hipStream_t>(stream)));
   return SPLA_OK;

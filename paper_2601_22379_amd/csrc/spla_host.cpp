@@ -218,7 +218,7 @@ extern "C" int32_t spla_attend8_workspace_bytes(const spla_config* c, int32_t n_
   if (st != SPLA_OK) return st;
   if (n_tokens < 0) return SPLA_ERR_INVALID_ARG;
   if (n_tokens > c->max_seq_len) return SPLA_ERR_CAPACITY;
-  *out = (size_t)spla::attend8_ws_layout(spla::make_dims(*c), n_tokens).total;
+  *out = (size_t)spla::attend8_ws_bytes(spla::make_dims(*c), n_tokens);
   return SPLA_OK;
 }
 

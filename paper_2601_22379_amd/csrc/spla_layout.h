@@ -531,8 +531,8 @@ struct AttendWs {
   int64_t total;
 };
 
-// rows_per_tile: query rows per tile.
-SPLA_HD AttendWs attend_ws_of(const Dims& m, int n_tokens, int rows_per_tile) {
+// rows_per_tile: query rows per tile; keys: those that a query can see, at most.
+SPLA_HD AttendWs attend_ws_of(const Dims& m, int n_tokens, int rows_per_tile, int keys) {
   AttendWs w;
   w.rows = rows_per_tile;
   w.shares = 0;
@@ -541,7 +541,7 @@ SPLA_HD AttendWs attend_ws_of(const Dims& m, int n_tokens, int rows_per_tile) {
   const int64_t wgs = (int64_t)m.bh * w.n_tiles;
   int64_t n = 1;
   if (wgs > 0) n = w.rows != kTileRows && kAttendFill / wgs > 1 ? kAttendFill / wgs : kTileFill / wgs;
-  const int64_t most = ceil_div(m.cap, attend_min_steps(w.rows) * kSubTokens);
+  const int64_t most = ceil_div(keys, attend_min_steps(w.rows) * kSubTokens);
   n = n < most ? n : most;
   n = n < kAttendMaxSplit ? n : kAttendMaxSplit;
   w.n_split = (int)(n > 1 ? n : 1);
@@ -566,7 +566,7 @@ SPLA_HD AttendWs attend_ws_of(const Dims& m, int n_tokens, int rows_per_tile) {
 }
 
 SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
-  return attend_ws_of(m, n_tokens, attend_rows(m, n_tokens));
+  return attend_ws_of(m, n_tokens, attend_rows(m, n_tokens), m.cap);
 }
 
 // ---- exact attention over the 8-bit cache: tiles of 16 rows (codes straight from the cache, made
@@ -574,14 +574,14 @@ SPLA_HD AttendWs attend_ws_layout(const Dims& m, int n_tokens) {
 // to read, tiles of 16 hold out longer than over the bf16 cache: until there are more than so
 // many (tile, 32-token step) pairs, 16 of which a step of 128 rows would save, though it takes
 // 1.1 us from codes to sums when it is alone. The lengths are on the device, so the capacity
-// counts. bf16, d 128: 16384 pairs 20.9 us, 24.5 in tiles of 128 (8 heads of 4096 tokens, 256
+// counts, or a window. bf16, d 128: 16384 pairs 20.9 us, 24.5 in tiles of 128 (8 heads of 4096 tokens, 256
 // rows), 16.4 and 25.5 (32 of 1000), 32768 pairs 32.7 and 31.0 (one head of 32K, 512 rows),
 // 48000 pairs 51.4 and 35.3 (32 of 8000, 96 rows), 45.4 and 46.3 (32 of 16000, 40 rows); fp32, d
 // 64: 84000 pairs 39.4 and 41.7, 131072 pairs 79.0 and 64.8 (d 128: 110 and 108).
 constexpr int64_t kTile8Steps = 32768, kTile8StepsF32 = 98304;
-SPLA_HD int attend8_rows(const Dims& m, int n_tokens) {
+SPLA_HD int attend8_rows(const Dims& m, int n_tokens, int keys) {
   const int64_t rows = (int64_t)n_tokens * m.group;
-  const int64_t steps = ceil_div(rows, kAttendRows) * m.bh * (m.cap / kSubTokens);
+  const int64_t steps = ceil_div(rows, kAttendRows) * m.bh * ceil_div(keys, kSubTokens);
   return rows <= 64 || steps <= (m.elem == 2 ? kTile8Steps : kTile8StepsF32) ? kAttendRows
                                                                              : kTileRows;
 }
@@ -594,11 +594,18 @@ constexpr int kShareBatch = 64, kShareSplits = 4, kShareSteps = 64;
 // Records that a tile's last workgroup joins at most (rows times splits).
 constexpr int kShareJoin = 512;
 
-SPLA_HD AttendWs attend8_ws_layout(const Dims& m, int n_tokens) {
-  AttendWs w = attend_ws_of(m, n_tokens, attend8_rows(m, n_tokens));
+// Keys that a tile of queries may read: all there may be, or those of the window and the sinks.
+SPLA_HD int attend8_keys(const Dims& m, int n_tokens, const spla_attend8_opts& o) {
+  if (o.window <= 0 || o.attend.prefix_len) return m.cap;
+  const int64_t n = (int64_t)o.window + o.sinks + n_tokens + 2 * kSubTokens;
+  return (int)(n < m.cap ? n : m.cap);
+}
+
+SPLA_HD AttendWs attend8_ws_layout(const Dims& m, int n_tokens, int keys) {
+  AttendWs w = attend_ws_of(m, n_tokens, attend8_rows(m, n_tokens, keys), keys);
   const int64_t units = (int64_t)m.bh * w.n_tiles;
   if (w.rows != kAttendRows || m.batch < 2 || m.batch > kShareBatch || n_tokens == 0 ||
-      units > kAttendFill / kShareSplits || m.cap / kSubTokens < kShareSteps * w.n_split)
+      units > kAttendFill / kShareSplits || keys / kSubTokens < kShareSteps * w.n_split)
     return w;
   int rows = 1;
   while (rows < kAttendRows && rows < (int64_t)n_tokens * m.group) rows *= 2;
@@ -610,6 +617,21 @@ SPLA_HD AttendWs attend8_ws_layout(const Dims& m, int n_tokens) {
   w.n_eff = w.total =
       align_up(w.ml + (int64_t)w.shares * w.rows * 2 * 4, SPLA_WORKSPACE_ALIGN);
   return w;
+}
+
+// Bytes that suffice whatever the options: fewer keys mean fewer splits, and may mean tiles of 16
+// rows in place of 128, or splits in place of shares.
+SPLA_HD int64_t attend8_ws_bytes(const Dims& m, int n_tokens) {
+  const int64_t a = attend8_ws_layout(m, n_tokens, m.cap).total;
+  const int64_t b = attend_ws_of(m, n_tokens, kAttendRows, m.cap).total;
+  const int64_t c = align_up((int64_t)kTileFill * kSyncLine * 4 +
+                                 (int64_t)kAttendFill * kAttendRows * (m.d + 2) * 4,
+                             SPLA_WORKSPACE_ALIGN);
+  const bool shares = m.batch > 1 && m.batch <= kShareBatch && n_tokens > 0 &&
+                      m.bh * ceil_div((int64_t)n_tokens * m.group, kAttendRows) <=
+                          kAttendFill / kShareSplits;
+  const int64_t most = a > b ? a : b;
+  return shares && c > most ? c : most;
 }
 
 // Appends of up to so many blocks count their workgroups in the cache's counters, and the last

@@ -225,6 +225,13 @@ def test_no_rows(dev):
         g = spla.norm_rotate_grad(cfg, rope, *e, *e, a, c)
         assert g[0].shape[0] == 0 and not g[2].any() and not g[3].any()
         assert g[2].shape == a.shape and g[3].shape == c.shape
+    # the library, which needs no workspace for that
+    dw = torch.ones(128, device=dev)
+    st = torch.cuda.current_stream().cuda_stream
+    assert spla.lib().spla_norm_rotate_grad(
+        ctypes.byref(cfg), ctypes.byref(rope), 0, None, None, None, None, 0, 1e-6, *[None, 0] * 6,
+        None, dw.data_ptr(), None, 0, st) == 0
+    assert not dw.any()
 
 
 def test_captured_replays(dev):
