@@ -609,8 +609,10 @@ SPLA_HD AttendWs attend8_ws_layout(const Dims& m, int n_tokens, int keys) {
     return w;
   int rows = 1;
   while (rows < kAttendRows && rows < (int64_t)n_tokens * m.group) rows *= 2;
+  const int most = kShareJoin / rows < kAttendMaxSplit ? kShareJoin / rows : kAttendMaxSplit;
+  if (2 * w.n_split > most) return w;  // a long sequence may take twice its even part at least
   w.shares = kAttendFill;
-  w.n_split = kShareJoin / rows < kAttendMaxSplit ? kShareJoin / rows : kAttendMaxSplit;
+  w.n_split = most;
   w.join = 0;
   w.part = (int64_t)kTileFill * kSyncLine * 4;  // behind the counters
   w.ml = align_up(w.part + (int64_t)w.shares * w.rows * m.d * 4, SPLA_WORKSPACE_ALIGN);
