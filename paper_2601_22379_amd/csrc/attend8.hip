@@ -434,12 +434,19 @@ struct StepCodes {  // a thread's chunks of a step: keys and values (d 64: one o
 };
 
 // Workgroups per compute unit: three, where their registers suffice (at d 128 with up to six of
-// the masks' bounds in scratch memory; two: 583 us for the prompt, 554 with three on that card).
-template <typename T, int KIND, bool SINKS>
-constexpr int kTile8Wgs = std::is_same<T, float>::value || (SINKS && KIND >= kBiased) ? 2 : 3;
+// the masks' bounds in scratch memory; two: 583 us for the prompt, 554 with three on that card),
+// four at d 64 (8192 tokens of 32 heads on 8: 372 us, 395 with three), two for the general form
+// (4096 tokens over 8192 under a cap of 60: 710 us, 758 with three).
+template <typename T, int D, int KIND, bool SINKS>
+constexpr bool kTile8Large =
+    std::is_same<T, float>::value ||
+    (D == 128 && (KIND == kGeneral || (SINKS && KIND == kBiased)));
+template <typename T, int D, int KIND, bool SINKS>
+constexpr int kTile8Wgs =
+    kTile8Large<T, D, KIND, SINKS> ? 2 : D == 64 && KIND == kPlain ? 4 : 3;
 
 template <typename T, int D, int KIND, bool SINKS>
-__global__ __launch_bounds__(256, (kTile8Wgs<T, KIND, SINKS>)) void attend8_tile_kernel(
+__global__ __launch_bounds__(256, (kTile8Wgs<T, D, KIND, SINKS>)) void attend8_tile_kernel(
     Attend8Args a) {
   constexpr int TERMS = std::is_same<T, float>::value ? 3 : 1;
   __shared__ TileBuf<D> buf[2];

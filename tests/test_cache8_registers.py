@@ -19,7 +19,8 @@ from test_kernel_registers import kernels  # noqa: F401  (the fixture)
     (r"attend8_tile_kernel<spla::bf16_t, 64", 8, 168, 0),
     (r"attend8_tile_kernel<spla::bf16_t, 128, [01], true", 2, 168, 4),
     (r"attend8_tile_kernel<spla::bf16_t, 128, [23], true", 2, 256, 0),
-    (r"attend8_tile_kernel<spla::bf16_t, 128, [0-3], false", 4, 168, 6),
+    (r"attend8_tile_kernel<spla::bf16_t, 128, [0-2], false", 3, 168, 6),
+    (r"attend8_tile_kernel<spla::bf16_t, 128, 3, false", 1, 256, 0),
 ])
 def test_registers(kernels, pattern, count, vgprs, spills):  # noqa: F811
     hit = {n: k for n, k in kernels.items() if re.match(pattern, n)}
