@@ -204,6 +204,21 @@ def test_capacity_and_pages(dev):
     same(got[:, 0], K.x[0, :, :32].transpose(0, 1).clone(), "bf16")
 
 
+def test_capacity_of_long_appends(dev):
+    """Appends whose length a launch of its own advances, past the capacity."""
+    cache = make(dev, "bf16", 2, 2, 128, 32, 256, paged=True)
+    K = C.Held(2, 2, 128, 32, 256)
+    for i, n in enumerate([[200, 130], [200, 126], [5, 256]]):
+        k = randn("bf16", 256 if i == 2 else 200, 2, 2, 128, seed=30 + i)
+        start = list(K.lens)
+        K.append(k, n, start)
+        cache.append(k.to(dev), k.to(dev), ints(dev, n))
+        assert cache.seq_lens.tolist() == K.lens
+        assert cache.device_errors() == (0 if i == 0 else spla.DEVERR_CAPACITY)
+    assert K.lens == [256, 256]
+    check_read(cache, K, K, K.lens, "bf16")
+
+
 def test_neighbours_stay(dev):
     """An append writes the blocks it touches and nothing else."""
     cache = make(dev, "bf16", 2, 2, 128, 64, 256)
