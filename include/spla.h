@@ -79,7 +79,8 @@ enum {
                                that gives up is detected; counters left non-zero by
                                other means are not checked at launch */
   SPLA_DEVERR_PAGE = 4      /* an append met a block_table entry outside [0, kv_pages):
-                               its rows were not written */
+                               its rows were not written (spla_read8: its rows were
+                               asked for, zeros were given) */
 };
 
 /* Library limits. */
@@ -672,10 +673,11 @@ int32_t spla_append8(const spla_config* cfg, const spla_cache8* cache, int32_t n
  * cache, to move a prefix elsewhere).
  *  first: device int32 [batch] or NULL (0): row (t, b) is the token at position
  *         first[b] + t. Positions that the sequence does not hold (negative ones too) give
- *         zeros.
+ *         zeros, and so do those of a block whose block_table entry is out of range
+ *         (SPLA_DEVERR_PAGE).
  *  k_out, v_out: device, dtype [n_tokens][batch][Hkv][d], 16-byte aligned; NULL: not
  *         read (one of the two must be given).
- * The cache is only read. n_tokens = 0 does nothing. */
+ * The cache is only read, but for its error word. n_tokens = 0 does nothing. */
 int32_t spla_read8(const spla_config* cfg, const spla_cache8* cache, int32_t n_tokens,
                    const int32_t* first, void* k_out, void* v_out, void* stream);
 

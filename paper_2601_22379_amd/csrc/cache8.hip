@@ -301,6 +301,7 @@ struct Read8Args {
   const uint8_t *k, *v;
   const float* scales;
   const int32_t *seq_lens, *table, *first;
+  int32_t* err;
   void *ko, *vo;
   int n_tokens, step0;  // first 32-token step of this launch
 };
@@ -319,12 +320,20 @@ __global__ __launch_bounds__(256) void read8_kernel(Read8Args a) {
   const int64_t r0 = p0 - f;  // row of the step's first token
   if (r0 >= a.n_tokens) return;
   const int len = min(max(a.seq_lens[b], 0), m.cap);
-  const bool any = p0 >= 0 && p0 < len;  // uniform
-  float ks = 0.f, vs = 0.f;
+  bool any = p0 >= 0 && max(p0, f) < len;  // uniform
+  int64_t slot = 0;
   if (any) {
     const int blk = (int)p0 / m.B;
-    int64_t slot = (int64_t)bh * m.nb_cap + blk;
-    if (a.table) slot = (int64_t)max(block_page(m, a.table, bh, blk), 0) * m.hkv + h;
+    slot = (int64_t)bh * m.nb_cap + blk;
+    if (a.table) {  // a block without a page is held by nobody (page 0 is another's)
+      const int p = block_page(m, a.table, bh, blk);
+      slot = (int64_t)p * m.hkv + h;
+      any = p >= 0;
+      if (!any && tid == 0 && a.err) atomicOr(a.err, SPLA_DEVERR_PAGE);
+    }
+  }
+  float ks = 0.f, vs = 0.f;
+  if (any) {
     ks = a.scales[2 * slot];
     vs = a.scales[2 * slot + 1];
     const int64_t o = (slot * m.B + (int)p0 % m.B) * D;
@@ -383,6 +392,7 @@ hipError_t launch_read8(const Dims& m, const spla_cache8& c, int n_tokens, const
   a.seq_lens = c.seq_lens;
   a.table = m.pages > 0 ? c.block_table : nullptr;
   a.first = first;
+  a.err = c.err_flags;
   a.ko = k_out;
   a.vo = v_out;
   a.n_tokens = n_tokens;
