@@ -506,6 +506,13 @@ def _head_weights(cfg, q_weight, k_weight, d, device):
     return 1 if qh or kh else 0, qw, kw
 
 
+def _unrecorded(*rows):
+    """Refuses rows, and memory for results, that autograd would record."""
+    for x in rows:
+        if x is not None and x.requires_grad and torch.is_grad_enabled():
+            raise ValueError("no gradient is recorded here (detach the rows, or torch.no_grad())")
+
+
 def _written(*pairs):
     """Counts the writes to (x, y) where y is x, for products that kept x."""
     for x, y in pairs:
@@ -966,10 +973,12 @@ class SplaCache8(_DeviceCache):
                n_new: Optional[torch.Tensor] = None):
         """k_new, v_new: [T, batch, Hkv, d] (or [batch, Hkv, d]: one token) in the cfg's dtype, as
         norm_rotate() and rotate() give them; rows may be slices of wider ones (a fused
-        projection's). n_new int32 [batch]: the tokens each sequence really has."""
+        projection's). n_new int32 [batch]: the tokens each sequence really has. Nothing here is
+        recorded for autograd, and tensors that it would record are refused by all calls."""
         n = k_new.dim()
         if n not in (3, 4):
             raise ValueError("k_new: [T, batch, Hkv, d] is needed")
+        _unrecorded(k_new, v_new)
         T = k_new.shape[0] if n == 4 else 1
         shape = (T,) + self._heads if n == 4 else self._heads
         kp, ks = self._new_rows("k_new", k_new, shape)
@@ -983,6 +992,7 @@ class SplaCache8(_DeviceCache):
         positions first[b] + t (first int32 [batch], or 0); zeros where a sequence holds none."""
         if n_tokens < 0:
             raise ValueError("n_tokens: a count is needed")
+        _unrecorded(k_out, v_out)
         shape, dtype = (int(n_tokens),) + self._heads, self._dtype
         if k_out is None:
             k_out = torch.empty(shape, dtype=dtype, device=self.device)
@@ -1013,6 +1023,7 @@ class SplaCache8(_DeviceCache):
         """Exact attention of the last T tokens of every sequence over the cache, as
         SplaCache.attend; window > 0: the query at position p sees the keys after p - window, and
         beside them the first `sinks` of the sequence (from first_key on where it is given)."""
+        _unrecorded(q, out, lse, slopes)
         T, qp, out, op, lse, lp, base = self._attend_args(q, out, lse, softcap, slopes, first_key,
                                                           prefix_len, n_new)
         if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
