@@ -419,6 +419,14 @@ def _row_words(name, t, shape, device):
     return t.data_ptr()
 
 
+def _written(*outs):
+    """Counts a write to each tensor that the caller handed in for results: products that kept it,
+    or memory of it under another name, then refuse their backward passes."""
+    for x in outs:
+        if x is not None:
+            torch.autograd.graph.increment_version(x)
+
+
 def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_lens=None,
            q_out=None, k_out=None, transpose=False):
     """Rotates q [T, batch, Hq, d] and / or k [T, batch, Hkv, d] (or without T: one position)
@@ -430,6 +438,7 @@ def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_
     x = k if q is None else q
     if x is None or (q is None and q_out is not None) or (k is None and k_out is not None):
         raise ValueError("q or k is needed, and no output without its input")
+    given = q_out, k_out
     n, batch, d, device, dtype = x.dim(), cfg.batch, cfg.head_dim, x.device, torch_dtype(cfg)
     if n not in (3, 4):
         raise ValueError(f"rows of [T, {batch}] or [{batch}] positions are needed")
@@ -449,9 +458,7 @@ def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_
     _launch(lib().spla_rotate, "spla_rotate", device,
             (ctypes.byref(cfg), ctypes.byref(rope), T, at, lens, qp, qs, op, os_, kp, ks, tp, ts,
              1 if transpose else 0))
-    if (q is not None and q_out is q) or (k is not None and k_out is k):  # products that kept them
-        torch.autograd.graph.increment_version([x for x, y in ((q, q_out), (k, k_out))
-                                                if x is not None and y is x])
+    _written(*given)
     return q_out, k_out
 
 
@@ -513,13 +520,6 @@ def _unrecorded(*rows):
             raise ValueError("no gradient is recorded here (detach the rows, or torch.no_grad())")
 
 
-def _written(*pairs):
-    """Counts the writes to (x, y) where y is x, for products that kept x."""
-    for x, y in pairs:
-        if y is x and x is not None:
-            torch.autograd.graph.increment_version(x)
-
-
 def norm_rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, q_weight=None, k_weight=None,
                 eps=1e-6, positions=None, seq_lens=None, q_out=None, k_out=None):
     """rotate() of rows whose heads are normed first: x / sqrt(mean(x^2) + eps) times the weight
@@ -528,6 +528,7 @@ def norm_rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, q_weight=None, 
     gradients)."""
     if (q is None and q_out is not None) or (k is None and k_out is not None):
         raise ValueError("no output without its input")
+    given = q_out, k_out
     T, lead, d, dtype, device, at, lens = _rotated_rows(cfg, q, k, positions, seq_lens)
     qp = qs = op = os_ = kp = ks = tp = ts = 0
     if q is not None:
@@ -538,7 +539,7 @@ def norm_rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, q_weight=None, 
     _launch(lib().spla_norm_rotate, "spla_norm_rotate", device,
             (ctypes.byref(cfg), ctypes.byref(rope), T, at, lens, qw, kw, per_head, eps, qp, qs, op,
              os_, kp, ks, tp, ts))
-    _written((q, q_out), (k, k_out))
+    _written(*given)
     return q_out, k_out
 
 
@@ -576,7 +577,7 @@ def norm_rotate_grad(cfg: SplaConfig, rope: SplaRope, q=None, k=None, q_grad=Non
             (ctypes.byref(cfg), ctypes.byref(rope), T, at, lens, qw, kw, per_head, eps, *args,
              None if qwg is None else qwg.data_ptr(), None if kwg is None else kwg.data_ptr(),
              None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel()))
-    _written((q, outs[0]), (q_grad, outs[0]), (k, outs[1]), (k_grad, outs[1]))
+    _written(q_out, k_out)
     return outs[0], outs[1], qwg, kwg
 
 
@@ -850,6 +851,7 @@ class SplaCache(_DeviceCache):
         every query sees. n_new int32 [batch]: the queries each sequence really has; the
         rows of out and lse past them are left as they are (zeros in tensors made here). Ahead
         of a graph capture a call of the same T makes the workspace."""
+        given = out, lse
         T, qp, out, op, lse, lp, opts = self._attend_args(q, out, lse, softcap, slopes, first_key,
                                                           prefix_len, n_new)
         ws = self._attend_ws = self._workspace("attend", T, attend_workspace_bytes,
@@ -857,6 +859,7 @@ class SplaCache(_DeviceCache):
         _launch(lib().spla_attend, "spla_attend", self.device,
                 (ctypes.byref(self.cfg), ctypes.byref(self._struct), T, qp, ctypes.byref(opts), op,
                  lp, ws.data_ptr(), ws.numel()))
+        _written(*given)
         return out, lse
 
     def norm_rotate(self, rope: SplaRope, q=None, k=None, q_weight=None, k_weight=None, eps=1e-6,
@@ -993,6 +996,7 @@ class SplaCache8(_DeviceCache):
         if n_tokens < 0:
             raise ValueError("n_tokens: a count is needed")
         _unrecorded(k_out, v_out)
+        given = k_out, v_out
         shape, dtype = (int(n_tokens),) + self._heads, self._dtype
         if k_out is None:
             k_out = torch.empty(shape, dtype=dtype, device=self.device)
@@ -1002,6 +1006,7 @@ class SplaCache8(_DeviceCache):
         vp = self._given("v_out", v_out, shape, dtype)
         fp = None if first is None else self._given("first", first, self._heads[:1], torch.int32)
         _launch(lib().spla_read8, "spla_read8", self.device, self._refs + (shape[0], fp, kp, vp))
+        _written(*given)
         return k_out, v_out
 
     def rotate(self, rope: SplaRope, q=None, k=None, positions=None, q_out=None, k_out=None,
@@ -1024,6 +1029,7 @@ class SplaCache8(_DeviceCache):
         SplaCache.attend; window > 0: the query at position p sees the keys after p - window, and
         beside them the first `sinks` of the sequence (from first_key on where it is given)."""
         _unrecorded(q, out, lse, slopes)
+        given = out, lse
         T, qp, out, op, lse, lp, base = self._attend_args(q, out, lse, softcap, slopes, first_key,
                                                           prefix_len, n_new)
         if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
@@ -1033,6 +1039,7 @@ class SplaCache8(_DeviceCache):
                                                self._attend_ws)
         _launch(lib().spla_attend8, "spla_attend8", self.device,
                 self._refs + (T, qp, ctypes.byref(opts), op, lp, ws.data_ptr(), ws.numel()))
+        _written(*given)
         return out, lse
 
 
