@@ -687,8 +687,8 @@ int32_t spla_read8(const spla_config* cfg, const spla_cache8* cache, int32_t n_t
  *   (window = 0 or j > p - window or j < first_key + sinks).
  * Arguments, results and limits as spla_attend, with opts of its own kind and the
  * workspace of spla_attend8_workspace_bytes. The products are those of the numbers the
- * cache holds, exactly; fp32 queries and weights enter them with all their bits, for
- * bf16 the weights are rounded to 16 bits, or to bf16 where a KV head has more than 64 query
+ * cache holds, exactly; fp32 queries and weights enter them with all their bits down to
+ * 2^-126, for bf16 the weights are rounded to 16 bits, or to bf16 where a KV head has more than 64 query
  * rows and the call is a large one. */
 int32_t spla_attend8(const spla_config* cfg, const spla_cache8* cache, int32_t n_tokens,
                      const void* q, const spla_attend8_opts* opts, void* out, float* lse,

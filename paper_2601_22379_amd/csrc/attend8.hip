@@ -109,7 +109,7 @@ struct Step8 {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           __bf16 t[QN];
-          split_bf16<QN>(f[i], t);
+          split_query<QN>(f[i], t);
 #pragma unroll
           for (int n = 0; n < QN; ++n) q[c][n][i] = t[n];
         }
@@ -473,7 +473,7 @@ __global__ __launch_bounds__(256, (kTile8Wgs<T, D, KIND, SINKS>)) void attend8_t
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           __bf16 t[TERMS];
-          split_bf16<TERMS>((float)qp[16 * s + i], t);
+          split_query<TERMS>((float)qp[16 * s + i], t);
 #pragma unroll
           for (int n = 0; n < TERMS; ++n) ps.q[n][s][i] = t[n];
         }

@@ -405,13 +405,27 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
-// x as N bf16 terms, largest first.
+// x as N bf16 terms, largest first (|x| up to bf16's largest, 2^128 - 2^120).
 template <int N>
 __device__ __forceinline__ void split_bf16(float x, __bf16 (&t)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     t[i] = (__bf16)x;
     if (i + 1 < N) x -= (float)t[i];
+  }
+}
+
+// A query's number likewise, whatever it is: past bf16's largest the first term is cut, not
+// rounded (to an infinity, whose rest is none), and an infinity is its own first term.
+template <int N>
+__device__ __forceinline__ void split_query(float x, __bf16 (&t)[N]) {
+  const bool past = fabsf(x) > 0x1.FEp127f;
+  t[0] = past ? __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(x) >> 16)) : (__bf16)x;
+  x = fabsf(x) == INFINITY ? 0.f : x - (float)t[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) {
+    t[i] = (__bf16)x;
+    x -= (float)t[i];
   }
 }
 
