@@ -415,13 +415,15 @@ __device__ __forceinline__ void split_bf16(float x, __bf16 (&t)[N]) {
   }
 }
 
-// A query's number likewise, whatever it is: past bf16's largest the first term is cut, not
-// rounded (to an infinity, whose rest is none), and an infinity is its own first term.
+// A query's number likewise, whatever it is: the first term is cut, not rounded (past bf16's
+// largest that would be an infinity), and an infinity is its own first term. Cut, too, three
+// terms hold all 24 bits: the rest has 16, of which the second term leaves 8.
 template <int N>
 __device__ __forceinline__ void split_query(float x, __bf16 (&t)[N]) {
-  const bool past = fabsf(x) > 0x1.FEp127f;
-  t[0] = past ? __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(x) >> 16)) : (__bf16)x;
-  x = fabsf(x) == INFINITY ? 0.f : x - (float)t[0];
+  const uint32_t w = __float_as_uint(x);
+  t[0] = __builtin_bit_cast(__bf16, (uint16_t)(w >> 16));
+  const float rest = x - __uint_as_float(w & 0xFFFF0000u);
+  x = fabsf(x) == INFINITY ? 0.f : rest;
 #pragma unroll
   for (int i = 1; i < N; ++i) {
     t[i] = (__bf16)x;
