@@ -419,12 +419,19 @@ def _row_words(name, t, shape, device):
     return t.data_ptr()
 
 
-def _written(*outs):
-    """Counts a write to each tensor that the caller handed in for results: products that kept it,
-    or memory of it under another name, then refuse their backward passes."""
-    for x in outs:
-        if x is not None:
-            torch.autograd.graph.increment_version(x)
+# A write to tensors of a list, as torch.autograd.graph.increment_version counts it (which takes as
+# long again to look at its argument).
+_count_writes = getattr(torch._C, "_increment_version", None) or (
+    torch.autograd.graph.increment_version)
+
+
+def _written(a, b):
+    """Counts a write to a and to b (or None), memory that the caller handed in for results:
+    products that kept it, under whatever name, then refuse their backward passes."""
+    if a is not None:
+        _count_writes((a,) if b is None else (a, b))
+    elif b is not None:
+        _count_writes((b,))
 
 
 def rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, positions=None, seq_lens=None,
@@ -513,11 +520,12 @@ def _head_weights(cfg, q_weight, k_weight, d, device):
     return 1 if qh or kh else 0, qw, kw
 
 
-def _unrecorded(*rows):
-    """Refuses rows, and memory for results, that autograd would record."""
-    for x in rows:
-        if x is not None and x.requires_grad and torch.is_grad_enabled():
-            raise ValueError("no gradient is recorded here (detach the rows, or torch.no_grad())")
+def _unrecorded(a, b, c=None, d=None):
+    """Refuses rows, and memory for results, that autograd would record (or None)."""
+    if ((a is not None and a.requires_grad or b is not None and b.requires_grad
+         or c is not None and c.requires_grad or d is not None and d.requires_grad)
+            and torch.is_grad_enabled()):
+        raise ValueError("no gradient is recorded here (detach the rows, or torch.no_grad())")
 
 
 def norm_rotate(cfg: SplaConfig, rope: SplaRope, q=None, k=None, q_weight=None, k_weight=None,
@@ -629,14 +637,14 @@ class _DeviceCache:
     def _given(self, name, t, shape, dtype):
         """The address of t, checked."""
         if (t.shape != shape or t.dtype is not dtype or not t.is_contiguous()
-                or t.device != self.seq_lens.device):
+                or t.device != self.device):
             raise ValueError(f"{name}: a contiguous {dtype} tensor {list(shape)} on the cache's "
                              "device is needed")
         return t.data_ptr()
 
-    def _attend_args(self, q, out, lse, softcap, slopes, first_key, prefix_len, n_new):
-        """Checked arguments of attend(): (T, address of q, out, its address, lse, its address,
-        SplaAttendOpts)."""
+    def _attend_args(self, opts, q, out, lse, softcap, slopes, first_key, prefix_len, n_new):
+        """Checked arguments of attend(): (T, address of q, out, its address, lse, its address);
+        fills opts, a zero-filled SplaAttendOpts."""
         c, shape, dtype = self.cfg, q.shape, torch_dtype(self.cfg)
         if len(shape) not in (3, 4):
             raise ValueError("q: [T, batch, Hq, d] is needed")
@@ -650,7 +658,7 @@ class _DeviceCache:
             lse = new(shape[:-1], dtype=torch.float32, device=q.device)
         op = self._given("out", out, shape, dtype)
         lp = self._given("lse", lse, shape[:-1], torch.float32)
-        opts = SplaAttendOpts(softcap)
+        opts.softcap = softcap
         if slopes is not None:
             opts.slopes = self._given("slopes", slopes, (c.n_q_heads,), torch.float32)
         if first_key is not None:
@@ -659,7 +667,8 @@ class _DeviceCache:
             opts.prefix_len = self._given("prefix_len", prefix_len, (c.batch,), torch.int32)
         if n_new is not None:
             opts.n_new = self._given("n_new", n_new, (c.batch,), torch.int32)
-        return T, qp, out, op, lse, lp, opts
+        return T, qp, out, op, lse, lp
+
 
 class SplaCache(_DeviceCache):
     """Device buffers of one SPLA cache, allocated with torch, plus the
@@ -851,15 +860,15 @@ class SplaCache(_DeviceCache):
         every query sees. n_new int32 [batch]: the queries each sequence really has; the
         rows of out and lse past them are left as they are (zeros in tensors made here). Ahead
         of a graph capture a call of the same T makes the workspace."""
-        given = out, lse
-        T, qp, out, op, lse, lp, opts = self._attend_args(q, out, lse, softcap, slopes, first_key,
-                                                          prefix_len, n_new)
+        opts = SplaAttendOpts()
+        T, qp, out, op, lse, lp = self._attend_args(opts, q, out, lse, softcap, slopes, first_key,
+                                                    prefix_len, n_new)
         ws = self._attend_ws = self._workspace("attend", T, attend_workspace_bytes,
                                                self._attend_ws)
         _launch(lib().spla_attend, "spla_attend", self.device,
                 (ctypes.byref(self.cfg), ctypes.byref(self._struct), T, qp, ctypes.byref(opts), op,
                  lp, ws.data_ptr(), ws.numel()))
-        _written(*given)
+        _count_writes((out, lse))
         return out, lse
 
     def norm_rotate(self, rope: SplaRope, q=None, k=None, q_weight=None, k_weight=None, eps=1e-6,
@@ -956,6 +965,7 @@ class SplaCache8(_DeviceCache):
         self._refs = (ctypes.byref(self.cfg), ctypes.byref(self._struct))
         self._dtype = torch_dtype(cfg)
         self._heads = (cfg.batch, cfg.n_kv_heads, cfg.head_dim)  # of a position's rows
+        self._batch = (cfg.batch,)
         self._row = cfg.n_kv_heads * cfg.head_dim
 
     @property
@@ -981,12 +991,13 @@ class SplaCache8(_DeviceCache):
         n = k_new.dim()
         if n not in (3, 4):
             raise ValueError("k_new: [T, batch, Hkv, d] is needed")
-        _unrecorded(k_new, v_new)
+        if k_new.requires_grad or v_new.requires_grad:
+            _unrecorded(k_new, v_new)
         T = k_new.shape[0] if n == 4 else 1
         shape = (T,) + self._heads if n == 4 else self._heads
         kp, ks = self._new_rows("k_new", k_new, shape)
         vp, vs = self._new_rows("v_new", v_new, shape)
-        np_ = None if n_new is None else self._given("n_new", n_new, self._heads[:1], torch.int32)
+        np_ = None if n_new is None else self._given("n_new", n_new, self._batch, torch.int32)
         _launch(lib().spla_append8, "spla_append8", self.device,
                 self._refs + (T, kp, ks, vp, vs, np_))
 
@@ -995,18 +1006,18 @@ class SplaCache8(_DeviceCache):
         positions first[b] + t (first int32 [batch], or 0); zeros where a sequence holds none."""
         if n_tokens < 0:
             raise ValueError("n_tokens: a count is needed")
-        _unrecorded(k_out, v_out)
-        given = k_out, v_out
         shape, dtype = (int(n_tokens),) + self._heads, self._dtype
         if k_out is None:
             k_out = torch.empty(shape, dtype=dtype, device=self.device)
         if v_out is None:
             v_out = torch.empty(shape, dtype=dtype, device=self.device)
+        if k_out.requires_grad or v_out.requires_grad:
+            _unrecorded(k_out, v_out)
         kp = self._given("k_out", k_out, shape, dtype)
         vp = self._given("v_out", v_out, shape, dtype)
-        fp = None if first is None else self._given("first", first, self._heads[:1], torch.int32)
+        fp = None if first is None else self._given("first", first, self._batch, torch.int32)
         _launch(lib().spla_read8, "spla_read8", self.device, self._refs + (shape[0], fp, kp, vp))
-        _written(*given)
+        _count_writes((k_out, v_out))
         return k_out, v_out
 
     def rotate(self, rope: SplaRope, q=None, k=None, positions=None, q_out=None, k_out=None,
@@ -1029,17 +1040,17 @@ class SplaCache8(_DeviceCache):
         SplaCache.attend; window > 0: the query at position p sees the keys after p - window, and
         beside them the first `sinks` of the sequence (from first_key on where it is given)."""
         _unrecorded(q, out, lse, slopes)
-        given = out, lse
-        T, qp, out, op, lse, lp, base = self._attend_args(q, out, lse, softcap, slopes, first_key,
-                                                          prefix_len, n_new)
+        opts = SplaAttend8Opts()
+        T, qp, out, op, lse, lp = self._attend_args(opts.attend, q, out, lse, softcap, slopes,
+                                                    first_key, prefix_len, n_new)
         if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
             raise ValueError("window and sinks: counts of tokens are needed")
-        opts = SplaAttend8Opts(base, window, sinks)
+        opts.window, opts.sinks = window, sinks
         ws = self._attend_ws = self._workspace("attend8", T, attend8_workspace_bytes,
                                                self._attend_ws)
         _launch(lib().spla_attend8, "spla_attend8", self.device,
                 self._refs + (T, qp, ctypes.byref(opts), op, lp, ws.data_ptr(), ws.numel()))
-        _written(*given)
+        _count_writes((out, lse))
         return out, lse
 
 
