@@ -636,7 +636,7 @@ int32_t spla_norm_rotate(const spla_config* cfg, const spla_rope* rope, int32_t 
  *                   allowed.
  *  q_weight_grad, k_weight_grad: device fp32, shaped as the weights, or NULL (not
  *                   needed); the sum over all rows (and, with weight_per_head = 0, heads),
- *                   in fp64 (for bf16 rows, up to 19 at a time in fp32) and in a fixed order.
+ *                   in fp64 (for bf16 rows, up to 18 at a time in fp32) and in a fixed order.
  *                   Zeros where there are no rows.
  *  workspace:       at least spla_norm_rotate_grad_workspace_bytes(cfg, n_tokens) bytes,
  *                   256-byte aligned, where a weight's gradient is given; NULL otherwise.
@@ -688,8 +688,11 @@ int32_t spla_read8(const spla_config* cfg, const spla_cache8* cache, int32_t n_t
  * Arguments, results and limits as spla_attend, with opts of its own kind and the
  * workspace of spla_attend8_workspace_bytes. The products are those of the numbers the
  * cache holds, exactly; fp32 queries and weights enter them with all their bits down to
- * 2^-126, for bf16 the weights are rounded to 16 bits, or to bf16 where a KV head has more than 64 query
- * rows and the call is a large one. */
+ * 2^-126. For bf16 the weights are rounded to 16 bits, or to bf16 where a KV head has more
+ * than 64 query rows and the call is a large one: more than 32768 of (16 query rows of a
+ * KV head and sequence) times (32 tokens of max_seq_len, or, with a window and no
+ * prefix_len, of window + sinks + n_tokens + 64 where that is less). A block whose
+ * block_table entry is out of range is read as page 0, as by a decode. */
 int32_t spla_attend8(const spla_config* cfg, const spla_cache8* cache, int32_t n_tokens,
                      const void* q, const spla_attend8_opts* opts, void* out, float* lse,
                      void* workspace, size_t workspace_bytes, void* stream);

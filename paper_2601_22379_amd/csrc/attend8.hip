@@ -7,7 +7,7 @@
 // bf16 in the registers, scale included, one conversion for two of them, and go to the bf16
 // matrix instructions. So the products are those of the values the cache stands for, whatever
 // the queries' type; fp32 queries and weights go in as three bf16 terms (all 24 bits), at three
-// times the products of bf16, a fifth of what fp32 instructions would take.
+// times the products of bf16: 365 TFLOP/s of many rows where a large fp32 product reaches 153.
 #include <type_traits>
 
 #include "spla_attend.h"
@@ -48,7 +48,8 @@ __device__ __forceinline__ Attend8Row attend8_row(const Attend8Args& a, const At
 }
 
 // The 32-token steps of a tile: those of the sinks, then those of the main runs (one run where
-// they meet), numbered from 0.
+// they meet), numbered from 0. The rows' sinks count as one run: where documents begin inside a
+// tile, steps between their sinks are gone through that no row sees.
 struct StepList {
   int sink0, n_sink, main0, n;
   // rows' least and greatest keys (none: lo = INT32_MAX, hi = 0)
@@ -302,11 +303,11 @@ __device__ __forceinline__ int ceil_ratio(int a, int b, float inv_b) {  // a < 2
   return k - ((k - 1) * b >= a ? 1 : 0);
 }
 // Shared evenly: with `per` steps to a workgroup, ceil(steps / per) of them go to each tile of a
-// sequence, in the order of the sequences; per is the least (to 3 %) that leaves as many
-// workgroups as fill the chip, for one more would wait for a compute unit of its own or share
-// one that has two already. (16 sequences of 16K to 65K tokens, 8 KV heads, 4 splits for each:
-// the longest ones' workgroups end long after the others.) The steps are estimated by
-// the length and the window; the tile's own are what is split.
+// sequence, in the order of the sequences; per is the least (to 3 % up to twice the even part, to
+// 19 % past it) that leaves as many workgroups as fill the chip, for one more would wait for a
+// compute unit of its own or share one that has two already. (16 sequences of 16K to 65K tokens, 8
+// KV heads, 4 splits for each: the longest ones' workgroups end long after the others.) The steps
+// are estimated by the length and the window; the tile's own are what is split.
 __device__ __forceinline__ Part8 share_part(const Attend8Args& a, int x) {
   const int lane = threadIdx.x & 63, batch = a.m.batch;
   const int units = a.m.hkv * a.n_tiles;  // of a sequence
@@ -391,8 +392,9 @@ __global__ __launch_bounds__(256, 2) void attend8_stream_kernel(Attend8Args a) {
 // chunks of the next step's codes while this one is used, then converts them into LDS, where the
 // step has the layout of the bf16 cache, and the products are those of its tiles. (The codes by
 // way of LDS, copied there by the loads themselves two steps ahead: 553 us against 541 for the
-// prompt below.) 8192 causal tokens of 32 heads on 8 (d 128): 541 us, 1.02 PFLOP/s (572 on another
-// card); fp32, 512 tokens of 32 heads on 8 over 8192, two sequences: 341 us, 390 TFLOP/s (d 64: 204).
+// prompt below.) 8192 causal tokens of 32 heads on 8 (d 128): 541 to 572 us by the card, 960 to 1020
+// TFLOP/s; fp32, 512 tokens of 32 heads on 8 over 8192, two sequences: 362 us, 367 TFLOP/s (d 64:
+// 206 us, 323).
 template <int D>
 struct StepCodes {  // a thread's chunks of a step: keys and values (d 64: one or the other)
   static constexpr int N = D / 64;
@@ -435,8 +437,9 @@ struct StepCodes {  // a thread's chunks of a step: keys and values (d 64: one o
 
 // Workgroups per compute unit: three, where their registers suffice (at d 128 with up to six of
 // the masks' bounds in scratch memory; two: 583 us for the prompt, 554 with three on that card),
-// four at d 64 (8192 tokens of 32 heads on 8: 372 us, 395 with three), two for the general form
-// (4096 tokens over 8192 under a cap of 60: 710 us, 758 with three).
+// four at d 64 (8192 tokens of 32 heads on 8: 372 us, 395 with three; 342 on another card, where
+// the 16-bit cache's takes 332: half the products beside the same conversions), two for the
+// general form (4096 tokens over 8192 under a cap of 60: 710 us, 758 with three).
 template <typename T, int D, int KIND, bool SINKS>
 constexpr bool kTile8Large =
     std::is_same<T, float>::value ||

@@ -105,8 +105,9 @@ struct Piece {
 // cache's order, with those of older rows (all of the block's, where the scale grows), and
 // written 16 bytes at a time. A thread holds consecutive tokens, so that values, whose chunks
 // are 8 tokens of a coordinate, go to LDS four tokens at a time (byte by byte, with each number
-// scaled, clamped and tested by itself: 60 us for 11003 and 16384 tokens of 8 KV heads; so 38 us, 168
-// MB at 4.5 TB/s; a token for each of 32 sequences 6.0 us).
+// scaled, clamped and tested by itself: 60 us for 11003 and 16384 tokens of 8 KV heads, in the
+// last-level cache for the most part; so 38 us, and 50 over changing inputs, the 168 MB from and to
+// memory at 3.3 TB/s; a token for each of 32 sequences 6.4 us).
 template <typename T, int D, int B>
 __global__ __launch_bounds__(256) void append8_kernel(Append8Args a) {
   constexpr int N = Piece<T>::N, W = N / 4;

@@ -10,7 +10,8 @@
 // overflow. Angles are fp64, as everywhere here. For fp32 rows so is all the rest, rounded once;
 // for bf16 rows it is fp32, a few 2^-24 beside the result's 2^-8 (all in fp64 the conversions, at
 // a quarter of the rate, and not the bytes bound them: 8192 rows of 40 heads, d 128, 57 us per
-// call against 41.6, of which the kernel takes 33, 5.1 TB/s; one row 4.7 us).
+// call against 41.6 over changing inputs, the 168 MB from and to memory at 4.0 TB/s; one row
+// 4.7 us).
 #include "spla_device.h"
 #include "spla_kernels.h"
 #include "spla_rope.h"
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(RotateRows rows, NormS
 // rows at a time where they are fewer; a thread keeps its head and coordinates, so that its sums
 // of g n stay in registers. They are summed over the workgroup's rows (and heads, where one
 // weight serves all) in a fixed order and left as a record of the run. 8192 rows of 40 heads (bf16,
-// d 128, 252 MB): 46.5 us, 5.4 TB/s, and 4.8 for the sum of the runs.
+// d 128, 252 MB) over changing inputs: 59.7 us, 4.2 TB/s, and 4.8 for the sum of the runs.
 template <typename T, int D, int VEC>
 __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, NormSet sa,
                                                                NormSet sb, spla_rope rope,
@@ -214,7 +215,8 @@ __global__ __launch_bounds__(256) void norm_rotate_grad_kernel(RotateRows rows, 
   using Unit = HeadUnit<T, D, VEC>;
   constexpr int UPH = Unit::LANES, E = Unit::E;
   constexpr int kRows = 32;      // at most, of those whose angles are formed at once
-  constexpr int kHeldRows = 16;  // that a thread sums before it turns to fp64
+  constexpr int kHeldRows = 16;  // that a thread sums before it turns to fp64 (in rounds of 1 to 4
+                                 // rows, so 18 at most)
   typedef typename Unit::R R;
   typedef typename Unit::R2 R2;
   __shared__ R2 cs[kRows][D / 2];

@@ -571,9 +571,11 @@ struct TilePass {
       const float w = __builtin_amdgcn_exp2f(KIND == kPlain ? fmaf(y, mul, -rf)
                                              : KIND == kCapped ? y : y - rf);
       sum += w;
-      // weights rounded to bf16 for the product (the sum keeps fp32): 2^-9 of each, beside the
-      // output's own rounding; a second term as in the tiles of 16 rows is half as many products
-      // again (8192 tokens: 764 us against 558)
+      // weights rounded to bf16 for the product (the sum keeps fp32): by 2^-8 of each at most,
+      // beside the output's own rounding by as much (a prompt of 8192 random tokens is off by
+      // 2.2e-3 of its result in the root of the mean square, 1.6e-3 by the output's rounding
+      // alone); a second term as in the tiles of 16 rows is half as many products again (8192
+      // tokens: 764 us against 558)
       if constexpr (TERMS == 1) {
         p[0][(i >> 2) & 1][4 * (i >> 3) + (i & 3)] = (__bf16)w;
       } else {
